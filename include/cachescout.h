@@ -27,6 +27,14 @@
  *                            paged KV (the decode that follows a prefill).
  *   cs_cascade_decode_attn - the same decode with each agent's shared anchor
  *                            attended once for all of its sequences.
+ *   cs_prefill_window_attn,
+ *   cs_decode_window_attn  - both kinds of attention with a sliding window and
+ *                            a few first tokens that stay visible.
+ *   cs_prefill_key_scores,
+ *   cs_decode_attn_scores,
+ *   cs_kv_evict            - the attention weight that every cached key has
+ *                            received, added up per key, and the eviction of
+ *                            a sequence's least attended keys.
  *
  * Conventions shared by all calls
  *   - Every pointer is caller-owned.  The GPU calls allocate no device or
@@ -418,6 +426,218 @@ int cs_cascade_decode_attn_noalloc(const void *q, const void *k_pool, const void
  * count or head_dim. */
 int64_t cs_cascade_decode_workspace_bytes(int32_t batch, int32_t num_q_heads, int32_t head_dim,
                                           int32_t max_shared_len, int32_t max_rest_len);
+
+/*
+ * Prefill attention with a sliding window and sinks.
+ *
+ * Operation (not in the paper, whose attention sees the whole prompt: it
+ * bounds what a long agent history costs per turn): cs_prefill_paged_attn
+ * where a row at prompt position p sees key j <= p only if
+ *
+ *   j > p - window   or   j < sinks,
+ *
+ * i.e. the last `window` positions, its own among them, and the first `sinks`
+ * tokens.  Steps of 64 keys that no row of a tile sees are left out, so a row
+ * costs about window + sinks keys whatever its position.  A window of at least
+ * max_kv_len hides nothing; such a call is cs_prefill_paged_attn_ws.
+ *
+ * Arguments as in cs_prefill_paged_attn_ws, plus
+ *   window         >= 1.
+ *   sinks          >= 0.
+ *   workspace,
+ *   workspace_bytes  as there, sized by cs_prefill_window_workspace_bytes.
+ * A block that no row of the invocation sees, i.e. whose positions are all in
+ * [sinks, P_r - window], may have been recycled: its block_tables entry is not
+ * read and may hold anything, and K and V at single such positions may hold
+ * anything too, NaN included.
+ */
+int cs_prefill_window_attn(const void *q, const void *k_pool, const void *v_pool,
+                           const int32_t *block_tables, const int32_t *prefix_lens,
+                           const int32_t *cu_q_lens, int32_t batch, int32_t total_q,
+                           int32_t max_q_len, int32_t max_kv_len, int32_t max_blocks_per_seq,
+                           int32_t num_blocks, int32_t num_q_heads, int32_t num_kv_heads,
+                           int32_t head_dim, int32_t block_size, float scale, int32_t window,
+                           int32_t sinks, void *workspace, int64_t workspace_bytes, void *out,
+                           cs_stream_t stream);
+
+/* Workspace bytes cs_prefill_window_attn needs, as
+ * cs_prefill_paged_attn_workspace_bytes; also -1 for a window below 1 or
+ * negative sinks. */
+int64_t cs_prefill_window_workspace_bytes(int32_t batch, int32_t total_q, int32_t max_q_len,
+                                          int32_t max_kv_len, int32_t num_q_heads,
+                                          int32_t num_kv_heads, int32_t head_dim, int32_t window,
+                                          int32_t sinks, int32_t num_cus);
+
+/*
+ * Decode attention with a sliding window and sinks: the one-token case of
+ * cs_prefill_window_attn.  The query of sequence r, at position L - 1 with
+ * L = seq_lens[r], sees the keys j >= L - window and j < sinks (j < L).
+ *
+ * Arguments as in cs_paged_decode_attn_ws, except
+ *   seq_lens       each in [0, max_seq_len]; a row with L = 0 (a batch padded to
+ *                  a captured size) gets zeros, and its block table is not read.
+ *   window, sinks  as in cs_prefill_window_attn.
+ *   workspace,
+ *   workspace_bytes  sized by cs_decode_window_workspace_bytes.
+ * Blocks whose positions are all in [sinks, L - window) may have been recycled,
+ * and single such positions may hold anything, as there.
+ */
+int cs_decode_window_attn(const void *q, const void *k_pool, const void *v_pool,
+                          const int32_t *block_tables, const int32_t *seq_lens, int32_t batch,
+                          int32_t max_seq_len, int32_t max_blocks_per_seq, int32_t num_blocks,
+                          int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim,
+                          int32_t block_size, float scale, int32_t window, int32_t sinks,
+                          void *workspace, int64_t workspace_bytes, void *out, cs_stream_t stream);
+
+/* Workspace bytes cs_decode_window_attn needs, as
+ * cs_paged_decode_workspace_bytes; also -1 for a window below 1 or negative
+ * sinks. */
+int64_t cs_decode_window_workspace_bytes(int32_t batch, int32_t max_seq_len, int32_t num_q_heads,
+                                         int32_t num_kv_heads, int32_t head_dim, int32_t window,
+                                         int32_t sinks, int32_t num_cus);
+
+/*
+ * Decode attention that adds every key's attention weight to its score.
+ *
+ * Operation (not in the paper, which evicts whole blocks between agents by
+ * their survival; the scores let cs_kv_evict choose within a sequence): the
+ * decode of cs_paged_decode_attn, and for every sequence r, KV head g and key
+ * j in [score_from[r], L), with p_h the softmax weights of query head h,
+ *
+ *   score(j, g) = (j < L - 1 ? decay * score(j, g) : 0)
+ *                 + sum over the query heads h of g of p_h(j).
+ *
+ * The query's own key L - 1 is new in this step, so its score starts here and
+ * what its slot held before does not matter.  Scores are held in
+ * score_pool[slot][g][position in the block], laid out as the pools are, so
+ * they move with the blocks.  Weights and their sums are fp32.  Keys before
+ * score_from[r] are attended but not scored: a shared anchor's blocks belong to
+ * several sequences.  Every block that holds scored keys must belong to one
+ * sequence of the call alone.  Nothing else in score_pool is changed.
+ *
+ * Arguments as in cs_paged_decode_attn_ws, except
+ *   seq_lens       each in [0, max_seq_len]; a row with L = 0 gets zeros and scores
+ *                  nothing.
+ *   score_from     device, int32 [batch], each >= 0 (at L or beyond: nothing is
+ *                  scored).
+ *   max_scored_len >= every L - score_from[r], <= max_seq_len; sizes the workspace
+ *                  (keys past it would not be scored).
+ *   decay          in [0, 1], else CS_ERR_INVALID_ARG; 1 adds up, less forgets.
+ *   score_pool     device, float [num_blocks][num_kv_heads][block_size], 16-byte
+ *                  aligned.
+ *   workspace,
+ *   workspace_bytes  sized by cs_decode_scores_workspace_bytes: the logits of the
+ *                  scored keys are kept there until the row's softmax is known.
+ */
+int cs_decode_attn_scores(const void *q, const void *k_pool, const void *v_pool,
+                          const int32_t *block_tables, const int32_t *seq_lens,
+                          const int32_t *score_from, int32_t batch, int32_t max_seq_len,
+                          int32_t max_scored_len, int32_t max_blocks_per_seq, int32_t num_blocks,
+                          int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim,
+                          int32_t block_size, float scale, float decay, float *score_pool,
+                          void *workspace, int64_t workspace_bytes, void *out, cs_stream_t stream);
+
+/* Workspace bytes cs_decode_attn_scores needs: those of
+ * cs_paged_decode_attn_ws, and 128 * batch * num_q_heads *
+ * floor((max_scored_len + 62) / 32) (0 for max_scored_len 0).  num_cus as there;
+ * -1 for a negative size, bad head counts, a head_dim other than 64 or 128, or
+ * max_scored_len above max_seq_len. */
+int64_t cs_decode_scores_workspace_bytes(int32_t batch, int32_t max_seq_len, int32_t max_scored_len,
+                                         int32_t num_q_heads, int32_t num_kv_heads,
+                                         int32_t head_dim, int32_t num_cus);
+
+/*
+ * Scores of a prompt: the attention weights that the last rows of every
+ * invocation's suffix give to its keys.
+ *
+ * Operation (the scores of cs_decode_attn_scores after a prefill): for every
+ * invocation r, KV head g and key j in [score_from[r], P + S), with n =
+ * min(rows, S) and p_{i,h} the weights of suffix row i and query head h as in
+ * cs_prefill_paged_attn,
+ *
+ *   score(j, g) = (j < P ? decay * score(j, g) : 0)
+ *                 + sum over S - n <= i < S and the query heads h of g of p_{i,h}(j).
+ *
+ * The suffix's own keys (j >= P) are new, so their scores start here.  An
+ * invocation with S = 0 changes nothing.  Logits are bf16 products with fp32
+ * accumulation; weights and their sums are fp32; there are no atomics, so the
+ * scores are the same from run to run.
+ *
+ * Arguments as in cs_prefill_paged_attn, plus
+ *   score_from     device, int32 [batch], each >= 0.  The blocks that hold scored
+ *                  keys must belong to one invocation of the call alone.
+ *   rows           >= 1: how many of the last suffix rows count; S or more: all.
+ *   decay          in [0, 1], else CS_ERR_INVALID_ARG.
+ *   score_pool     as in cs_decode_attn_scores.
+ *   workspace      device, 16-byte aligned, caller-owned scratch of at least
+ *                  cs_prefill_scores_workspace_bytes(batch, max_q_len,
+ *                  max_kv_len, rows, num_q_heads, num_kv_heads, 0) bytes; calls
+ *                  that share one must be ordered on one stream.
+ *   workspace_bytes  its size; smaller than required -> CS_ERR_INVALID_ARG.
+ * batch == 0, total_q == 0 or max_q_len == 0 is a no-op returning CS_OK.
+ */
+int cs_prefill_key_scores(const void *q, const void *k_pool, const int32_t *block_tables,
+                          const int32_t *prefix_lens, const int32_t *cu_q_lens,
+                          const int32_t *score_from, int32_t batch, int32_t total_q,
+                          int32_t max_q_len, int32_t max_kv_len, int32_t max_blocks_per_seq,
+                          int32_t num_blocks, int32_t num_q_heads, int32_t num_kv_heads,
+                          int32_t head_dim, int32_t block_size, float scale, int32_t rows,
+                          float decay, float *score_pool, void *workspace,
+                          int64_t workspace_bytes, cs_stream_t stream);
+
+/* Workspace bytes cs_prefill_key_scores needs.  num_cus: compute units to size
+ * for, 0 = the current device's (-1 if there is none).  -1 for a negative size,
+ * rows below 1 or bad head counts. */
+int64_t cs_prefill_scores_workspace_bytes(int32_t batch, int32_t max_q_len, int32_t max_kv_len,
+                                          int32_t rows, int32_t num_q_heads, int32_t num_kv_heads,
+                                          int32_t num_cus);
+
+/*
+ * Eviction within sequences by accumulated attention weight.
+ *
+ * Operation: sequence r's own keys are j in [F, L), F = keep_from[r], L =
+ * seq_lens[r]; the keys before F (a shared anchor, the first tokens) stay.  If it
+ * has more than `trigger` of them, every KV head g keeps `budget`: the last
+ * `recent`, and of the others the budget - recent with the largest scores (of
+ * equal scores the lowest j; the two zeros are equal, NaN is below every number).
+ * With k_0 < k_1 < ... the kept keys of head g,
+ *
+ *   kept[r][g][i] = k_i
+ *   K, V and score of head g at position F + i = those at position k_i, 0 <= i < budget
+ *   new_lens[r] = F + budget,
+ *
+ * so the sequence then has new_lens[r] keys and the blocks behind them are free.
+ * Else kept[r][g][0] = -1, new_lens[r] = L and nothing moves.  Attention over the
+ * kept keys is cs_paged_decode_attn's (or any other call's) with the new length:
+ * the keys keep the positions that were encoded into them when they were written.
+ *
+ * Arguments
+ *   score_pool     device, float [num_blocks][num_kv_heads][block_size]; 16-byte
+ *                  aligned, as the pools.
+ *   k_pool, v_pool as in cs_prefill_paged_attn.
+ *   block_tables   device, int32 [batch][max_blocks_per_seq].
+ *   dst_block_tables  where the kept keys go: NULL (or block_tables itself): the
+ *                  sequence's own blocks, those from position F on must then be
+ *                  its alone; else device, int32 [batch][max_blocks_per_seq], whose
+ *                  blocks F / 16 .. (F + budget - 1) / 16 of every sequence that is
+ *                  evicted from are blocks no sequence uses.  In the latter case
+ *                  the keys before F in F's block are copied along, the old blocks
+ *                  are left as they are (sequences may share them), and the caller
+ *                  uses the new table for the sequences with kept[r][0][0] >= 0.
+ *   seq_lens       device, int32 [batch], each in [0, max_seq_len].
+ *   keep_from      device, int32 [batch], each >= 0.
+ *   max_seq_len    max_blocks_per_seq * block_size must be >= max_seq_len.
+ *   budget >= 1, trigger >= budget, recent in [0, budget].
+ *   kept           device, int32 [batch][num_kv_heads][budget].
+ *   new_lens       device, int32 [batch]; may be seq_lens itself.
+ * batch == 0 is a no-op returning CS_OK.
+ */
+int cs_kv_evict(float *score_pool, void *k_pool, void *v_pool, const int32_t *block_tables,
+                const int32_t *dst_block_tables, const int32_t *seq_lens,
+                const int32_t *keep_from, int32_t batch, int32_t max_seq_len,
+                int32_t max_blocks_per_seq, int32_t num_blocks, int32_t num_kv_heads,
+                int32_t head_dim, int32_t block_size, int32_t budget, int32_t trigger,
+                int32_t recent, int32_t *kept, int32_t *new_lens, cs_stream_t stream);
 
 /*
  * KV write-back: store the K/V rows of new tokens into their pool slots.

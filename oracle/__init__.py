@@ -39,6 +39,12 @@ values, closed forms, breadth-first distances against all-pairs shortest
 paths, the exact survival probability by path enumeration, and planted
 mistakes (``tests/test_control_plane_oracle.py``).
 
+The operators that bound a sequence's cache (attention with a sliding window
+and sinks, the weights that keys receive, eviction by them) are outside the
+paper; ``bounded_cache.py`` evaluates their definitions in float64, pinned to
+the attention oracle and to scalar loops, with planted mistakes
+(``tests/test_bounded_cache_oracle.py``).
+
 Every function here is pinned; none is "parity unpinned".  The full
 attention oracle is pinned by the brute force, the invariants, the closed
 forms and the golden case (``tests/test_oracle_*.py``); the row-by-row
@@ -59,3 +65,9 @@ from .paged_attention import (  # noqa: F401
 from .prefetch import kv_prefetch  # noqa: F401
 from .kv_copy import kv_offload, kv_write  # noqa: F401
 from .brute import brute_attention_rows  # noqa: F401
+from .bounded_cache import (  # noqa: F401
+    add_key_scores,
+    evict,
+    window_attention,
+    window_weights,
+)

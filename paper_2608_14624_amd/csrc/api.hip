@@ -90,7 +90,7 @@ hipError_t copy_to_host(std::vector<T>& dst, const T* src, size_t count, hipStre
 
 int debug_check_attn(const int32_t* block_tables, const int32_t* prefix_lens,
                      const int32_t* cu_q_lens, int batch, int total_q, int max_q_len,
-                     int max_kv_len, int max_blocks_per_seq, int num_blocks,
+                     int max_kv_len, int max_blocks_per_seq, int num_blocks, const cs::Window& win,
                      hipStream_t stream) {
   std::vector<int32_t> cu, pl, bt;
   hipError_t e = copy_to_host(cu, cu_q_lens, (size_t)batch + 1, stream);
@@ -110,6 +110,7 @@ int debug_check_attn(const int32_t* block_tables, const int32_t* prefix_lens,
       return fail(CS_ERR_INVALID_ARG, "P_%d + S_%d = %lld exceeds max_kv_len %d", r, r, len, max_kv_len);
     const long long nb = (len + 15) / 16;
     for (long long b = 0; b < nb; ++b) {
+      if (win.hides(16 * b, pl[r])) continue;
       const int32_t slot = bt[(size_t)r * max_blocks_per_seq + b];
       if (slot < 0 || slot >= num_blocks)
         return fail(CS_ERR_INVALID_ARG, "block_tables[%d][%lld] = %d outside [0, %d)", r, b, slot, num_blocks);
@@ -158,19 +159,79 @@ int debug_check_block_ids(const int32_t* ids_d, int n, int num_blocks, hipStream
 }
 
 int debug_check_decode(const int32_t* block_tables, const int32_t* seq_lens, int batch,
-                       int max_seq_len, int max_blocks_per_seq, int num_blocks,
-                       hipStream_t stream) {
+                       int max_seq_len, int max_blocks_per_seq, int num_blocks, int min_len,
+                       const cs::Window& win, hipStream_t stream) {
   std::vector<int32_t> sl, bt;
   hipError_t e = copy_to_host(sl, seq_lens, (size_t)batch, stream);
   if (e == hipSuccess) e = copy_to_host(bt, block_tables, (size_t)batch * max_blocks_per_seq, stream);
   if (e != hipSuccess) return hip_fail(e, "CS_DEBUG_CHECK metadata copy");
   for (int r = 0; r < batch; ++r) {
-    if (sl[r] < 1 || sl[r] > max_seq_len)
-      return fail(CS_ERR_INVALID_ARG, "seq_lens[%d] = %d outside [1, %d]", r, sl[r], max_seq_len);
+    if (sl[r] < min_len || sl[r] > max_seq_len)
+      return fail(CS_ERR_INVALID_ARG, "seq_lens[%d] = %d outside [%d, %d]", r, sl[r], min_len, max_seq_len);
     for (int b = 0; b < (sl[r] + 15) / 16; ++b) {
+      if (win.hides(16LL * b, sl[r] - 1)) continue;
       const int32_t slot = bt[(size_t)r * max_blocks_per_seq + b];
       if (slot < 0 || slot >= num_blocks)
         return fail(CS_ERR_INVALID_ARG, "block_tables[%d][%d] = %d outside [0, %d)", r, b, slot, num_blocks);
+    }
+  }
+  return CS_OK;
+}
+
+// Every key from keep[r] on lies in a block of one sequence alone (scores are added
+// without atomics, and an eviction moves keys).
+int debug_check_private(const int32_t* block_tables, const std::vector<int32_t>& lens, const int32_t* keep_d,
+                        const char* what, int batch, int max_blocks_per_seq, int num_blocks, hipStream_t stream) {
+  std::vector<int32_t> from, bt;
+  hipError_t e = copy_to_host(from, keep_d, (size_t)batch, stream);
+  if (e == hipSuccess) e = copy_to_host(bt, block_tables, (size_t)batch * max_blocks_per_seq, stream);
+  if (e != hipSuccess) return hip_fail(e, "CS_DEBUG_CHECK metadata copy");
+  std::vector<unsigned char> seen((size_t)num_blocks, 0);
+  for (int r = 0; r < batch; ++r) {
+    if (from[r] < 0) return fail(CS_ERR_INVALID_ARG, "%s[%d] = %d is negative", what, r, from[r]);
+    for (int b = from[r] / 16; b < (lens[r] + 15) / 16; ++b) {
+      const int32_t slot = bt[(size_t)r * max_blocks_per_seq + b];
+      if (slot < 0 || slot >= num_blocks)
+        return fail(CS_ERR_INVALID_ARG, "block_tables[%d][%d] = %d outside [0, %d)", r, b, slot, num_blocks);
+      if (seen[slot])
+        return fail(CS_ERR_INVALID_ARG, "block %d holds keys past %s of two places (sequence %d)", slot, what, r);
+      seen[slot] = 1;
+    }
+  }
+  return CS_OK;
+}
+
+int debug_check_evict(const int32_t* block_tables, const int32_t* dst_tables, const int32_t* seq_lens,
+                      const int32_t* keep_from, int batch, int max_seq_len, int max_blocks_per_seq, int num_blocks,
+                      int budget, int trigger, hipStream_t stream) {
+  std::vector<int32_t> sl, from, dt;
+  hipError_t e = copy_to_host(sl, seq_lens, (size_t)batch, stream);
+  if (e == hipSuccess) e = copy_to_host(from, keep_from, (size_t)batch, stream);
+  if (e == hipSuccess && dst_tables) e = copy_to_host(dt, dst_tables, (size_t)batch * max_blocks_per_seq, stream);
+  if (e != hipSuccess) return hip_fail(e, "CS_DEBUG_CHECK metadata copy");
+  for (int r = 0; r < batch; ++r)
+    if (sl[r] < 0 || sl[r] > max_seq_len)
+      return fail(CS_ERR_INVALID_ARG, "seq_lens[%d] = %d outside [0, %d]", r, sl[r], max_seq_len);
+  int st = debug_check_private(block_tables, sl, keep_from, "keep_from", batch, max_blocks_per_seq, num_blocks, stream);
+  if (st != CS_OK || !dst_tables) return st;
+  // the new blocks: different, and none that a sequence's keys past keep_from lie in
+  std::vector<int32_t> bt;
+  e = copy_to_host(bt, block_tables, (size_t)batch * max_blocks_per_seq, stream);
+  if (e != hipSuccess) return hip_fail(e, "CS_DEBUG_CHECK metadata copy");
+  std::vector<unsigned char> seen((size_t)num_blocks, 0);
+  for (int r = 0; r < batch; ++r)
+    for (int b = 0; b < (sl[r] + 15) / 16; ++b) {
+      const int32_t slot = bt[(size_t)r * max_blocks_per_seq + b];
+      if (slot >= 0 && slot < num_blocks) seen[slot] = 1;
+    }
+  for (int r = 0; r < batch; ++r) {
+    if (sl[r] - from[r] <= trigger) continue;
+    for (int b = from[r] / 16; b < (from[r] + budget + 15) / 16; ++b) {
+      const int32_t slot = dt[(size_t)r * max_blocks_per_seq + b];
+      if (slot < 0 || slot >= num_blocks)
+        return fail(CS_ERR_INVALID_ARG, "dst_block_tables[%d][%d] = %d outside [0, %d)", r, b, slot, num_blocks);
+      if (seen[slot]) return fail(CS_ERR_INVALID_ARG, "dst_block_tables[%d][%d] = %d is in use", r, b, slot);
+      seen[slot] = 1;
     }
   }
   return CS_OK;
@@ -286,6 +347,27 @@ int64_t decode_range_bytes(const cs::DecodeGeometry& geo, int32_t num_q_heads, i
          (int64_t)sizeof(int2);
 }
 
+// What a decode call asks for beyond cs_paged_decode_attn's: a window (cs_decode_window_attn),
+// or attention weights added to scores (cs_decode_attn_scores)
+struct DecodeExtras {
+  cs::Window win = {};
+  const int32_t* score_from = nullptr;
+  float* score_pool = nullptr;
+  int max_scored_len = 0;
+  float decay = 0.f;
+  bool empty_rows() const { return win.size > 0 || score_pool != nullptr; }
+};
+
+// 32-key units that hold the keys from a sequence's first scored one to its end
+int64_t scored_units(int32_t max_scored_len) {
+  return max_scored_len > 0 ? ((int64_t)max_scored_len + 62) / 32 : 0;
+}
+
+// Workspace bytes of the kept logits
+int64_t logit_bytes(int32_t batch, int32_t max_scored_len, int32_t num_q_heads) {
+  return (int64_t)batch * num_q_heads * scored_units(max_scored_len) * 32 * (int64_t)sizeof(float);
+}
+
 // cs_paged_decode_attn, and with a workspace (has_ws) the variant whose
 // launches deal their keys out in ranges
 int paged_decode(const void* q, const void* k_pool, const void* v_pool,
@@ -293,7 +375,7 @@ int paged_decode(const void* q, const void* k_pool, const void* v_pool,
                  int32_t max_seq_len, int32_t max_blocks_per_seq, int32_t num_blocks,
                  int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim, int32_t block_size,
                  float scale, bool has_ws, void* workspace, int64_t workspace_bytes, void* out,
-                 cs_stream_t stream) {
+                 cs_stream_t stream, const DecodeExtras& extra = {}) {
   bool noop;
   int st0 = validate_decode(q, k_pool, v_pool, block_tables, seq_lens, batch, max_seq_len,
                             max_blocks_per_seq, num_blocks, num_q_heads, num_kv_heads, head_dim,
@@ -302,12 +384,13 @@ int paged_decode(const void* q, const void* k_pool, const void* v_pool,
   if (has_ws && workspace_bytes < 0) return fail(CS_ERR_INVALID_ARG, "negative workspace_bytes");
   if (noop) return ok();
   cs::DecodeGeometry geo = {};
+  const int64_t logits = extra.score_pool ? logit_bytes(batch, extra.max_scored_len, num_q_heads) : 0;
   if (has_ws) {
     int cus = 0;
     hipError_t ecu = cs::current_device_cus(&cus);
     if (ecu != hipSuccess) return hip_fail(ecu, "compute-unit count of the current device");
-    geo = cs::decode_geometry(batch, max_seq_len, num_kv_heads, head_dim, cus);
-    const int64_t need = decode_range_bytes(geo, num_q_heads, head_dim);
+    geo = cs::decode_geometry(batch, extra.win.visible(max_seq_len, 1, 32), num_kv_heads, head_dim, cus);
+    const int64_t need = logits + decode_range_bytes(geo, num_q_heads, head_dim);
     if (need > 0) {
       if (!workspace || !aligned16(workspace))
         return fail(CS_ERR_INVALID_ARG, "workspace must be a 16-byte aligned device buffer");
@@ -320,7 +403,14 @@ int paged_decode(const void* q, const void* k_pool, const void* v_pool,
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   if (debug_checks_enabled()) {
     int st = debug_check_decode(block_tables, seq_lens, batch, max_seq_len, max_blocks_per_seq,
-                                num_blocks, s);
+                                num_blocks, extra.empty_rows() ? 0 : 1, extra.win, s);
+    if (st == CS_OK && extra.score_pool) {
+      std::vector<int32_t> sl;
+      hipError_t e = copy_to_host(sl, seq_lens, (size_t)batch, s);
+      if (e != hipSuccess) return hip_fail(e, "CS_DEBUG_CHECK metadata copy");
+      st = debug_check_private(block_tables, sl, extra.score_from, "score_from", batch, max_blocks_per_seq,
+                               num_blocks, s);
+    }
     if (st != CS_OK) return st;
   }
   cs::DecodeLaunch a;
@@ -339,7 +429,13 @@ int paged_decode(const void* q, const void* k_pool, const void* v_pool,
   a.ranges = geo.ranges;
   a.aligned_ranges = geo.aligned_ranges;
   a.slots = geo.slots;
-  a.workspace = geo.ranges > 0 ? workspace : nullptr;
+  a.workspace = geo.ranges > 0 ? static_cast<char*>(workspace) + logits : nullptr;
+  a.win = extra.win;
+  a.score_from = extra.score_from;
+  a.score_pool = extra.score_pool;
+  a.decay = extra.decay;
+  a.logits = logits > 0 ? static_cast<float*>(workspace) : nullptr;
+  a.logit_units = (int)scored_units(extra.max_scored_len);
   hipError_t e = cs::launch_paged_decode_attn(a, s);
   if (e != hipSuccess) return hip_fail(e, "paged_decode_attn launch");
   return ok();
@@ -357,6 +453,14 @@ int64_t key_part_bytes(const cs::AttnGeometry& geo, int32_t total_q, int32_t num
   return (int64_t)geo.parts * total_q * num_q_heads * (head_dim + 2) * (int64_t)sizeof(float);
 }
 
+// Geometry of a prefill launch: under a window its tiles' key steps are those in sight
+cs::AttnGeometry prefill_geometry(int32_t batch, int32_t max_q_len, int32_t max_kv_len, const cs::Window& win,
+                                  int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim, int cus,
+                                  bool allow_parts) {
+  return cs::attn_geometry(batch, max_q_len, win.visible(max_kv_len, max_q_len < 128 ? max_q_len : 128, 64),
+                           num_q_heads, num_kv_heads, head_dim, cus, allow_parts);
+}
+
 // cs_prefill_paged_attn, and with a workspace (has_ws) the variant whose
 // launches that would leave CUs idle split their keys into parts
 int prefill_paged_attn(const void* q, const void* k_pool, const void* v_pool,
@@ -365,7 +469,7 @@ int prefill_paged_attn(const void* q, const void* k_pool, const void* v_pool,
                        int32_t max_kv_len, int32_t max_blocks_per_seq, int32_t num_blocks,
                        int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim,
                        int32_t block_size, float scale, bool has_ws, void* workspace,
-                       int64_t workspace_bytes, void* out, cs_stream_t stream) {
+                       int64_t workspace_bytes, void* out, cs_stream_t stream, const cs::Window& win = {}) {
   if (batch < 0 || total_q < 0 || max_q_len < 0 || max_kv_len < 0 || max_blocks_per_seq < 0 ||
       num_blocks < 0)
     return fail(CS_ERR_INVALID_ARG, "negative size argument");
@@ -392,8 +496,8 @@ int prefill_paged_attn(const void* q, const void* k_pool, const void* v_pool,
   int cus = 0;
   hipError_t ecu = cs::current_device_cus(&cus);
   if (ecu != hipSuccess) return hip_fail(ecu, "compute-unit count of the current device");
-  const cs::AttnGeometry geo = cs::attn_geometry(batch, max_q_len, max_kv_len, num_q_heads,
-                                                 num_kv_heads, head_dim, cus, has_ws);
+  const cs::AttnGeometry geo = prefill_geometry(batch, max_q_len, max_kv_len, win, num_q_heads,
+                                                num_kv_heads, head_dim, cus, has_ws);
   if (geo.grid > 0x7fffffffLL) return fail(CS_ERR_INVALID_ARG, "launch too large");
   const int64_t need = key_part_bytes(geo, total_q, num_q_heads, head_dim);
   if (need > 0) {
@@ -407,7 +511,7 @@ int prefill_paged_attn(const void* q, const void* k_pool, const void* v_pool,
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   if (debug_checks_enabled()) {
     int st = debug_check_attn(block_tables, prefix_lens, cu_q_lens, batch, total_q, max_q_len,
-                              max_kv_len, max_blocks_per_seq, num_blocks, s);
+                              max_kv_len, max_blocks_per_seq, num_blocks, win, s);
     if (st != CS_OK) return st;
   }
   cs::AttnLaunch a;
@@ -426,12 +530,37 @@ int prefill_paged_attn(const void* q, const void* k_pool, const void* v_pool,
   a.head_dim = head_dim;
   a.scale = scale;
   a.cus = cus;
-  a.max_kv_len = max_kv_len;
   a.total_q = total_q;
   a.workspace = need > 0 ? workspace : nullptr;
-  hipError_t e = cs::launch_prefill_paged_attn(a, s);
+  a.win = win;
+  hipError_t e = cs::launch_prefill_paged_attn(a, geo, s);
   if (e != hipSuccess) return hip_fail(e, "prefill_paged_attn launch");
   return ok();
+}
+
+
+// The window that a call asks for; none where it hides nothing
+int checked_window(int32_t window, int32_t sinks, int32_t max_kv_len, cs::Window* win) {
+  if (window < 1 || sinks < 0)
+    return fail(CS_ERR_INVALID_ARG, "window %d must be positive, sinks %d not negative", window, sinks);
+  *win = cs::Window{};
+  if (window < max_kv_len) *win = cs::Window{window, sinks < max_kv_len ? sinks : max_kv_len};
+  return CS_OK;
+}
+
+int64_t prefill_workspace_bytes(int32_t batch, int32_t total_q, int32_t max_q_len, int32_t max_kv_len,
+                                const cs::Window& win, int32_t num_q_heads, int32_t num_kv_heads,
+                                int32_t head_dim, int32_t num_cus) {
+  if (batch < 0 || total_q < 0 || max_q_len < 0 || max_kv_len < 0 || num_cus < 0 ||
+      num_q_heads <= 0 || num_kv_heads <= 0 || num_q_heads % num_kv_heads != 0 ||
+      (head_dim != 64 && head_dim != 128))
+    return -1;
+  if (batch == 0 || total_q == 0 || max_q_len == 0) return 0;
+  int cus = num_cus;
+  if (cus == 0 && cs::current_device_cus(&cus) != hipSuccess) return -1;
+  const cs::AttnGeometry geo = prefill_geometry(batch, max_q_len, max_kv_len, win, num_q_heads,
+                                                num_kv_heads, head_dim, cus, true);
+  return key_part_bytes(geo, total_q, num_q_heads, head_dim);
 }
 
 }  // namespace
@@ -521,7 +650,7 @@ int cascade_decode(const void* q, const void* k_pool, const void* v_pool,
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   if (!use_scratch && debug_checks_enabled()) {
     int st = debug_check_decode(block_tables, seq_lens, batch, max_seq_len, max_blocks_per_seq,
-                                num_blocks, s);
+                                num_blocks, 1, cs::Window{}, s);
     if (st == CS_OK)
       st = debug_check_groups(block_tables, seq_lens, cu_groups, shared_lens, batch, num_groups,
                               max_group_seqs, max_shared_len, max_rest_len, max_blocks_per_seq, s);
@@ -618,16 +747,230 @@ int64_t cs_prefill_paged_attn_workspace_bytes(int32_t batch, int32_t total_q, in
                                               int32_t max_kv_len, int32_t num_q_heads,
                                               int32_t num_kv_heads, int32_t head_dim,
                                               int32_t num_cus) {
-  if (batch < 0 || total_q < 0 || max_q_len < 0 || max_kv_len < 0 || num_cus < 0 ||
-      num_q_heads <= 0 || num_kv_heads <= 0 || num_q_heads % num_kv_heads != 0 ||
-      (head_dim != 64 && head_dim != 128))
+  return prefill_workspace_bytes(batch, total_q, max_q_len, max_kv_len, cs::Window{}, num_q_heads, num_kv_heads,
+                                 head_dim, num_cus);
+}
+
+int cs_prefill_window_attn(const void* q, const void* k_pool, const void* v_pool, const int32_t* block_tables,
+                           const int32_t* prefix_lens, const int32_t* cu_q_lens, int32_t batch, int32_t total_q,
+                           int32_t max_q_len, int32_t max_kv_len, int32_t max_blocks_per_seq, int32_t num_blocks,
+                           int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim, int32_t block_size,
+                           float scale, int32_t window, int32_t sinks, void* workspace, int64_t workspace_bytes,
+                           void* out, cs_stream_t stream) {
+  cs::Window win;
+  const int st = checked_window(window, sinks, max_kv_len, &win);
+  if (st != CS_OK) return st;
+  return prefill_paged_attn(q, k_pool, v_pool, block_tables, prefix_lens, cu_q_lens, batch, total_q, max_q_len,
+                            max_kv_len, max_blocks_per_seq, num_blocks, num_q_heads, num_kv_heads, head_dim,
+                            block_size, scale, true, workspace, workspace_bytes, out, stream, win);
+}
+
+int64_t cs_prefill_window_workspace_bytes(int32_t batch, int32_t total_q, int32_t max_q_len, int32_t max_kv_len,
+                                          int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim,
+                                          int32_t window, int32_t sinks, int32_t num_cus) {
+  cs::Window win;
+  if (max_kv_len < 0 || checked_window(window, sinks, max_kv_len, &win) != CS_OK) return -1;
+  return prefill_workspace_bytes(batch, total_q, max_q_len, max_kv_len, win, num_q_heads, num_kv_heads, head_dim,
+                                 num_cus);
+}
+
+int cs_decode_window_attn(const void* q, const void* k_pool, const void* v_pool, const int32_t* block_tables,
+                          const int32_t* seq_lens, int32_t batch, int32_t max_seq_len, int32_t max_blocks_per_seq,
+                          int32_t num_blocks, int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim,
+                          int32_t block_size, float scale, int32_t window, int32_t sinks, void* workspace,
+                          int64_t workspace_bytes, void* out, cs_stream_t stream) {
+  DecodeExtras extra;
+  if (window < 1 || sinks < 0) return fail(CS_ERR_INVALID_ARG, "window %d must be positive, sinks %d not negative", window, sinks);
+  // (kept where it hides nothing too: these calls allow empty sequences)
+  extra.win.size = window < max_seq_len || max_seq_len <= 0 ? window : max_seq_len;
+  extra.win.sinks = sinks < max_seq_len || max_seq_len <= 0 ? sinks : max_seq_len;
+  return paged_decode(q, k_pool, v_pool, block_tables, seq_lens, batch, max_seq_len, max_blocks_per_seq, num_blocks,
+                      num_q_heads, num_kv_heads, head_dim, block_size, scale, true, workspace, workspace_bytes, out,
+                      stream, extra);
+}
+
+int64_t cs_decode_window_workspace_bytes(int32_t batch, int32_t max_seq_len, int32_t num_q_heads,
+                                         int32_t num_kv_heads, int32_t head_dim, int32_t window, int32_t sinks,
+                                         int32_t num_cus) {
+  if (window < 1 || sinks < 0 || max_seq_len < 0) return -1;
+  const cs::Window win = {window, sinks};
+  return cs_paged_decode_workspace_bytes(batch, win.visible(max_seq_len, 1, 32), num_q_heads, num_kv_heads,
+                                         head_dim, num_cus);
+}
+
+int cs_decode_attn_scores(const void* q, const void* k_pool, const void* v_pool, const int32_t* block_tables,
+                          const int32_t* seq_lens, const int32_t* score_from, int32_t batch, int32_t max_seq_len,
+                          int32_t max_scored_len, int32_t max_blocks_per_seq, int32_t num_blocks,
+                          int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim, int32_t block_size,
+                          float scale, float decay, float* score_pool, void* workspace, int64_t workspace_bytes,
+                          void* out, cs_stream_t stream) {
+  if (batch < 0 || max_seq_len < 0 || max_scored_len < 0) return fail(CS_ERR_INVALID_ARG, "negative size argument");
+  if (max_scored_len > max_seq_len)
+    return fail(CS_ERR_INVALID_ARG, "max_scored_len %d exceeds max_seq_len %d", max_scored_len, max_seq_len);
+  if (!(decay >= 0.f && decay <= 1.f)) return fail(CS_ERR_INVALID_ARG, "decay %g outside [0, 1]", (double)decay);
+  if (batch > 0 && (!score_from || !score_pool)) return fail(CS_ERR_INVALID_ARG, "null pointer argument");
+  if (!aligned16(score_pool)) return fail(CS_ERR_INVALID_ARG, "score_pool must be 16-byte aligned");
+  if (num_q_heads > 0 && num_kv_heads > 0 &&
+      (long long)batch * num_kv_heads * (1 + (scored_units(max_scored_len) + 63) / 64) > 0x7fffffffLL)
+    return fail(CS_ERR_INVALID_ARG, "launch too large");
+  DecodeExtras extra;
+  extra.score_from = score_from;
+  extra.score_pool = score_pool;
+  extra.max_scored_len = max_scored_len;
+  extra.decay = decay;
+  return paged_decode(q, k_pool, v_pool, block_tables, seq_lens, batch, max_seq_len, max_blocks_per_seq, num_blocks,
+                      num_q_heads, num_kv_heads, head_dim, block_size, scale, true, workspace, workspace_bytes, out,
+                      stream, extra);
+}
+
+int64_t cs_decode_scores_workspace_bytes(int32_t batch, int32_t max_seq_len, int32_t max_scored_len,
+                                         int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim,
+                                         int32_t num_cus) {
+  if (max_scored_len < 0 || max_scored_len > max_seq_len) return -1;
+  const int64_t ranges = cs_paged_decode_workspace_bytes(batch, max_seq_len, num_q_heads, num_kv_heads, head_dim,
+                                                         num_cus);
+  return ranges < 0 ? -1 : ranges + logit_bytes(batch, max_scored_len, num_q_heads);
+}
+
+int cs_prefill_key_scores(const void* q, const void* k_pool, const int32_t* block_tables,
+                          const int32_t* prefix_lens, const int32_t* cu_q_lens, const int32_t* score_from,
+                          int32_t batch, int32_t total_q, int32_t max_q_len, int32_t max_kv_len,
+                          int32_t max_blocks_per_seq, int32_t num_blocks, int32_t num_q_heads,
+                          int32_t num_kv_heads, int32_t head_dim, int32_t block_size, float scale, int32_t rows,
+                          float decay, float* score_pool, void* workspace, int64_t workspace_bytes,
+                          cs_stream_t stream) {
+  if (batch < 0 || total_q < 0 || max_q_len < 0 || max_kv_len < 0 || max_blocks_per_seq < 0 || num_blocks < 0 ||
+      workspace_bytes < 0)
+    return fail(CS_ERR_INVALID_ARG, "negative size argument");
+  if (num_q_heads <= 0 || num_kv_heads <= 0 || head_dim <= 0 || block_size <= 0)
+    return fail(CS_ERR_INVALID_ARG, "head counts, head_dim and block_size must be positive");
+  if (num_q_heads % num_kv_heads != 0)
+    return fail(CS_ERR_INVALID_ARG, "num_q_heads %d is not a multiple of num_kv_heads %d", num_q_heads, num_kv_heads);
+  if (head_dim != 64 && head_dim != 128)
+    return fail(CS_ERR_UNSUPPORTED, "head_dim %d (supported: 64, 128)", head_dim);
+  if (block_size != 16) return fail(CS_ERR_UNSUPPORTED, "block_size %d (supported: 16)", block_size);
+  if (!isfinite(scale)) return fail(CS_ERR_INVALID_ARG, "scale is not finite");
+  if (!(scale > 0.f)) return fail(CS_ERR_UNSUPPORTED, "scale %g (supported: > 0)", (double)scale);
+  if (rows < 1) return fail(CS_ERR_INVALID_ARG, "rows %d must be positive", rows);
+  if (!(decay >= 0.f && decay <= 1.f)) return fail(CS_ERR_INVALID_ARG, "decay %g outside [0, 1]", (double)decay);
+  if (batch == 0 || total_q == 0 || max_q_len == 0) return ok();
+  if (!q || !k_pool || !block_tables || !prefix_lens || !cu_q_lens || !score_from || !score_pool)
+    return fail(CS_ERR_INVALID_ARG, "null pointer argument");
+  if (num_blocks == 0) return fail(CS_ERR_INVALID_ARG, "num_blocks is 0");
+  if (max_q_len > max_kv_len) return fail(CS_ERR_INVALID_ARG, "max_q_len exceeds max_kv_len");
+  if ((long long)max_blocks_per_seq * block_size < max_kv_len)
+    return fail(CS_ERR_INVALID_ARG, "max_blocks_per_seq * block_size < max_kv_len");
+  if (!aligned16(q) || !aligned16(k_pool) || !aligned16(score_pool))
+    return fail(CS_ERR_INVALID_ARG, "q, k_pool and score_pool must be 16-byte aligned");
+  int cus = 0;
+  hipError_t e = cs::current_device_cus(&cus);
+  if (e != hipSuccess) return hip_fail(e, "compute-unit count of the current device");
+  cs::KeyScoreLaunch a;
+  a.geo = cs::key_score_geometry(batch, max_q_len, max_kv_len, rows, num_q_heads, num_kv_heads, cus);
+  if (a.geo.stat_grid > 0x7fffffffLL || a.geo.weight_grid > 0x7fffffffLL)
+    return fail(CS_ERR_INVALID_ARG, "launch too large");
+  if (!workspace || !aligned16(workspace))
+    return fail(CS_ERR_INVALID_ARG, "workspace must be a 16-byte aligned device buffer");
+  if (workspace_bytes < a.geo.stat_bytes)
+    return fail(CS_ERR_INVALID_ARG, "workspace_bytes %lld < %lld required", (long long)workspace_bytes,
+                (long long)a.geo.stat_bytes);
+  hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+  if (debug_checks_enabled()) {
+    int st = debug_check_attn(block_tables, prefix_lens, cu_q_lens, batch, total_q, max_q_len, max_kv_len,
+                              max_blocks_per_seq, num_blocks, cs::Window{}, s);
+    if (st != CS_OK) return st;
+    std::vector<int32_t> cu, lens;
+    e = copy_to_host(cu, cu_q_lens, (size_t)batch + 1, s);
+    if (e == hipSuccess) e = copy_to_host(lens, prefix_lens, (size_t)batch, s);
+    if (e != hipSuccess) return hip_fail(e, "CS_DEBUG_CHECK metadata copy");
+    for (int r = 0; r < batch; ++r) lens[r] += cu[r + 1] - cu[r];
+    st = debug_check_private(block_tables, lens, score_from, "score_from", batch, max_blocks_per_seq, num_blocks, s);
+    if (st != CS_OK) return st;
+  }
+  a.q = static_cast<const uint16_t*>(q);
+  a.k_pool = static_cast<const uint16_t*>(k_pool);
+  a.block_tables = block_tables;
+  a.prefix_lens = prefix_lens;
+  a.cu_q_lens = cu_q_lens;
+  a.score_from = score_from;
+  a.score_pool = score_pool;
+  a.workspace = workspace;
+  a.batch = batch;
+  a.max_blocks_per_seq = max_blocks_per_seq;
+  a.rows = rows;
+  a.num_q_heads = num_q_heads;
+  a.num_kv_heads = num_kv_heads;
+  a.head_dim = head_dim;
+  a.scale = scale;
+  a.decay = decay;
+  e = cs::launch_key_scores(a, s);
+  if (e != hipSuccess) return hip_fail(e, "key_scores launch");
+  return ok();
+}
+
+int64_t cs_prefill_scores_workspace_bytes(int32_t batch, int32_t max_q_len, int32_t max_kv_len, int32_t rows,
+                                          int32_t num_q_heads, int32_t num_kv_heads, int32_t num_cus) {
+  if (batch < 0 || max_q_len < 0 || max_kv_len < 0 || rows < 1 || num_cus < 0 || num_q_heads <= 0 ||
+      num_kv_heads <= 0 || num_q_heads % num_kv_heads != 0)
     return -1;
-  if (batch == 0 || total_q == 0 || max_q_len == 0) return 0;
+  if (batch == 0 || max_q_len == 0) return 0;
   int cus = num_cus;
   if (cus == 0 && cs::current_device_cus(&cus) != hipSuccess) return -1;
-  const cs::AttnGeometry geo = cs::attn_geometry(batch, max_q_len, max_kv_len, num_q_heads,
-                                                 num_kv_heads, head_dim, cus, true);
-  return key_part_bytes(geo, total_q, num_q_heads, head_dim);
+  return cs::key_score_geometry(batch, max_q_len, max_kv_len, rows, num_q_heads, num_kv_heads, cus).stat_bytes;
+}
+
+int cs_kv_evict(float* score_pool, void* k_pool, void* v_pool, const int32_t* block_tables,
+                const int32_t* dst_block_tables, const int32_t* seq_lens, const int32_t* keep_from, int32_t batch,
+                int32_t max_seq_len, int32_t max_blocks_per_seq, int32_t num_blocks, int32_t num_kv_heads,
+                int32_t head_dim, int32_t block_size, int32_t budget, int32_t trigger, int32_t recent,
+                int32_t* kept, int32_t* new_lens, cs_stream_t stream) {
+  if (batch < 0 || max_seq_len < 0 || max_blocks_per_seq < 0 || num_blocks < 0)
+    return fail(CS_ERR_INVALID_ARG, "negative size argument");
+  if (num_kv_heads <= 0 || head_dim <= 0 || block_size <= 0)
+    return fail(CS_ERR_INVALID_ARG, "num_kv_heads, head_dim and block_size must be positive");
+  if (head_dim != 64 && head_dim != 128)
+    return fail(CS_ERR_UNSUPPORTED, "head_dim %d (supported: 64, 128)", head_dim);
+  if (block_size != 16) return fail(CS_ERR_UNSUPPORTED, "block_size %d (supported: 16)", block_size);
+  if (budget < 1) return fail(CS_ERR_INVALID_ARG, "budget %d must be positive", budget);
+  if (trigger < budget) return fail(CS_ERR_INVALID_ARG, "trigger %d is less than budget %d", trigger, budget);
+  if (recent < 0 || recent > budget) return fail(CS_ERR_INVALID_ARG, "recent %d outside [0, budget = %d]", recent, budget);
+  if (batch == 0) return ok();
+  if (!score_pool || !k_pool || !v_pool || !block_tables || !seq_lens || !keep_from || !kept || !new_lens)
+    return fail(CS_ERR_INVALID_ARG, "null pointer argument");
+  if (num_blocks == 0) return fail(CS_ERR_INVALID_ARG, "num_blocks is 0");
+  if ((long long)max_blocks_per_seq * block_size < max_seq_len)
+    return fail(CS_ERR_INVALID_ARG, "max_blocks_per_seq * block_size < max_seq_len");
+  if (!aligned16(score_pool) || !aligned16(k_pool) || !aligned16(v_pool))
+    return fail(CS_ERR_INVALID_ARG, "the pools must be 16-byte aligned");
+  if ((long long)batch * num_kv_heads * ((budget + 15LL + 63) / 64 + 33) > 0x7fffffffLL)
+    return fail(CS_ERR_INVALID_ARG, "launch too large");
+  hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+  if (dst_block_tables == block_tables) dst_block_tables = nullptr;
+  if (debug_checks_enabled()) {
+    int st = debug_check_evict(block_tables, dst_block_tables, seq_lens, keep_from, batch, max_seq_len,
+                               max_blocks_per_seq, num_blocks, budget, trigger, s);
+    if (st != CS_OK) return st;
+  }
+  cs::EvictLaunch a;
+  a.score_pool = score_pool;
+  a.k_pool = static_cast<uint16_t*>(k_pool);
+  a.v_pool = static_cast<uint16_t*>(v_pool);
+  a.block_tables = block_tables;
+  a.dst_tables = dst_block_tables;
+  a.seq_lens = seq_lens;
+  a.keep_from = keep_from;
+  a.kept = kept;
+  a.new_lens = new_lens;
+  a.batch = batch;
+  a.max_blocks_per_seq = max_blocks_per_seq;
+  a.num_kv_heads = num_kv_heads;
+  a.head_dim = head_dim;
+  a.budget = budget;
+  a.trigger = trigger;
+  a.recent = recent;
+  hipError_t e = cs::launch_kv_evict(a, s);
+  if (e != hipSuccess) return hip_fail(e, "kv_evict launch");
+  return ok();
 }
 
 int cs_prefill_paged_attn_launch_shape(int32_t batch, int32_t max_q_len, int32_t num_q_heads,

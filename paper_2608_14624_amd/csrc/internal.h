@@ -6,6 +6,21 @@
 
 namespace cs {
 
+// A sliding window over the keys: a row at position p sees key j <= p if j < sinks or
+// j > p - size.  size 0: every key up to p.
+struct Window {
+  int size = 0;
+  int sinks = 0;
+  // Bound of the keys that the steps of `step` keys hold which `rows` consecutive rows see.
+  int visible(int max_len, int rows, int step) const {
+    if (size == 0) return max_len;
+    const long long n = (long long)size + rows - 1 + sinks + 2 * (step - 1);
+    return n < max_len ? (int)n : max_len;
+  }
+  // No row from position p on sees a key of the block of 16 from `key` on.
+  bool hides(long long key, long long p) const { return size > 0 && key >= sinks && key + 15 <= p - size; }
+};
+
 // Everything the attention kernel needs, already validated by the ABI layer.
 struct AttnLaunch {
   const uint16_t* q;
@@ -23,9 +38,9 @@ struct AttnLaunch {
   int head_dim;
   float scale;
   int cus;            // compute units of the device (sizes the rounds)
-  int max_kv_len;
   int total_q;
   void* workspace;    // null: no key parts (see attn_geometry)
+  Window win;
 };
 
 // most key parts a split launch takes (work-groups per tile), the fewest
@@ -65,7 +80,7 @@ struct AttnGeometry {
 // a merge kernel combines.
 AttnGeometry attn_geometry(int batch, int max_q_len, int max_kv_len, int num_q_heads, int num_kv_heads,
                            int head_dim, int cus, bool allow_parts);
-hipError_t launch_prefill_paged_attn(const AttnLaunch& a, hipStream_t stream);
+hipError_t launch_prefill_paged_attn(const AttnLaunch& a, const AttnGeometry& geo, hipStream_t stream);
 
 struct PrefetchLaunch {
   const uint16_t* host_k;   // device-visible addresses of the pinned host buffers
@@ -122,6 +137,12 @@ struct DecodeLaunch {
   int aligned_ranges;
   int slots;
   void* workspace;          // decode_workspace_bytes of scratch (ranges > 0 only)
+  Window win;
+  const int32_t* score_from;
+  float* score_pool;        // not null: every key's attention weight into its score
+  float decay;
+  float* logits;            // [batch][num_kv_heads][logit_units][32 * group]
+  int logit_units;
 };
 
 // A decode launch with a workspace deals the batch's keys to one-wave
@@ -138,6 +159,61 @@ constexpr int kRangeMaxBatch = 1024;
 
 DecodeGeometry decode_geometry(int batch, int max_seq_len, int num_kv_heads, int head_dim, int cus);
 hipError_t launch_paged_decode_attn(const DecodeLaunch& a, hipStream_t stream);
+
+// Attention weights of a prompt's last rows into the keys' scores (key_scores.hip).
+struct KeyScoreGeometry {
+  int max_rows;             // observed rows of any invocation
+  int parts;                // key parts of the row statistics
+  long long row_tiles;      // statistics work-groups per (invocation, KV head) and part
+  long long key_tiles;      // weights work-groups per (invocation, KV head)
+  long long stat_grid;
+  long long weight_grid;
+  long long stat_bytes;     // workspace
+};
+KeyScoreGeometry key_score_geometry(int batch, int max_q_len, int max_kv_len, int rows, int num_q_heads,
+                                    int num_kv_heads, int cus);
+
+struct KeyScoreLaunch {
+  const uint16_t* q;
+  const uint16_t* k_pool;
+  const int32_t* block_tables;
+  const int32_t* prefix_lens;
+  const int32_t* cu_q_lens;
+  const int32_t* score_from;
+  float* score_pool;
+  void* workspace;
+  int batch;
+  int max_blocks_per_seq;
+  int rows;
+  int num_q_heads;
+  int num_kv_heads;
+  int head_dim;
+  float scale;
+  float decay;
+  KeyScoreGeometry geo;
+};
+hipError_t launch_key_scores(const KeyScoreLaunch& a, hipStream_t stream);
+
+// Eviction within sequences by score (kv_evict.hip).
+struct EvictLaunch {
+  float* score_pool;
+  uint16_t* k_pool;
+  uint16_t* v_pool;
+  const int32_t* block_tables;
+  const int32_t* dst_tables;   // null: within the sequences' own blocks
+  const int32_t* seq_lens;
+  const int32_t* keep_from;
+  int32_t* kept;
+  int32_t* new_lens;
+  int batch;
+  int max_blocks_per_seq;
+  int num_kv_heads;
+  int head_dim;
+  int budget;
+  int trigger;
+  int recent;
+};
+hipError_t launch_kv_evict(const EvictLaunch& a, hipStream_t stream);
 
 // Cascade decode: the shared prefix of each group of sequences is attended
 // once with the group's queries stacked (shared_prefix_partials_kernel), in

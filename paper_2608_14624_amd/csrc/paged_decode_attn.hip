@@ -56,6 +56,11 @@ constexpr int kThreads = 256;        // the merge kernel
 // plain decode batches up to this size run longest sequence first
 constexpr int kLptMaxBatch = 1024;
 
+// What a decode launch attends over: all keys of a sequence; its own keys past a shared
+// prefix (the cascade's rest); those under a window and the first few (sinks); or all of
+// them, adding every key's attention weight to its score.
+enum class Keys { kAll, kCascade, kWindow, kScored };
+
 struct DecParams {
   const uint16_t* q;          // [B][Hq][D]
   const uint16_t* k_pool;
@@ -85,7 +90,106 @@ struct DecParams {
   float* ws_o;                  // [chunks + segments][batch * num_q_heads][D]
   float* ws_ml;                 // [chunks + segments][batch * num_q_heads][2]
   int ws_rows;
+  // Keys::kWindow
+  int window;
+  int sinks;
+  // Keys::kScored: a sequence's logits from the unit of its first scored key on,
+  // [batch][num_kv_heads][logit_units][8 quads of keys][group][4]
+  const int32_t* score_from;
+  float* score_pool;            // [num_blocks][num_kv_heads][16]
+  float decay;
+  float* logits;
+  int logit_units;
 };
+
+// The units of a sequence of len keys that its query sees, as a list: under a window
+// those with a key below `sinks` or from `lo` on, unit x of the list being the
+// sequence's unit x or (past the sinks) x + skip; else all of them.
+template <Keys kKeys>
+struct SeenUnits {
+  int sinks, lo, sink_units, skip;
+  __device__ __forceinline__ SeenUnits(const DecParams& p, int len) {
+    if constexpr (kKeys == Keys::kWindow) {
+      sinks = min(p.sinks, len);
+      lo = max(0, len - p.window);
+      sink_units = units_of(sinks);
+      skip = max(0, lo / kUnitKeys - sink_units);
+    }
+  }
+  __device__ __forceinline__ int count(int len) const {
+    if constexpr (kKeys == Keys::kWindow) return units_of(len) - skip;
+    else return units_of(len);
+  }
+  __device__ __forceinline__ int unit(int x) const {
+    if constexpr (kKeys == Keys::kWindow) return x < sink_units ? x : x + skip;
+    else return x;
+  }
+  __device__ __forceinline__ bool key(int k) const {
+    if constexpr (kKeys == Keys::kWindow) return k >= lo || k < sinks;
+    else return true;
+  }
+  // no key of pool block b is seen: its table entry is not read
+  __device__ __forceinline__ bool hidden(int b) const {
+    if constexpr (kKeys == Keys::kWindow) return b * kBlock >= sinks && (b + 1) * kBlock <= lo;
+    else return false;
+  }
+  // V rows of hidden keys in a unit's LDS tile as zeros (0 times a NaN there is NaN)
+  template <int D>
+  __device__ __forceinline__ void zero_hidden(int lane, int key0, uint16_t* tile) const {
+    if constexpr (kKeys == Keys::kWindow) {
+      if (key0 < lo && key0 + kUnitKeys > sinks) {
+#pragma unroll
+        for (int v = 0; v < kChunk * D / 8 / 64; ++v) {
+          const int cc = lane + 64 * v;
+          if (!key(key0 + cc / (D / 8)))
+            *reinterpret_cast<bf16x8*>(&tile[(cc / (D / 8)) * v_tile_stride(D) + (cc % (D / 8)) * 8]) = bf16x8{};
+        }
+      }
+    }
+  }
+};
+
+template <Keys kKeys>
+__device__ __forceinline__ int seen_units(const DecParams& p, int len) {
+  return SeenUnits<kKeys>(p, len).count(len);
+}
+
+// Where the lane's four logits (quad mt * 4 + qd, head j of the group) of a unit are
+// kept, or null: a unit before the first scored key, or past the bound of their number.
+__device__ __forceinline__ float* logits_at(const DecParams& p, int r, int g, int unit, int from_unit) {
+  const int u = unit - from_unit;
+  if (u < 0 || u >= p.logit_units) return nullptr;
+  return p.logits + (((size_t)r * p.num_kv_heads + g) * p.logit_units + u) * (size_t)(kUnitKeys * p.group);
+}
+__device__ __forceinline__ void keep_logits(const DecParams& p, float* unit_logits, int lane, const f32x4 (&s)[2]) {
+#pragma unroll
+  for (int mt = 0; mt < 2; ++mt)
+    *reinterpret_cast<f32x4*>(unit_logits + 4 * ((4 * mt + (lane >> 4)) * p.group + (lane & 15))) = s[mt];
+}
+
+// The weights of the four keys key .. key + 3, of the group's heads together, into their
+// scores.  stat: m c and 1 / l of every head.
+__device__ __forceinline__ void add_scores(const DecParams& p, const float2* stat, int r, int g, int key, int len, int from,
+                                           int id) {
+  const float* at = logits_at(p, r, g, key / kUnitKeys, from / kUnitKeys) + 4 * (key / 4 % 8) * p.group;
+  f32x4 w = f32x4{};
+  for (int j = 0; j < p.group; ++j) {
+    const f32x4 x = *reinterpret_cast<const f32x4*>(at + 4 * j);
+    const float2 st = stat[j];
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      w[e] = __builtin_fmaf(__builtin_amdgcn_exp2f(__builtin_fmaf(x[e], p.scale_log2, -st.x)), st.y, w[e]);
+  }
+  float* score = p.score_pool + ((size_t)id * p.num_kv_heads + g) * kBlock + key % kBlock;
+  const f32x4 old = *reinterpret_cast<const f32x4*>(score);
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    // the query's own key is new in this step: what its slot held is another key's
+    const float kept = key + e == len - 1 ? 0.f : p.decay * old[e];
+    w[e] = key + e >= from && key + e < len ? kept + w[e] : old[e];
+  }
+  *reinterpret_cast<f32x4*>(score) = w;
+}
 
 // first key of sequence r that its group does not share
 __device__ __forceinline__ int shared_len_of(const DecParams& p, int r) {
@@ -112,8 +216,10 @@ struct DecLds {
 
 __device__ __forceinline__ bf16x8 as_bf16x8(uint4 v) { return __builtin_bit_cast(bf16x8, v); }
 
-template <int D, bool kCascade>
-__global__ __launch_bounds__(64 * (kCascade ? kCascadeWaves : kDecodeWaves)) void paged_decode_attn_kernel(DecParams p) {
+template <int D, Keys kKeys>
+__global__ __launch_bounds__(64 * (kKeys == Keys::kCascade ? kCascadeWaves : kDecodeWaves)) void paged_decode_attn_kernel(
+    DecParams p) {
+  constexpr bool kCascade = kKeys == Keys::kCascade;
   constexpr int kWaves = kCascade ? kCascadeWaves : kDecodeWaves;
   constexpr int kWGThreads = 64 * kWaves;
   __shared__ DecLds<D, kWaves> sm;
@@ -142,8 +248,9 @@ __global__ __launch_bounds__(64 * (kCascade ? kCascadeWaves : kDecodeWaves)) voi
     // LDS): the order is a permutation whatever the lengths hold, so every
     // (sequence, head) is still computed exactly once, and each output is
     // the same as in any other order.
+    // (Under a window the sequences' work is about the same.)
     r = blockIdx.x / p.num_kv_heads;
-    if (p.batch <= kLptMaxBatch) {
+    if (kKeys != Keys::kWindow && p.batch <= kLptMaxBatch) {
       __shared__ int lens[kLptMaxBatch];
       __shared__ int pick;
       for (int s = threadIdx.x; s < p.batch; s += kWGThreads) lens[s] = p.seq_lens[s];
@@ -171,8 +278,9 @@ __global__ __launch_bounds__(64 * (kCascade ? kCascadeWaves : kDecodeWaves)) voi
     if (start >= end) return;          // nothing of this sequence's own here
   }
   const int n_blk = (end + kBlock - 1) / kBlock;
+  const SeenUnits<kKeys> seen(p, L);
   const int first_chunk = start / kChunk;
-  const int ch_end = (end + kChunk - 1) / kChunk;
+  const int ch_end = kKeys == Keys::kWindow ? seen.count(L) : (end + kChunk - 1) / kChunk;
   const size_t tile_elems = (size_t)kBlock * D;
   const size_t slot_elems = (size_t)p.num_kv_heads * tile_elems;
   const uint16_t* kbase = p.k_pool + (size_t)g * tile_elems;
@@ -197,9 +305,9 @@ __global__ __launch_bounds__(64 * (kCascade ? kCascadeWaves : kDecodeWaves)) voi
   uint4 kreg[2][DC];
   uint4 vreg[kVLoads];
   auto load_chunk = [&](int ch) {
-    const int b0 = 2 * ch;
-    const int id0 = b0 < n_blk ? bt[b0] : -1;
-    const int id1 = b0 + 1 < n_blk ? bt[b0 + 1] : -1;
+    const int b0 = 2 * seen.unit(ch);
+    const int id0 = b0 < n_blk && !seen.hidden(b0) ? bt[b0] : -1;
+    const int id1 = b0 + 1 < n_blk && !seen.hidden(b0 + 1) ? bt[b0 + 1] : -1;
 #pragma unroll
     for (int mt = 0; mt < 2; ++mt) {
       const int id = mt ? id1 : id0;
@@ -241,11 +349,13 @@ __global__ __launch_bounds__(64 * (kCascade ? kCascadeWaves : kDecodeWaves)) voi
     // rows past the end of the sequence (inside its last block) overwritten
     // with zeros: their probabilities are 0, but 0 times a stale NaN or Inf
     // in the pool is NaN
-    if ((ch + 1) * kChunk > end) {
+    const int kbase_idx = seen.unit(ch) * kChunk;
+    seen.template zero_hidden<D>(lane, kbase_idx, sm.v[wave]);
+    if (kbase_idx + kChunk > end) {
 #pragma unroll
       for (int u = 0; u < kVLoads; ++u) {
         const int cc = lane + 64 * u;
-        if (ch * kChunk + cc / kRowChunks >= end)
+        if (kbase_idx + cc / kRowChunks >= end)
           *reinterpret_cast<uint4*>(&sm.v[wave][(cc / kRowChunks) * vStride + (cc % kRowChunks) * 8]) =
               make_uint4(0, 0, 0, 0);
       }
@@ -260,16 +370,19 @@ __global__ __launch_bounds__(64 * (kCascade ? kCascadeWaves : kDecodeWaves)) voi
     if (ch + kWaves < ch_end) load_chunk(ch + kWaves);     // in flight during the math
 
     // mask keys past the end; register r of tile mt holds key 32*ch + 16*mt + 4*qd + r
-    const int kbase_idx = ch * kChunk;
     float mloc = -INFINITY;
 #pragma unroll
     for (int mt = 0; mt < 2; ++mt)
 #pragma unroll
       for (int rr = 0; rr < 4; ++rr) {
         const int key = kbase_idx + 16 * mt + 4 * qd + rr;
-        s[mt][rr] = (key < end && key >= start) ? s[mt][rr] : -INFINITY;
+        s[mt][rr] = (key < end && key >= start && seen.key(key)) ? s[mt][rr] : -INFINITY;
         mloc = fmaxf(mloc, s[mt][rr]);
       }
+    if constexpr (kKeys == Keys::kScored) {
+      float* keep = logits_at(p, r, g, ch, max(0, p.score_from[r]) / kUnitKeys);
+      if (keep != nullptr && head_valid) keep_logits(p, keep, lane, s);
+    }
     mloc = fmaxf(mloc, __shfl_xor(mloc, 16));
     mloc = fmaxf(mloc, __shfl_xor(mloc, 32));
     const float m_new = fmaxf(m_run, mloc);
@@ -286,7 +399,8 @@ __global__ __launch_bounds__(64 * (kCascade ? kCascadeWaves : kDecodeWaves)) voi
       for (int rr = 0; rr < 4; ++rr) {
         const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s[mt][rr], c, -mc));
         pb[4 * mt + rr] = (__bf16)e;
-        l_run += (float)pb[4 * mt + rr];
+        // (scores are sums of fp32 weights, which are normalised by a sum of such)
+        l_run += kKeys == Keys::kScored ? e : (float)pb[4 * mt + rr];
       }
     // O^T += V^T P^T
 #pragma unroll
@@ -330,9 +444,29 @@ __global__ __launch_bounds__(64 * (kCascade ? kCascadeWaves : kDecodeWaves)) voi
         p.ws_ml[2 * widx] = mx;
         p.ws_ml[2 * widx + 1] = den;
       }
-    } else {
+    } else if constexpr (kKeys == Keys::kAll) {
       p.out[row * D + d] = __builtin_bit_cast(uint16_t, (__bf16)(num / den));
+    } else {
+      // a row of an empty sequence (a padded batch) is zero
+      p.out[row * D + d] = __builtin_bit_cast(uint16_t, (__bf16)(L > 0 ? num / den : 0.f));
     }
+  }
+  if constexpr (kKeys == Keys::kScored) {
+    __shared__ float2 stat[kMaxGroup];
+    if ((int)threadIdx.x < p.group) {
+      const int hj = threadIdx.x;
+      float mx = -INFINITY, den = 0.f;
+      for (int w = 0; w < kWaves; ++w) mx = fmaxf(mx, sm.merge.m[w][hj]);
+      for (int w = 0; w < kWaves; ++w) den += __builtin_amdgcn_exp2f((sm.merge.m[w][hj] - mx) * c) * sm.merge.l[w][hj];
+      stat[hj] = make_float2(mx * c, 1.f / den);
+    }
+    __syncthreads();
+    // the logits that the work-group's waves kept (at most logit_units of them)
+    const int from = max(0, p.score_from[r]);
+    const int first = from / 4 * 4;
+    const int last = (int)min((long long)L, (long long)(from / kUnitKeys + p.logit_units) * kUnitKeys);
+    for (int key = first + 4 * threadIdx.x; key < last; key += 4 * kWGThreads)
+      add_scores(p, stat, r, g, key, L, from, bt[key / kBlock]);
   }
 }
 
@@ -446,17 +580,19 @@ struct RangeCursor {
   int r;          // sequence
   int len;        // its keys
   int x, xe;      // unit within the sequence, end of the piece
-  int slot;       // where the piece's partial goes, -1: the piece is the whole sequence
+  int slot;       // where the piece's partial goes; negative: the piece is the whole
+                  // sequence (~ the slot its m and l go to where scores are asked)
   bool valid;
 };
 
-template <int D>
+template <int D, Keys kKeys>
 __global__ __launch_bounds__(64) void decode_ranges_kernel(DecParams p) {
   constexpr int vStride = v_tile_stride(D);
   constexpr int DC = D / 32;
   constexpr int DT = D / 16;
   constexpr int kVLoads = kChunk * D / 8 / 64;
   constexpr int kManyUnits = 0xffff;
+  constexpr bool kScored = kKeys == Keys::kScored;
   __shared__ union {
     struct {
       uint16_t v[kChunk * vStride];
@@ -471,6 +607,7 @@ __global__ __launch_bounds__(64) void decode_ranges_kernel(DecParams p) {
   const int g = blockIdx.x % p.num_kv_heads;
   const int w = blockIdx.x / p.num_kv_heads;
   const ScalarInts lens_c = (ScalarInts)p.seq_lens;
+  const ScalarInts from_c = (ScalarInts)p.score_from;
 
   // ---- the plan.  All lengths and probed blocks are asked for at once, and the
   // units then kept in LDS: read from memory again for every piece, a batch of
@@ -485,7 +622,8 @@ __global__ __launch_bounds__(64) void decode_ranges_kernel(DecParams p) {
   int total = 0, longest = 0;
   plan_rounds(p.batch, [&](int i) __attribute__((always_inline)) {
     if (n_of[i] <= kProbeBlock * kBlock) ids_probed[i] = -1;      // an entry past its last block
-    n_of[i] = units_of(n_of[i]);
+    if (SeenUnits<kKeys>(p, n_of[i]).hidden(kProbeBlock)) ids_probed[i] = -1;
+    n_of[i] = seen_units<kKeys>(p, n_of[i]);
     total += wave_total(n_of[i]);
     longest = max(longest, wave_max(n_of[i]));
   });
@@ -502,7 +640,7 @@ __global__ __launch_bounds__(64) void decode_ranges_kernel(DecParams p) {
   auto units_at = [&](int s) {           // of sequence s (a lane's), 0 past the batch
     if (s >= p.batch) return 0;
     const int n = sm.units[s];
-    return n == kManyUnits ? units_of(p.seq_lens[s]) : n;
+    return n == kManyUnits ? seen_units<kKeys>(p, p.seq_lens[s]) : n;
   };
   const int ranges = aligned ? p.aligned_ranges : p.ranges;     // waves that take part
   // With few KV heads there are more waves than the merge has use for: few
@@ -548,17 +686,20 @@ __global__ __launch_bounds__(64) void decode_ranges_kernel(DecParams p) {
     }
     c.len = lens_c[c.r];
     c.x = piece * per;
-    c.xe = min(units_of(c.len), c.x + per);
-    c.slot = units_of(c.len) <= per ? -1 : piece_base(c.r) + piece;
+    const int n = seen_units<kKeys>(p, c.len);
+    c.xe = min(n, c.x + per);
+    const bool whole = n <= per;
+    c.slot = whole && !kScored ? -1 : piece_base(c.r) + piece;
+    if (kScored && whole) c.slot = ~c.slot;
     c.valid = true;
   };
   // contiguous ranges: `left` units of the range lie past the cursor's piece
   int left = 0;
   auto contiguous_piece = [&](RangeCursor& c) {      // from unit c.x of sequence c.r on
-    const int n = units_of(c.len);
+    const int n = seen_units<kKeys>(p, c.len);
     c.xe = min(n, c.x + left);
     left -= c.xe - c.x;
-    c.slot = (c.x == 0 && c.xe == n) ? -1 : c.r + w;
+    c.slot = (c.x == 0 && c.xe == n) ? (kScored ? ~(c.r + w) : -1) : c.r + w;
     c.valid = true;
   };
 
@@ -630,9 +771,15 @@ __global__ __launch_bounds__(64) void decode_ranges_kernel(DecParams p) {
   // (its keys there are masked, its V rows zeroed)
   auto ids_of = [&](const RangeCursor& cu, int& id0, int& id1) {
     const ScalarInts bt = (ScalarInts)(p.block_tables + (size_t)cu.r * p.max_blocks_per_seq);
-    const int b0 = cu.x * kUnitBlocks;
+    const SeenUnits<kKeys> seen(p, cu.len);
+    int b0 = seen.unit(cu.x) * kUnitBlocks;
+    int b1 = min(b0 + 1, (cu.len - 1) / kBlock);
+    // (a hidden block stands for the unit's other one; its keys are masked, its V zeroed)
+    const int hidden0 = seen.hidden(b0) ? b1 : b0;
+    b1 = seen.hidden(b1) ? b0 : b1;
+    b0 = hidden0;
     id0 = bt[b0];
-    id1 = bt[min(b0 + 1, (cu.len - 1) / kBlock)];
+    id1 = bt[b1];
   };
   bf16x8 qreg[DC];
   auto load_q = [&](int r) {
@@ -660,6 +807,8 @@ __global__ __launch_bounds__(64) void decode_ranges_kernel(DecParams p) {
     int id0, id1;
     ids_of(cur, id0, id1);
     load_q(cur.r);
+    int from_unit = 0;                   // of the sequence's first scored key
+    if constexpr (kScored) from_unit = max(0, from_c[cur.r]) / kUnitKeys;
     load_chunk(id0, id1, tag);
     reset();
     advance(ids, tag);
@@ -667,8 +816,10 @@ __global__ __launch_bounds__(64) void decode_ranges_kernel(DecParams p) {
     if (nxt.valid) ids_of(nxt, id0, id1);
 
     for (;;) {
-      const int key0 = cur.x * kUnitKeys;
+      const SeenUnits<kKeys> seen(p, cur.len);
+      const int key0 = seen.unit(cur.x) * kUnitKeys;
       store_v_tile<D>(vreg, lane, key0, cur.len, sm.v);
+      seen.template zero_hidden<D>(lane, key0, sm.v);
       f32x4 s[2] = {f32x4{}, f32x4{}};
   #pragma unroll
       for (int mt = 0; mt < 2; ++mt)
@@ -687,9 +838,13 @@ __global__ __launch_bounds__(64) void decode_ranges_kernel(DecParams p) {
   #pragma unroll
         for (int rr = 0; rr < 4; ++rr) {
           const int key = key0 + 16 * mt + 4 * qd + rr;
-          s[mt][rr] = key < cur.len ? s[mt][rr] : -INFINITY;
+          s[mt][rr] = key < cur.len && seen.key(key) ? s[mt][rr] : -INFINITY;
           mloc = fmaxf(mloc, s[mt][rr]);
         }
+      if constexpr (kScored) {
+        float* keep = logits_at(p, cur.r, g, cur.x, from_unit);
+        if (keep != nullptr && head_valid) keep_logits(p, keep, lane, s);
+      }
       // A unit's probabilities are relative to its own maximum and its O is
       // rescaled in fp32: the largest of every 32 are then exact in bf16, where
       // against the running maximum of a whole range only a few were.  Relative
@@ -710,7 +865,8 @@ __global__ __launch_bounds__(64) void decode_ranges_kernel(DecParams p) {
         for (int rr = 0; rr < 4; ++rr) {
           const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s[mt][rr], c, -mc));
           pb[4 * mt + rr] = (__bf16)e;
-          l_unit += (float)pb[4 * mt + rr];
+          // (scores are sums of fp32 weights, which are normalised by a sum of such)
+          l_unit += kScored ? e : (float)pb[4 * mt + rr];
         }
       l_run = __builtin_fmaf(l_run, alpha, l_unit * beta);
   #pragma unroll
@@ -734,6 +890,10 @@ __global__ __launch_bounds__(64) void decode_ranges_kernel(DecParams p) {
               for (int e = 0; e < 4; ++e) o[e] = (__bf16)(oacc[dt][e] / l_run);
               *reinterpret_cast<uint2*>(orow + 16 * dt + 4 * qd) = __builtin_bit_cast(uint2, o);
             }
+            if constexpr (kScored) {
+              const size_t at = ((size_t)g * p.slots + ~cur.slot) * p.group + j;
+              if (qd == 0) *reinterpret_cast<float2*>(p.ws_ml + 2 * at) = make_float2(m_run, l_run);
+            }
           } else {
             const size_t at = ((size_t)g * p.slots + cur.slot) * p.group + j;
   #pragma unroll
@@ -742,6 +902,7 @@ __global__ __launch_bounds__(64) void decode_ranges_kernel(DecParams p) {
           }
         }
         if (!nxt.valid) return;
+        if constexpr (kScored) from_unit = max(0, from_c[nxt.r]) / kUnitKeys;
         reset();
       }
       cur = nxt;
@@ -754,43 +915,94 @@ __global__ __launch_bounds__(64) void decode_ranges_kernel(DecParams p) {
     run(std::false_type{});
 }
 
-// One work-group per (sequence, KV head): combines the pieces that
-// decode_ranges_kernel left of a sequence (a sequence of one piece has its
-// output already).
-template <int D>
-__global__ __launch_bounds__(kMergeThreads) void decode_ranges_merge_kernel(DecParams p) {
-  const int lane = threadIdx.x & 63;
-  const int g = blockIdx.x % p.num_kv_heads;
-  const int r = blockIdx.x / p.num_kv_heads;
+// The pieces that decode_ranges_kernel left of sequence r: its first slot and their number.
+template <Keys kKeys>
+__device__ __forceinline__ int2 pieces_of(const DecParams& p, int r, int lane) {
   const int2 plan = *p.plan;
   const bool aligned = plan.x != 0;
   const int per = plan.y;
   // units before r, or (aligned) pieces before r
   int before = 0;
   for (int s = 0; s < r; s += 64) {
-    const int x = s + lane < r ? units_of(p.seq_lens[s + lane]) : 0;
+    const int x = s + lane < r ? seen_units<kKeys>(p, p.seq_lens[s + lane]) : 0;
     before += wave_total(aligned ? ceil_div(x, per) : x);
   }
-  const int units = units_of(p.seq_lens[r]);
-  int first, n;                          // the sequence's first slot, and its pieces
-  if (aligned) {
-    first = before;
-    n = ceil_div(units, per);
-  } else {
-    const int w0 = before / per;
-    first = r + w0;
-    n = (before + units - 1) / per - w0 + 1;
-  }
-  // a sequence of one piece has its output; one without keys gets NaN here, as
-  // from one work-group per pair
-  if (units == 0) n = 0;
-  if (n == 1) return;
-  const size_t base = ((size_t)g * p.slots + first) * p.group;
+  const int units = seen_units<kKeys>(p, p.seq_lens[r]);
+  if (units == 0) return make_int2(0, 0);
+  if (aligned) return make_int2(before, ceil_div(units, per));
+  const int w0 = before / per;
+  return make_int2(r + w0, (before + units - 1) / per - w0 + 1);
+}
+
+// Combines the pieces of a sequence and KV head into its output (a sequence of one
+// piece has it already).  A sequence without keys gets NaN, as from one work-group per
+// pair, or zeros where the call allows such rows.
+template <int D, Keys kKeys>
+__device__ __forceinline__ void merge_sequence(const DecParams& p, int g, int r, int2 piece) {
+  if (piece.y == 1) return;
+  const size_t base = ((size_t)g * p.slots + piece.x) * p.group;
   const size_t row = (size_t)r * p.num_q_heads + g * p.group;
+  const bool empty = kKeys != Keys::kAll && piece.y == 0;
   merge_pieces<D>(
-      p.ws_o, p.ws_ml, p.group, p.scale_log2, [&](int) { return n; },
+      p.ws_o, p.ws_ml, p.group, p.scale_log2, [&](int) { return piece.y; },
       [&](int hj, int k) { return base + (size_t)k * p.group + hj; },
-      [&](int hj, int d, bf16x4 o) { *reinterpret_cast<uint2*>(p.out + (row + hj) * D + d) = __builtin_bit_cast(uint2, o); });
+      [&](int hj, int d, bf16x4 o) {
+        *reinterpret_cast<uint2*>(p.out + (row + hj) * D + d) = __builtin_bit_cast(uint2, empty ? bf16x4{} : o);
+      });
+}
+
+// One work-group per (sequence, KV head).
+template <int D, Keys kKeys>
+__global__ __launch_bounds__(kMergeThreads) void decode_ranges_merge_kernel(DecParams p) {
+  const int g = blockIdx.x % p.num_kv_heads;
+  const int r = blockIdx.x / p.num_kv_heads;
+  merge_sequence<D, kKeys>(p, g, r, pieces_of<kKeys>(p, r, threadIdx.x & 63));
+}
+
+// The end of a decode in ranges that adds attention weights to scores: the first
+// work-groups, one per (sequence, KV head), merge its pieces, and the others, one per
+// kScoreKeys of its scored keys too, turn the logits that the ranges kept into weights.
+// Every one of these finds the row statistics (m, l) itself from the pieces'.
+constexpr int kScoreKeys = 4 * kMergeThreads;
+template <int D>
+__global__ __launch_bounds__(kMergeThreads) void decode_scores_kernel(DecParams p) {
+  const int lane = threadIdx.x & 63;
+  const int pairs = p.batch * p.num_kv_heads;
+  const int g = blockIdx.x % p.num_kv_heads;
+  const int r = blockIdx.x / p.num_kv_heads % p.batch;
+  if ((int)blockIdx.x < pairs) {
+    merge_sequence<D, Keys::kScored>(p, g, r, pieces_of<Keys::kScored>(p, r, lane));
+    return;
+  }
+  const int chunk = blockIdx.x / pairs - 1;
+  const int len = p.seq_lens[r];
+  const int from = max(0, p.score_from[r]);
+  const int first = from / kUnitKeys * kUnitKeys + chunk * kScoreKeys;
+  if (first >= len) return;
+  const int2 piece = pieces_of<Keys::kScored>(p, r, lane);
+  __shared__ float2 stat[kMaxGroup];
+  const float c = p.scale_log2;
+  for (int j = threadIdx.x >> 6; j < p.group; j += kMergeThreads / 64) {
+    float m = -INFINITY, l = 0.f;
+    for (int k = lane; k < piece.y; k += 64) {
+      const size_t at = ((size_t)g * p.slots + piece.x + k) * p.group + j;
+      const float2 ml = *reinterpret_cast<const float2*>(p.ws_ml + 2 * at);
+      const float m_new = fmaxf(m, ml.x);
+      l = l * __builtin_amdgcn_exp2f((m - m_new) * c) + ml.y * __builtin_amdgcn_exp2f((ml.x - m_new) * c);
+      m = m_new;
+    }
+    float m_all = m;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) m_all = fmaxf(m_all, __shfl_xor(m_all, o));
+    l = m == -INFINITY ? 0.f : l * __builtin_amdgcn_exp2f((m - m_all) * c);
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) l += __shfl_xor(l, o);
+    if (lane == 0) stat[j] = make_float2(m_all * c, 1.f / l);
+  }
+  __syncthreads();
+  const int key = first + 4 * threadIdx.x;
+  if (key + 3 < from || key >= len || (key - from / kUnitKeys * kUnitKeys) / kUnitKeys >= p.logit_units) return;
+  add_scores(p, stat, r, g, key, len, from, p.block_tables[(size_t)r * p.max_blocks_per_seq + key / kBlock]);
 }
 
 // One work-group per (sequence, KV head): the final output of cascade decode
@@ -878,6 +1090,37 @@ DecodeGeometry decode_geometry(int batch, int max_seq_len, int num_kv_heads, int
   return geo;
 }
 
+namespace {
+
+template <int D, Keys kKeys>
+void launch_decode(const DecodeLaunch& a, const DecParams& p, hipStream_t stream) {
+  const unsigned rows = (unsigned)((long long)a.batch * a.num_kv_heads);
+  if (a.ranges == 0) {
+    hipLaunchKernelGGL((paged_decode_attn_kernel<D, kKeys>), dim3(rows), dim3(64 * kDecodeWaves), 0, stream, p);
+    return;
+  }
+  const dim3 grid((unsigned)(std::max(a.ranges, a.aligned_ranges) * a.num_kv_heads)), block(64);
+  hipLaunchKernelGGL((decode_ranges_kernel<D, kKeys>), grid, block, 0, stream, p);
+  if constexpr (kKeys == Keys::kScored) {
+    const unsigned chunks = (unsigned)(((long long)a.logit_units * kUnitKeys + kScoreKeys - 1) / kScoreKeys);
+    hipLaunchKernelGGL(decode_scores_kernel<D>, dim3(rows * (1 + chunks)), dim3(kMergeThreads), 0, stream, p);
+  } else {
+    hipLaunchKernelGGL((decode_ranges_merge_kernel<D, kKeys>), dim3(rows), dim3(kMergeThreads), 0, stream, p);
+  }
+}
+
+template <int D>
+void launch_decode(const DecodeLaunch& a, const DecParams& p, hipStream_t stream) {
+  if (a.score_pool != nullptr)
+    launch_decode<D, Keys::kScored>(a, p, stream);
+  else if (a.win.size > 0)
+    launch_decode<D, Keys::kWindow>(a, p, stream);
+  else
+    launch_decode<D, Keys::kAll>(a, p, stream);
+}
+
+}  // namespace
+
 hipError_t launch_paged_decode_attn(const DecodeLaunch& a, hipStream_t stream) {
   DecParams p = {};
   p.q = a.q;
@@ -892,7 +1135,13 @@ hipError_t launch_paged_decode_attn(const DecodeLaunch& a, hipStream_t stream) {
   p.group = a.num_q_heads / a.num_kv_heads;
   p.scale_log2 = a.scale * kLog2e;
   p.batch = a.batch;
-  const unsigned rows = (unsigned)((long long)a.batch * a.num_kv_heads);
+  p.window = a.win.size;
+  p.sinks = a.win.sinks;
+  p.score_from = a.score_from;
+  p.score_pool = a.score_pool;
+  p.decay = a.decay;
+  p.logits = a.logits;
+  p.logit_units = a.logit_units;
   if (a.ranges > 0) {
     p.ranges = a.ranges;
     p.aligned_ranges = a.aligned_ranges;
@@ -900,22 +1149,11 @@ hipError_t launch_paged_decode_attn(const DecodeLaunch& a, hipStream_t stream) {
     p.ws_o = static_cast<float*>(a.workspace);
     p.ws_ml = p.ws_o + (size_t)a.slots * a.num_q_heads * a.head_dim;
     p.plan = reinterpret_cast<int2*>(p.ws_ml + (size_t)a.slots * a.num_q_heads * 2);
-    const dim3 grid((unsigned)(std::max(a.ranges, a.aligned_ranges) * a.num_kv_heads)), block(64);
-    if (a.head_dim == 128) {
-      hipLaunchKernelGGL(decode_ranges_kernel<128>, grid, block, 0, stream, p);
-      hipLaunchKernelGGL(decode_ranges_merge_kernel<128>, dim3(rows), dim3(kMergeThreads), 0, stream, p);
-    } else {
-      hipLaunchKernelGGL(decode_ranges_kernel<64>, grid, block, 0, stream, p);
-      hipLaunchKernelGGL(decode_ranges_merge_kernel<64>, dim3(rows), dim3(kMergeThreads), 0, stream, p);
-    }
-    return hipGetLastError();
   }
-  const dim3 grid(rows), block(64 * kDecodeWaves);
-  if (a.head_dim == 128) {
-    hipLaunchKernelGGL((paged_decode_attn_kernel<128, false>), grid, block, 0, stream, p);
-  } else {
-    hipLaunchKernelGGL((paged_decode_attn_kernel<64, false>), grid, block, 0, stream, p);
-  }
+  if (a.head_dim == 128)
+    launch_decode<128>(a, p, stream);
+  else
+    launch_decode<64>(a, p, stream);
   return hipGetLastError();
 }
 
@@ -948,9 +1186,9 @@ hipError_t launch_cascade_decode_rest(const CascadeLaunch& a, hipStream_t stream
   if (geo.segments > 0) {
     const dim3 grid((unsigned)(rows * geo.segments)), block(64 * kCascadeWaves);
     if (a.head_dim == 128) {
-      hipLaunchKernelGGL((paged_decode_attn_kernel<128, true>), grid, block, 0, stream, p);
+      hipLaunchKernelGGL((paged_decode_attn_kernel<128, Keys::kCascade>), grid, block, 0, stream, p);
     } else {
-      hipLaunchKernelGGL((paged_decode_attn_kernel<64, true>), grid, block, 0, stream, p);
+      hipLaunchKernelGGL((paged_decode_attn_kernel<64, Keys::kCascade>), grid, block, 0, stream, p);
     }
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;

@@ -70,6 +70,7 @@
 #include "internal.h"
 #include "wave_ops.h"
 
+#include <float.h>
 #include <math.h>
 
 #include <algorithm>
@@ -132,6 +133,9 @@ struct Params {
   int parts;
   int split_tiles;
   long long part_rows;          // total_q * num_q_heads
+  // windowed launches: a row at position p sees key j <= p if j < sinks or j > p - window
+  int window;
+  int sinks;
 };
 
 template <int D>
@@ -254,6 +258,68 @@ __device__ __forceinline__ bool even_tile(const Params& p, int wg, TileAt& t) {
   if (t.token_tile * p.span >= t.S) return false;
   t.P = p.prefix_lens[t.r];
   return true;
+}
+
+// What the rows of a tile at positions qlo .. kv_end - 1 see under a window: the keys
+// below `sinks` and those from `lo` on.  The 64-key steps that hold none of them are
+// left out, so the tile's step j is the sequence's step j, or (j past the sinks)
+// j + skip; without a window nothing is left out.  A pool block in a step that no row
+// sees is never read (its table entry may name a recycled block, or none), and V rows of
+// keys that no row sees are zeroed as those past the sequence's end are: a probability
+// of 0 times a NaN there would not be 0.
+template <bool kWindow>
+struct Visible {
+  int sinks, lo, sink_steps, skip;
+  __device__ __forceinline__ Visible(const Params& p, int qlo, int kv_end) {
+    if constexpr (kWindow) {
+      sinks = min(p.sinks, kv_end);
+      lo = max(0, qlo - p.window + 1);
+      sink_steps = ceil_div(sinks, kBN);
+      skip = max(0, lo / kBN - sink_steps);
+    }
+  }
+  __device__ __forceinline__ int step(int j) const {
+    if constexpr (kWindow) return j < sink_steps ? j : j + skip;
+    else return j;
+  }
+  __device__ __forceinline__ int steps(int kv_end) const {
+    const int all = (kv_end + kBN - 1) / kBN;
+    if constexpr (kWindow) return all - skip;
+    else return all;
+  }
+  __device__ __forceinline__ bool block(int lb) const {
+    if constexpr (kWindow) return lb * kBlock < sinks || (lb + 1) * kBlock > lo;
+    else return true;
+  }
+  // some of the kBlock keys from key0 on is to be zeroed / this one is
+  __device__ __forceinline__ bool zeroes(int key0, int L) const {
+    if constexpr (kWindow) return key0 + kBlock > L || (key0 < lo && key0 + kBlock > sinks);
+    else return key0 + kBlock > L;
+  }
+  __device__ __forceinline__ bool zero(int key, int L) const {
+    if constexpr (kWindow) return key >= L || (key < lo && key >= sinks);
+    else return key >= L;
+  }
+};
+
+// The logits of a windowed step for a wave whose rows are at positions qmin .. qmax
+// (its lane's at qpos): keys the row does not see become -inf.  Steps that every row
+// sees whole are passed by.
+__device__ __forceinline__ void mask_window(const Params& p, int sinks, int kstart, int qmin, int qmax, int qpos,
+                                            int half, f32x16 (&s)[2]) {
+  if (kstart + kBN - 1 <= qmin && (kstart > qmax - p.window || kstart + kBN <= sinks)) return;
+  // in the step, the lane's key of constant offset o is visible if o <= last and o > old or o < sink
+  const int last = qpos - kstart - 4 * half;
+  const int old = last - p.window;
+  const int sink = sinks - kstart - 4 * half;
+#pragma unroll
+  for (int mt = 0; mt < 2; ++mt) {
+#pragma unroll
+    for (int rr = 0; rr < 16; ++rr) {
+      const int o = mt * 32 + 8 * (rr >> 2) + (rr & 3);
+      s[mt][rr] = (o <= last && (o > old || o < sink)) ? s[mt][rr] : -INFINITY;
+    }
+  }
 }
 
 // The same in any other batch; false: no tile is left for the work-group.
@@ -635,7 +701,7 @@ __global__ __launch_bounds__(kThreads) void shared_prefix_partials_kernel(Params
 // merge through LDS at the end.  Per step the arithmetic of a row is that of
 // the ping-pong kernel (logits, mask, lazy rescale, exp2, bf16 P, row sums
 // over the same bf16 values, PV), in the same order.
-template <int D, bool kTailTile, bool kPartial = false>
+template <int D, bool kTailTile, bool kPartial, bool kWindow>
 __device__ __forceinline__ void ppd_split_tile(const Params& p, const int wg, const TileAt& at, uint16_t* k0,
                                                uint16_t* k1, uint16_t* k2, uint16_t* k3, uint16_t* v0,
                                                uint16_t* v1, uint16_t* v2, uint16_t* v3) {
@@ -695,7 +761,8 @@ __device__ __forceinline__ void ppd_split_tile(const Params& p, const int wg, co
   const size_t qrow = ((size_t)(q0 + (row_valid ? t : 0)) * p.num_q_heads + h) * D;
   const int qpos = row_valid ? P + t : L - 1;               // last visible key
   const int kv_end = P + min(S, t0 + span);                 // keys the tile needs
-  const int n_all = (kv_end + kBN - 1) / kBN;
+  const Visible<kWindow> vis(p, P + t0, kv_end);
+  const int n_all = vis.steps(kv_end);
   // this work-group's key steps [s0, s1): all of them, or one of p.parts
   // contiguous parts (a part may be empty)
   int s0 = 0, s1 = n_all;
@@ -730,8 +797,8 @@ __device__ __forceinline__ void ppd_split_tile(const Params& p, const int wg, co
   const __attribute__((address_space(4))) int32_t* bt_c =
       (const __attribute__((address_space(4))) int32_t*)bt;
   auto block_id = [&](int step) __attribute__((always_inline)) -> int {
-    const int lb = (j0 + step) * (kBN / kBlock) + slot_u;
-    return (step < n_steps && lb < n_blk) ? bt_c[lb] : -1;          // -1: past the end
+    const int lb = vis.step(j0 + step) * (kBN / kBlock) + slot_u;
+    return (step < n_steps && lb < n_blk && vis.block(lb)) ? bt_c[lb] : -1;   // -1: past the end, or out of sight
   };
   // staging and operand addressing as in the ppd kernel (DirectLayout<D>)
   const int dma_d = lane / (D / 8);
@@ -746,10 +813,10 @@ __device__ __forceinline__ void ppd_split_tile(const Params& p, const int wg, co
                                                16, 2 * dma_off, 2 * u * kGroupElems, 0, 0);
   };
   auto zero_tail = [&](uint16_t* buf, int key0) __attribute__((always_inline)) {
-    if (key0 + kBlock > L) {
+    if (vis.zeroes(key0, L)) {
 #pragma unroll
       for (int u = 0; u < kLoads; ++u) {
-        if (key0 + DL::kRows * u + dma_d >= L)
+        if (vis.zero(key0 + DL::kRows * u + dma_d, L))
           *reinterpret_cast<uint4*>(&buf[(kLoads * slot_u + u) * kGrp + 8 * lane]) = make_uint4(0, 0, 0, 0);
       }
     }
@@ -797,7 +864,7 @@ __device__ __forceinline__ void ppd_split_tile(const Params& p, const int wg, co
 
   // logits, mask, online softmax and PV product of step j
   auto step = [&](const int j, const uint16_t* kbuf, const uint16_t* vbuf) __attribute__((always_inline)) {
-    const int kstart = (j0 + j) * kBN;
+    const int kstart = vis.step(j0 + j) * kBN;
     f32x16 s_cur[2];
     s_cur[0] = f32x16{};
     s_cur[1] = f32x16{};
@@ -821,7 +888,9 @@ __device__ __forceinline__ void ppd_split_tile(const Params& p, const int wg, co
     __builtin_amdgcn_s_setprio(0);
     // accumulator register rr of tile mt holds key
     //   kstart + 32*mt + 8*(rr/4) + 4*half + rr%4   for query qi
-    if (kstart + kBN - 1 > wave_qmin) {
+    if constexpr (kWindow) {
+      mask_window(p, vis.sinks, kstart, wave_qmin, min(wave_qmin + kNQ - 1, L - 1), qpos, half, s_cur);
+    } else if (kstart + kBN - 1 > wave_qmin) {
       // key kj <= qpos  <=>  its constant offset in the step <= lim
       const int lim = qpos - kstart - 4 * half;
 #pragma unroll
@@ -838,8 +907,8 @@ __device__ __forceinline__ void ppd_split_tile(const Params& p, const int wg, co
       for (int rr = 0; rr < 16; ++rr) mloc = fmaxf(mloc, s_cur[mt][rr]);
     }
     mloc = pair_max(mloc);
-    // lazy rescale (a row whose keys so far were all masked keeps
-    // m_run = -inf: possible only in the second half)
+    // lazy rescale (a row whose keys so far were all masked keeps m_run = -inf:
+    // possible only in the second half, or under a window)
     const bool grow = (mloc - m_run) * c > 8.f;
     if (__builtin_amdgcn_ballot_w64(grow) != 0) {
       const float m_new = grow ? mloc : m_run;
@@ -898,7 +967,7 @@ __device__ __forceinline__ void ppd_split_tile(const Params& p, const int wg, co
     auto iteration = [&](const int j, uint16_t* kcur, uint16_t* vcur, uint16_t* knext,
                          uint16_t* vnext) __attribute__((always_inline)) {
       __builtin_amdgcn_s_waitcnt(kWaitVmcnt0);
-      if (j < n_steps) zero_tail(vcur, (j0 + j) * kBN + slot_u * kBlock);
+      if (j < n_steps) zero_tail(vcur, vis.step(j0 + j) * kBN + slot_u * kBlock);
       __builtin_amdgcn_s_waitcnt(kWaitLgkmcnt0);
       asm volatile("s_barrier" ::: "memory");
       if (j + 1 < n_steps) {
@@ -996,7 +1065,7 @@ __device__ __forceinline__ void ppd_split_tile(const Params& p, const int wg, co
 // At head_dim 64 the kernel holds at most 128 VGPRs (at least four waves per
 // SIMD) and 50,688 bytes of LDS (67,584 with the halves' two more buffers),
 // so two work-groups share a CU.
-template <int D, PPMode kMode>
+template <int D, PPMode kMode, bool kWindow>
 __global__ __launch_bounds__(kPPThreads, D == 64 ? 4 : 2) void prefill_paged_attn_ppd_kernel(Params p) {
   using DL = DirectLayout<D>;
   // K and V of three steps, each in its own array so that the compiler can
@@ -1015,7 +1084,7 @@ __global__ __launch_bounds__(kPPThreads, D == 64 ? 4 : 2) void prefill_paged_att
     if (at.half >= 0) {
       // the halves' two-deep rings take two more buffers
       __shared__ __attribute__((aligned(16))) uint16_t k3[kBuf], v3[kBuf];
-      ppd_split_tile<D, true>(p, blockIdx.x, at, k0, k1, k2, k3, v0, v1, v2, v3);
+      ppd_split_tile<D, true, false, kWindow>(p, blockIdx.x, at, k0, k1, k2, k3, v0, v1, v2, v3);
       return;
     }
   }
@@ -1042,7 +1111,8 @@ __global__ __launch_bounds__(kPPThreads, D == 64 ? 4 : 2) void prefill_paged_att
   const size_t qrow = ((size_t)(q0 + (row_valid ? t : 0)) * p.num_q_heads + h) * D;
   const int qpos = row_valid ? P + t : L - 1;               // last visible key
   const int kv_end = P + min(S, t0 + p.span);               // keys the tile needs
-  const int n_steps = (kv_end + kBN - 1) / kBN;
+  const Visible<kWindow> vis(p, P + t0, kv_end);
+  const int n_steps = vis.steps(kv_end);
   const int n_blk = (L + kBlock - 1) / kBlock;
   const int32_t* bt = p.block_tables + (size_t)r * p.max_blocks_per_seq;
   // first key position some row of this wave cannot see
@@ -1073,8 +1143,8 @@ __global__ __launch_bounds__(kPPThreads, D == 64 ? 4 : 2) void prefill_paged_att
   const __attribute__((address_space(4))) int32_t* bt_c =
       (const __attribute__((address_space(4))) int32_t*)bt;
   auto block_id = [&](int step) __attribute__((always_inline)) -> int {
-    const int lb = step * (kBN / kBlock) + slot_u;
-    return (step < n_steps && lb < n_blk) ? bt_c[lb] : -1;          // -1: past the end
+    const int lb = vis.step(step) * (kBN / kBlock) + slot_u;
+    return (step < n_steps && lb < n_blk && vis.block(lb)) ? bt_c[lb] : -1;   // -1: past the end, or out of sight
   };
   // lane i of a load: row d = i / (D / 8) of the group, stored chunk
   // i % (D / 8), which holds the row's chunk (i % (D / 8)) ^ swz(d)
@@ -1096,10 +1166,10 @@ __global__ __launch_bounds__(kPPThreads, D == 64 ? 4 : 2) void prefill_paged_att
   // blocks past it) overwritten with zeros once their load has landed:
   // their probabilities are 0, but 0 times a stale NaN or Inf is NaN
   auto zero_tail = [&](uint16_t* buf, int key0) __attribute__((always_inline)) {
-    if (key0 + kBlock > L) {
+    if (vis.zeroes(key0, L)) {
 #pragma unroll
       for (int u = 0; u < kLoads; ++u) {
-        if (key0 + DL::kRows * u + dma_d >= L)
+        if (vis.zero(key0 + DL::kRows * u + dma_d, L))
           *reinterpret_cast<uint4*>(&buf[(kLoads * slot_u + u) * kGrp + 8 * lane]) = make_uint4(0, 0, 0, 0);
       }
     }
@@ -1155,9 +1225,11 @@ __global__ __launch_bounds__(kPPThreads, D == 64 ? 4 : 2) void prefill_paged_att
     for (int dt = 0; dt < DT; ++dt) oacc[dt] = f32x16{};
     f32x16 s_acc[2];             // logits of the step whose softmax is pending
     bf16x8 pb[kBN / 16];         // probabilities of the step whose PV is pending
-    float m_run = -INFINITY;     // running max of the raw (unscaled) logits
-    float l_part[4] = {0.f, 0.f, 0.f, 0.f};
     const float c = p.scale_log2;
+    // running max of the raw (unscaled) logits; under a window a row may see none of
+    // the first steps' keys: finite, so that those weigh 0 and not NaN
+    float m_run = kWindow ? -FLT_MAX / fmaxf(c, 1.f) : -INFINITY;
+    float l_part[4] = {0.f, 0.f, 0.f, 0.f};
 
     // M phase of iteration j: S_j = K_j Q^T, then O += P_{j-1} V_{j-1} (the
     // softmax of S_j can start while the PV MFMAs drain; at normal priority,
@@ -1207,10 +1279,12 @@ __global__ __launch_bounds__(kPPThreads, D == 64 ? 4 : 2) void prefill_paged_att
     // V phase for step x: mask, online softmax, P_x in bf16, row sums
     auto valu_phase = [&](int x) __attribute__((always_inline)) {
       if (x < 0 || x >= n_steps) return;
-      const int kstart = x * kBN;
+      const int kstart = vis.step(x) * kBN;
       // accumulator register rr of tile mt holds key
       //   kstart + 32*mt + 8*(rr/4) + 4*half + rr%4   for query qi
-      if (kstart + kBN - 1 > wave_qmin) {
+      if constexpr (kWindow) {
+        mask_window(p, vis.sinks, kstart, wave_qmin, min(wave_qmin + kNQ - 1, L - 1), qpos, half, s_acc);
+      } else if (kstart + kBN - 1 > wave_qmin) {
         // key kj <= qpos  <=>  its constant offset in the step <= lim
         const int lim = qpos - kstart - 4 * half;
   #pragma unroll
@@ -1278,7 +1352,7 @@ __global__ __launch_bounds__(kPPThreads, D == 64 ? 4 : 2) void prefill_paged_att
       // loads issued two iterations back have landed (vmcnt <= kLoads); the
       // V block read in this iteration gets its tail zeroed; then the barrier
       __builtin_amdgcn_s_waitcnt(D == 128 ? kWaitVmcnt4 : kWaitVmcnt2);
-      if (kB && j >= 1) zero_tail(vprev, (j - 1) * kBN + slot_u * kBlock);
+      if (kB && j >= 1) zero_tail(vprev, vis.step(j - 1) * kBN + slot_u * kBlock);
       __builtin_amdgcn_s_waitcnt(kWaitLgkmcnt0);
       asm volatile("s_barrier" ::: "memory");
       const int id = id_next;
@@ -1334,13 +1408,13 @@ __global__ __launch_bounds__(kPPThreads, D == 64 ? 4 : 2) void prefill_paged_att
 // Launches of less than one round of ping-pong tiles: split tiles (128 rows x
 // 8 waves over two halves of the keys) with direct-to-LDS staging.  At head
 // dim 64, 128 VGPRs and 67,584 bytes of LDS: two work-groups per CU.
-template <int D, bool kPartial>
+template <int D, bool kPartial, bool kWindow>
 __global__ __launch_bounds__(kPPThreads, D == 64 ? 4 : 2) void prefill_paged_attn_ppd_split_kernel(Params p) {
   using DL = DirectLayout<D>;
   constexpr int kBuf = (kBN / DL::kRows) * DL::kGrp;
   __shared__ __attribute__((aligned(16))) uint16_t k0[kBuf], k1[kBuf], k2[kBuf], k3[kBuf];
   __shared__ __attribute__((aligned(16))) uint16_t v0[kBuf], v1[kBuf], v2[kBuf], v3[kBuf];
-  ppd_split_tile<D, false, kPartial>(p, blockIdx.x, TileAt{}, k0, k1, k2, k3, v0, v1, v2, v3);
+  ppd_split_tile<D, false, kPartial, kWindow>(p, blockIdx.x, TileAt{}, k0, k1, k2, k3, v0, v1, v2, v3);
 }
 
 // The output of a split launch with key parts: each (token, head) row
@@ -1473,9 +1547,38 @@ AttnGeometry attn_geometry(int batch, int max_q_len, int max_kv_len, int num_q_h
   return geo;
 }
 
-hipError_t launch_prefill_paged_attn(const AttnLaunch& a, hipStream_t stream) {
-  const AttnGeometry geo = attn_geometry(a.batch, a.max_q_len, a.max_kv_len, a.num_q_heads, a.num_kv_heads,
-                                         a.head_dim, a.cus, a.workspace != nullptr);
+namespace {
+
+template <int D, bool kWindow>
+void launch_prefill(const Params& p, const AttnGeometry& geo, hipStream_t stream) {
+  const dim3 grid((unsigned)geo.grid), block(kPPThreads);
+  if (geo.parts > 1) {
+    // key parts on more work-groups, then the merge of their partials
+    const long long rows_per_block = kThreads / (D / 4);
+    const dim3 mgrid((unsigned)((p.part_rows + rows_per_block - 1) / rows_per_block));
+    hipLaunchKernelGGL((prefill_paged_attn_ppd_split_kernel<D, true, kWindow>), grid, block, 0, stream, p);
+    if (geo.parts == 2)
+      hipLaunchKernelGGL((prefill_split_merge_kernel<D, 2>), mgrid, dim3(kThreads), 0, stream, p);
+    else if (geo.parts <= 4)
+      hipLaunchKernelGGL((prefill_split_merge_kernel<D, 4>), mgrid, dim3(kThreads), 0, stream, p);
+    else
+      hipLaunchKernelGGL((prefill_split_merge_kernel<D, 8>), mgrid, dim3(kThreads), 0, stream, p);
+  } else if (geo.waves != kPPWaves) {
+    // fewer than one ping-pong work-group per CU: 128-row tiles, each run
+    // by 8 waves over two halves of its keys
+    hipLaunchKernelGGL((prefill_paged_attn_ppd_split_kernel<D, false, kWindow>), grid, block, 0, stream, p);
+  } else if (p.even && geo.grid == geo.pp_grid) {
+    hipLaunchKernelGGL((prefill_paged_attn_ppd_kernel<D, PPMode::kEven, kWindow>), grid, block, 0, stream, p);
+  } else if (D == 128 || p.even || geo.grid < (long long)kRoundsWithoutHalves * p.cus) {
+    hipLaunchKernelGGL((prefill_paged_attn_ppd_kernel<D, PPMode::kHalves, kWindow>), grid, block, 0, stream, p);
+  } else if constexpr (D == 64) {
+    hipLaunchKernelGGL((prefill_paged_attn_ppd_kernel<D, PPMode::kRagged, kWindow>), grid, block, 0, stream, p);
+  }
+}
+
+}  // namespace
+
+hipError_t launch_prefill_paged_attn(const AttnLaunch& a, const AttnGeometry& geo, hipStream_t stream) {
   Params p;
   p.q = a.q;
   p.k_pool = a.k_pool;
@@ -1508,49 +1611,12 @@ hipError_t launch_prefill_paged_attn(const AttnLaunch& a, hipStream_t stream) {
   p.part_rows = (long long)a.total_q * a.num_q_heads;
   p.ws_o = static_cast<float*>(a.workspace);
   p.ws_ml = p.ws_o ? p.ws_o + (size_t)geo.parts * p.part_rows * a.head_dim : nullptr;
-  const dim3 grid((unsigned)geo.grid);
-  if (geo.parts > 1) {
-    // key parts on more work-groups, then the merge of their partials
-    const long long rows_per_block = kThreads / (a.head_dim / 4);
-    const dim3 mgrid((unsigned)((p.part_rows + rows_per_block - 1) / rows_per_block));
-    auto merge = [&](auto d_tag) {
-      constexpr int D = decltype(d_tag)::value;
-      hipLaunchKernelGGL((prefill_paged_attn_ppd_split_kernel<D, true>), grid, dim3(kPPThreads), 0, stream, p);
-      if (geo.parts == 2)
-        hipLaunchKernelGGL((prefill_split_merge_kernel<D, 2>), mgrid, dim3(kThreads), 0, stream, p);
-      else if (geo.parts <= 4)
-        hipLaunchKernelGGL((prefill_split_merge_kernel<D, 4>), mgrid, dim3(kThreads), 0, stream, p);
-      else
-        hipLaunchKernelGGL((prefill_split_merge_kernel<D, 8>), mgrid, dim3(kThreads), 0, stream, p);
-    };
-    if (a.head_dim == 128)
-      merge(std::integral_constant<int, 128>{});
-    else
-      merge(std::integral_constant<int, 64>{});
-    return hipGetLastError();
-  }
-  if (geo.waves == kPPWaves) {
-    const bool halves = geo.grid > geo.pp_grid;
-    if (a.head_dim == 128) {
-      if (p.even && !halves) {
-        hipLaunchKernelGGL((prefill_paged_attn_ppd_kernel<128, PPMode::kEven>), grid, dim3(kPPThreads), 0, stream, p);
-      } else {
-        hipLaunchKernelGGL((prefill_paged_attn_ppd_kernel<128, PPMode::kHalves>), grid, dim3(kPPThreads), 0, stream, p);
-      }
-    } else if (p.even && !halves) {
-      hipLaunchKernelGGL((prefill_paged_attn_ppd_kernel<64, PPMode::kEven>), grid, dim3(kPPThreads), 0, stream, p);
-    } else if (p.even || geo.grid < (long long)kRoundsWithoutHalves * a.cus) {
-      hipLaunchKernelGGL((prefill_paged_attn_ppd_kernel<64, PPMode::kHalves>), grid, dim3(kPPThreads), 0, stream, p);
-    } else {
-      hipLaunchKernelGGL((prefill_paged_attn_ppd_kernel<64, PPMode::kRagged>), grid, dim3(kPPThreads), 0, stream, p);
-    }
-  } else if (a.head_dim == 128) {
-    // fewer than one ping-pong work-group per CU: 128-row tiles, each run
-    // by 8 waves over two halves of its keys
-    hipLaunchKernelGGL((prefill_paged_attn_ppd_split_kernel<128, false>), grid, dim3(kPPThreads), 0, stream, p);
-  } else {
-    hipLaunchKernelGGL((prefill_paged_attn_ppd_split_kernel<64, false>), grid, dim3(kPPThreads), 0, stream, p);
-  }
+  p.window = a.win.size;
+  p.sinks = a.win.sinks;
+  if (a.head_dim == 128)
+    a.win.size > 0 ? launch_prefill<128, true>(p, geo, stream) : launch_prefill<128, false>(p, geo, stream);
+  else
+    a.win.size > 0 ? launch_prefill<64, true>(p, geo, stream) : launch_prefill<64, false>(p, geo, stream);
   return hipGetLastError();
 }
 

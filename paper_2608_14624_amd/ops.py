@@ -34,7 +34,11 @@ EXPORTED = ("cs_prefill_paged_attn", "cs_kv_prefetch", "cs_kv_write", "cs_kv_off
             "cs_cascade_decode_workspace_bytes", "cs_prefill_paged_attn_launch_shape",
             "cs_source_digest", "cs_cascade_decode_attn_noalloc", "cs_prefill_paged_attn_ws",
             "cs_prefill_paged_attn_workspace_bytes", "cs_paged_decode_attn_ws",
-            "cs_paged_decode_workspace_bytes")
+            "cs_paged_decode_workspace_bytes", "cs_prefill_window_attn",
+            "cs_prefill_window_workspace_bytes", "cs_decode_window_attn",
+            "cs_decode_window_workspace_bytes", "cs_decode_attn_scores",
+            "cs_decode_scores_workspace_bytes", "cs_prefill_key_scores",
+            "cs_prefill_scores_workspace_bytes", "cs_kv_evict")
 
 # bytes of the device scratch array behind cs_cascade_decode_attn_noalloc
 NOALLOC_SCRATCH_BYTES = 32 * 1024 * 1024
@@ -121,6 +125,19 @@ def _load():
         "cs_prefill_paged_attn_launch_shape": ([i32, i32, i32, i32, i32, ctypes.POINTER(i32),
                                                 ctypes.POINTER(i64), ctypes.POINTER(i64)],
                                                ctypes.c_int),
+        "cs_prefill_window_attn": ([vp] * 6 + [i32] * 10 + [f32, i32, i32, vp, i64, vp, vp],
+                                   ctypes.c_int),
+        "cs_prefill_window_workspace_bytes": ([i32] * 10, i64),
+        "cs_decode_window_attn": ([vp] * 5 + [i32] * 8 + [f32, i32, i32, vp, i64, vp, vp],
+                                  ctypes.c_int),
+        "cs_decode_window_workspace_bytes": ([i32] * 8, i64),
+        "cs_decode_attn_scores": ([vp] * 6 + [i32] * 9 + [f32, f32, vp, vp, i64, vp, vp],
+                                  ctypes.c_int),
+        "cs_decode_scores_workspace_bytes": ([i32] * 7, i64),
+        "cs_prefill_key_scores": ([vp] * 6 + [i32] * 10 + [f32, i32, f32, vp, vp, i64, vp],
+                                  ctypes.c_int),
+        "cs_prefill_scores_workspace_bytes": ([i32] * 7, i64),
+        "cs_kv_evict": ([vp] * 7 + [i32] * 10 + [vp, vp, vp], ctypes.c_int),
     }
     for name, (args, res) in sigs.items():
         fn = getattr(lib, name)
@@ -607,6 +624,258 @@ def cs_cascade_decode_attn_noalloc(q, k_pool, v_pool, block_tables, seq_lens, cu
         int(max_seq_len), block_tables.shape[1], num_blocks, _ptr(cu_groups), _ptr(shared_lens),
         num_groups, int(max_group_seqs), int(max_shared_len), int(max_rest_len), hq, hkv, d, bs,
         float(scale), _ptr(out), _stream_handle(stream, dev)))
+
+
+def cs_prefill_window_attn_raw(q, k_pool, v_pool, block_tables, prefix_lens, cu_q_lens, batch,
+                               total_q, max_q_len, max_kv_len, max_blocks_per_seq, num_blocks,
+                               num_q_heads, num_kv_heads, head_dim, block_size, scale, window, sinks,
+                               workspace, workspace_bytes, out, stream=0):
+    """The C call with raw pointers (ints or None); returns the status code."""
+    return _lib.cs_prefill_window_attn(q, k_pool, v_pool, block_tables, prefix_lens, cu_q_lens, batch,
+                                       total_q, max_q_len, max_kv_len, max_blocks_per_seq, num_blocks,
+                                       num_q_heads, num_kv_heads, head_dim, block_size,
+                                       ctypes.c_float(scale), window, sinks, workspace,
+                                       workspace_bytes, out, stream)
+
+
+def prefill_window_workspace_bytes(batch, total_q, max_q_len, max_kv_len, num_q_heads, num_kv_heads,
+                                   head_dim, window, sinks, num_cus=0):
+    """Bytes of workspace ``cs_prefill_window_attn`` takes (0: none; negative: bad arguments, or
+    no GPU to size for)."""
+    return int(_lib.cs_prefill_window_workspace_bytes(batch, total_q, max_q_len, max_kv_len, num_q_heads,
+                                                      num_kv_heads, head_dim, window, sinks, num_cus))
+
+
+def _workspace(workspace, need, stream, dev):
+    """The workspace of a call that needs ``need`` bytes, as a tensor or None: ``workspace``
+    itself, or ("auto") a new one for work on ``stream``.  On the per-thread stream, which has
+    no pool of its own, it comes from the current stream's, and the caller orders the two."""
+    _require(need >= 0, "no workspace size for these arguments")
+    if isinstance(workspace, str) and workspace == "auto":
+        if need == 0:
+            return None
+        ws = _scratch(need, stream, dev)
+        return _scratch(need, None, dev) if ws is None else ws
+    _require(workspace.is_cuda and workspace.device == dev, f"workspace must be on {dev}")
+    _require(workspace.is_contiguous(), "workspace must be contiguous")
+    return workspace
+
+
+def _nbytes(ws):
+    return 0 if ws is None else ws.numel() * ws.element_size()
+
+
+def cs_prefill_window_attn(q, k_pool, v_pool, block_tables, prefix_lens, cu_q_lens, out, *,
+                           max_q_len, max_kv_len, window, sinks, scale, workspace="auto", stream=None):
+    """Enqueue paged prefill attention with a sliding window on ``stream``: a row sees the last
+    ``window`` positions, its own among them, and the first ``sinks`` tokens.  Tensors and bounds
+    as for :func:`cs_prefill_paged_attn`; ``workspace``: "auto" (allocated here if the launch needs
+    one) or a uint8 GPU tensor of :func:`prefill_window_workspace_bytes`."""
+    args, outp, dev = _prefill_args(q, k_pool, v_pool, block_tables, prefix_lens, cu_q_lens, out,
+                                    max_q_len, max_kv_len, scale)
+    window, sinks = int(window), int(sinks)
+    _require(window >= 1 and sinks >= 0, "window must be positive and sinks not negative")
+    ws = _workspace(workspace, prefill_window_workspace_bytes(args[6], args[7], args[8], args[9], args[12],
+                                                              args[13], args[14], window, sinks), stream, dev)
+    _check(_lib.cs_prefill_window_attn(*args, window, sinks, _ptr(ws), _nbytes(ws), outp,
+                                       _stream_handle(stream, dev)))
+
+
+def _decode_args(q, k_pool, v_pool, block_tables, seq_lens, out, max_seq_len):
+    """Validate a decode call's tensors; its sizes (batch, query heads, KV heads, head_dim, blocks,
+    block size, table width) and the device."""
+    dev = q.device
+    _require_tensors(dev, q.get_device(), ("q", q, _BF16), ("k_pool", k_pool, _BF16),
+                     ("v_pool", v_pool, _BF16), ("out", out, _BF16),
+                     ("block_tables", block_tables, _I32), ("seq_lens", seq_lens, _I32))
+    _require(q.dim() == 3 and out.shape == q.shape, "q and out must be [B, Hq, D]")
+    _require(k_pool.shape == v_pool.shape and k_pool.dim() == 4, "pools must match")
+    batch, hq, d = q.shape
+    num_blocks, hkv, bs, d2 = k_pool.shape
+    _require(d == d2, "head_dim of q and pools differ")
+    _require(block_tables.dim() == 2 and block_tables.shape[0] == batch, "block_tables must be [B, max_blocks]")
+    _require(seq_lens.numel() == batch, "seq_lens must have B entries")
+    return batch, hq, hkv, d, num_blocks, bs, block_tables.shape[1], dev
+
+
+def cs_decode_window_attn_raw(q, k_pool, v_pool, block_tables, seq_lens, batch, max_seq_len,
+                              max_blocks_per_seq, num_blocks, num_q_heads, num_kv_heads, head_dim,
+                              block_size, scale, window, sinks, workspace, workspace_bytes, out, stream=0):
+    """The C call with raw pointers (ints or None); returns the status code."""
+    return _lib.cs_decode_window_attn(q, k_pool, v_pool, block_tables, seq_lens, batch, max_seq_len,
+                                      max_blocks_per_seq, num_blocks, num_q_heads, num_kv_heads, head_dim,
+                                      block_size, ctypes.c_float(scale), window, sinks, workspace,
+                                      workspace_bytes, out, stream)
+
+
+def decode_window_workspace_bytes(batch, max_seq_len, num_q_heads, num_kv_heads, head_dim, window, sinks,
+                                  num_cus=0):
+    """Bytes of workspace ``cs_decode_window_attn`` takes (0: none; negative: bad arguments, or
+    no GPU to size for)."""
+    return int(_lib.cs_decode_window_workspace_bytes(batch, max_seq_len, num_q_heads, num_kv_heads,
+                                                     head_dim, window, sinks, num_cus))
+
+
+def cs_decode_window_attn(q, k_pool, v_pool, block_tables, seq_lens, out, *, max_seq_len, window, sinks,
+                          scale, workspace="auto", stream=None):
+    """Enqueue paged decode attention with a sliding window: the token at the end of every sequence
+    sees its last ``window`` keys and the first ``sinks``.  Tensors as for
+    :func:`cs_paged_decode_attn`; a length of 0 gives a row of zeros.  ``workspace``: "auto"
+    (allocated here) or a uint8 GPU tensor of :func:`decode_window_workspace_bytes`."""
+    batch, hq, hkv, d, num_blocks, bs, width, dev = _decode_args(q, k_pool, v_pool, block_tables, seq_lens,
+                                                                 out, max_seq_len)
+    window, sinks, max_seq_len = int(window), int(sinks), int(max_seq_len)
+    _require(window >= 1 and sinks >= 0, "window must be positive and sinks not negative")
+    ws = _workspace(workspace, decode_window_workspace_bytes(batch, max_seq_len, hq, hkv, d, window, sinks),
+                    stream, dev)
+    _check(_lib.cs_decode_window_attn(_ptr(q), _ptr(k_pool), _ptr(v_pool), _ptr(block_tables), _ptr(seq_lens),
+                                      batch, max_seq_len, width, num_blocks, hq, hkv, d, bs,
+                                      ctypes.c_float(scale), window, sinks, _ptr(ws), _nbytes(ws), _ptr(out),
+                                      _stream_handle(stream, dev)))
+
+
+_F32 = torch.float32
+
+
+def _require_scores(score_pool, k_pool, dev):
+    _require_tensors(dev, k_pool.get_device(), ("score_pool", score_pool, _F32))
+    _require(tuple(score_pool.shape) == tuple(k_pool.shape[:3]), "score_pool must be [num_blocks, Hkv, block_size]")
+
+
+def cs_decode_attn_scores_raw(q, k_pool, v_pool, block_tables, seq_lens, score_from, batch, max_seq_len,
+                              max_scored_len, max_blocks_per_seq, num_blocks, num_q_heads, num_kv_heads,
+                              head_dim, block_size, scale, decay, score_pool, workspace, workspace_bytes,
+                              out, stream=0):
+    """The C call with raw pointers (ints or None); returns the status code."""
+    return _lib.cs_decode_attn_scores(q, k_pool, v_pool, block_tables, seq_lens, score_from, batch,
+                                      max_seq_len, max_scored_len, max_blocks_per_seq, num_blocks,
+                                      num_q_heads, num_kv_heads, head_dim, block_size,
+                                      ctypes.c_float(scale), ctypes.c_float(decay), score_pool, workspace,
+                                      workspace_bytes, out, stream)
+
+
+def decode_scores_workspace_bytes(batch, max_seq_len, max_scored_len, num_q_heads, num_kv_heads, head_dim,
+                                  num_cus=0):
+    """Bytes of workspace ``cs_decode_attn_scores`` takes (negative: bad arguments, or no GPU to
+    size for)."""
+    return int(_lib.cs_decode_scores_workspace_bytes(batch, max_seq_len, max_scored_len, num_q_heads,
+                                                     num_kv_heads, head_dim, num_cus))
+
+
+def cs_decode_attn_scores(q, k_pool, v_pool, block_tables, seq_lens, score_from, score_pool, out, *,
+                          max_seq_len, max_scored_len, scale, decay=1.0, workspace="auto", stream=None):
+    """Enqueue paged decode attention that adds every key's attention weight, summed over the query
+    heads of its KV head, to its score in ``score_pool`` (float32 ``[num_blocks, Hkv, 16]``).  The
+    keys of sequence r from ``score_from[r]`` (int32 ``[B]`` on the GPU) on are scored; their blocks
+    belong to that sequence alone.  Tensors as for :func:`cs_paged_decode_attn`; a length of 0 gives
+    a row of zeros.  ``max_scored_len`` bounds ``seq_lens - score_from``; ``workspace``: "auto"
+    (allocated here) or a uint8 GPU tensor of :func:`decode_scores_workspace_bytes`."""
+    batch, hq, hkv, d, num_blocks, bs, width, dev = _decode_args(q, k_pool, v_pool, block_tables, seq_lens,
+                                                                 out, max_seq_len)
+    _require_tensors(dev, q.get_device(), ("score_from", score_from, _I32))
+    _require(score_from.numel() == batch, "score_from must have B entries")
+    _require_scores(score_pool, k_pool, dev)
+    max_seq_len, max_scored_len = int(max_seq_len), int(max_scored_len)
+    ws = _workspace(workspace, decode_scores_workspace_bytes(batch, max_seq_len, max_scored_len, hq, hkv, d),
+                    stream, dev)
+    _check(_lib.cs_decode_attn_scores(_ptr(q), _ptr(k_pool), _ptr(v_pool), _ptr(block_tables), _ptr(seq_lens),
+                                      _ptr(score_from), batch, max_seq_len, max_scored_len, width, num_blocks,
+                                      hq, hkv, d, bs, ctypes.c_float(scale), ctypes.c_float(decay),
+                                      _ptr(score_pool), _ptr(ws), _nbytes(ws), _ptr(out),
+                                      _stream_handle(stream, dev)))
+
+
+def cs_prefill_key_scores_raw(q, k_pool, block_tables, prefix_lens, cu_q_lens, score_from, batch, total_q,
+                              max_q_len, max_kv_len, max_blocks_per_seq, num_blocks, num_q_heads,
+                              num_kv_heads, head_dim, block_size, scale, rows, decay, score_pool, workspace,
+                              workspace_bytes, stream=0):
+    """The C call with raw pointers (ints or None); returns the status code."""
+    return _lib.cs_prefill_key_scores(q, k_pool, block_tables, prefix_lens, cu_q_lens, score_from, batch,
+                                      total_q, max_q_len, max_kv_len, max_blocks_per_seq, num_blocks,
+                                      num_q_heads, num_kv_heads, head_dim, block_size,
+                                      ctypes.c_float(scale), rows, ctypes.c_float(decay), score_pool,
+                                      workspace, workspace_bytes, stream)
+
+
+def prefill_scores_workspace_bytes(batch, max_q_len, max_kv_len, rows, num_q_heads, num_kv_heads,
+                                   num_cus=0):
+    """Bytes of workspace ``cs_prefill_key_scores`` takes (negative: bad arguments, or no GPU to
+    size for)."""
+    return int(_lib.cs_prefill_scores_workspace_bytes(batch, max_q_len, max_kv_len, rows, num_q_heads,
+                                                      num_kv_heads, num_cus))
+
+
+def cs_prefill_key_scores(q, k_pool, block_tables, prefix_lens, cu_q_lens, score_from, score_pool, *,
+                          max_q_len, max_kv_len, rows, scale, decay=1.0, workspace="auto", stream=None):
+    """Enqueue the scores of a prompt: the attention weights of the last ``rows`` suffix rows of every
+    invocation, summed over them and the query heads of a KV head, into ``score_pool`` (float32
+    ``[num_blocks, Hkv, 16]``).  The suffix's own keys start there, cached ones are added to
+    ``decay`` times what they had.  Tensors as for :func:`cs_prefill_paged_attn`; ``score_from`` as
+    for :func:`cs_decode_attn_scores`; ``workspace``: "auto" (allocated here) or a uint8 GPU tensor
+    of :func:`prefill_scores_workspace_bytes`."""
+    dev = q.device
+    _require_tensors(dev, q.get_device(), ("q", q, _BF16), ("k_pool", k_pool, _BF16),
+                     ("block_tables", block_tables, _I32), ("prefix_lens", prefix_lens, _I32),
+                     ("cu_q_lens", cu_q_lens, _I32), ("score_from", score_from, _I32))
+    _require(q.dim() == 3 and k_pool.dim() == 4 and q.shape[2] == k_pool.shape[3],
+             "q must be [total_q, Hq, D] and the pool [num_blocks, Hkv, block_size, D]")
+    _require(block_tables.dim() == 2, "block_tables must be [B, max_blocks]")
+    total_q, hq, d = q.shape
+    num_blocks, hkv, bs, _ = k_pool.shape
+    batch = block_tables.shape[0]
+    _require(prefix_lens.numel() == batch and cu_q_lens.numel() == batch + 1 and score_from.numel() == batch,
+             "prefix_lens and score_from must have B entries and cu_q_lens B + 1")
+    _require_scores(score_pool, k_pool, dev)
+    max_q_len, max_kv_len, rows = int(max_q_len), int(max_kv_len), int(rows)
+    ws = _workspace(workspace, prefill_scores_workspace_bytes(batch, max_q_len, max_kv_len, rows, hq, hkv),
+                    stream, dev)
+    _check(_lib.cs_prefill_key_scores(_ptr(q), _ptr(k_pool), _ptr(block_tables), _ptr(prefix_lens),
+                                      _ptr(cu_q_lens), _ptr(score_from), batch, total_q, max_q_len,
+                                      max_kv_len, block_tables.shape[1], num_blocks, hq, hkv, d, bs,
+                                      ctypes.c_float(scale), rows, ctypes.c_float(decay), _ptr(score_pool),
+                                      _ptr(ws), _nbytes(ws), _stream_handle(stream, dev)))
+
+
+def cs_kv_evict_raw(score_pool, k_pool, v_pool, block_tables, dst_block_tables, seq_lens, keep_from, batch,
+                    max_seq_len, max_blocks_per_seq, num_blocks, num_kv_heads, head_dim, block_size, budget,
+                    trigger, recent, kept, new_lens, stream=0):
+    """The C call with raw pointers (ints or None); returns the status code."""
+    return _lib.cs_kv_evict(score_pool, k_pool, v_pool, block_tables, dst_block_tables, seq_lens, keep_from,
+                            batch, max_seq_len, max_blocks_per_seq, num_blocks, num_kv_heads, head_dim,
+                            block_size, budget, trigger, recent, kept, new_lens, stream)
+
+
+def cs_kv_evict(score_pool, k_pool, v_pool, block_tables, dst_block_tables, seq_lens, keep_from, kept,
+                new_lens, *, max_seq_len, budget, trigger, recent, stream=None):
+    """Enqueue the eviction of the least attended keys of every sequence with more than ``trigger``
+    keys from ``keep_from[r]`` (int32 ``[B]``) on: each KV head keeps its last ``recent`` keys and
+    those with the largest scores, ``budget`` in all, in ascending order, moved to the positions
+    from ``keep_from[r]`` on (K, V and scores).  ``dst_block_tables``: None (within the sequence's
+    own blocks) or an int32 table like ``block_tables`` that names unused blocks for these
+    positions.  ``kept`` int32 ``[B, Hkv, budget]`` gets the kept keys (a first entry of -1:
+    nothing was evicted), ``new_lens`` int32 ``[B]`` the new lengths (it may be ``seq_lens``)."""
+    dev = k_pool.device
+    tensors = [("k_pool", k_pool, _BF16), ("v_pool", v_pool, _BF16), ("block_tables", block_tables, _I32),
+               ("seq_lens", seq_lens, _I32), ("keep_from", keep_from, _I32), ("kept", kept, _I32),
+               ("new_lens", new_lens, _I32)]
+    if dst_block_tables is not None:
+        tensors.append(("dst_block_tables", dst_block_tables, _I32))
+    _require_tensors(dev, k_pool.get_device(), *tensors)
+    _require(k_pool.shape == v_pool.shape and k_pool.dim() == 4, "pools must match")
+    _require_scores(score_pool, k_pool, dev)
+    _require(block_tables.dim() == 2, "block_tables must be [B, max_blocks]")
+    _require(dst_block_tables is None or dst_block_tables.shape == block_tables.shape,
+             "dst_block_tables must have block_tables' shape")
+    num_blocks, hkv, bs, d = k_pool.shape
+    batch, budget = block_tables.shape[0], int(budget)
+    _require(seq_lens.numel() == batch and keep_from.numel() == batch and new_lens.numel() == batch,
+             "seq_lens, keep_from and new_lens must have B entries")
+    _require(tuple(kept.shape) == (batch, hkv, budget), "kept must be [B, Hkv, budget]")
+    _check(_lib.cs_kv_evict(_ptr(score_pool), _ptr(k_pool), _ptr(v_pool), _ptr(block_tables),
+                            _ptr(dst_block_tables), _ptr(seq_lens), _ptr(keep_from), batch,
+                            int(max_seq_len), block_tables.shape[1], num_blocks, hkv, d, bs, budget,
+                            int(trigger), int(recent), _ptr(kept), _ptr(new_lens),
+                            _stream_handle(stream, dev)))
 
 
 def scout_default_params():

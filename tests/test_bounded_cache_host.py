@@ -1,0 +1,139 @@
+"""Refusals and workspace sizes of the operators that bound a cache, on the CPU: every call here
+returns from its argument checks, or is a documented no-op, before any GPU work."""
+
+
+import pytest
+
+ops = pytest.importorskip("paper_2608_14624_amd.ops",
+                          reason="libcachescout.so not built (run __graft_entry__.build())")
+
+FAKE = 1 << 20   # a 16-byte aligned non-null address; never dereferenced here
+BAD, UNSUPPORTED = ops.CS_ERR_INVALID_ARG, ops.CS_ERR_UNSUPPORTED
+
+HEADS = dict(num_q_heads=8, num_kv_heads=2, head_dim=64, block_size=16)
+PREFILL = dict(q=FAKE, k_pool=FAKE, v_pool=FAKE, block_tables=FAKE, prefix_lens=FAKE, cu_q_lens=FAKE, batch=2,
+               total_q=10, max_q_len=8, max_kv_len=40, max_blocks_per_seq=3, num_blocks=64, **HEADS, scale=0.125,
+               window=16, sinks=4, workspace=None, workspace_bytes=0, out=FAKE)
+DECODE = dict(q=FAKE, k_pool=FAKE, v_pool=FAKE, block_tables=FAKE, seq_lens=FAKE, batch=3, max_seq_len=48,
+              max_blocks_per_seq=3, num_blocks=64, **HEADS, scale=0.125, window=16, sinks=4, workspace=None,
+              workspace_bytes=0, out=FAKE)
+SCORES = dict({k: v for k, v in DECODE.items() if k not in ("window", "sinks")}, score_from=FAKE,
+              max_scored_len=40, decay=1.0, score_pool=FAKE)
+PROMPT = dict({k: v for k, v in PREFILL.items() if k not in ("v_pool", "window", "sinks", "out")},
+              score_from=FAKE, rows=4, decay=1.0, score_pool=FAKE)
+EVICT = dict(score_pool=FAKE, k_pool=FAKE, v_pool=FAKE, block_tables=FAKE, dst_block_tables=None, seq_lens=FAKE,
+             keep_from=FAKE, batch=3, max_seq_len=48, max_blocks_per_seq=3, num_blocks=64, num_kv_heads=2,
+             head_dim=64, block_size=16, budget=8, trigger=8, recent=2, kept=FAKE, new_lens=FAKE)
+CALLS = {
+    "prefill": (ops.cs_prefill_window_attn_raw, PREFILL),
+    "decode": (ops.cs_decode_window_attn_raw, DECODE),
+    "scores": (ops.cs_decode_attn_scores_raw, SCORES),
+    "prompt": (ops.cs_prefill_key_scores_raw, PROMPT),
+    "evict": (ops.cs_kv_evict_raw, EVICT),
+}
+
+
+def call(name, **kw):
+    fn, good = CALLS[name]
+    assert set(kw) <= set(good)
+    return fn(**dict(good, **kw))
+
+
+COMMON = [(dict(batch=-1), BAD), (dict(num_blocks=-1), BAD), (dict(num_blocks=0), BAD),
+          (dict(num_kv_heads=0), BAD), (dict(head_dim=96), UNSUPPORTED), (dict(block_size=32), UNSUPPORTED),
+          (dict(max_blocks_per_seq=2), BAD), (dict(block_tables=None), BAD), (dict(k_pool=FAKE + 8), BAD),
+          (dict(k_pool=None), BAD)]
+ATTENTION = [(dict(num_kv_heads=3), BAD), (dict(scale=float("nan")), BAD), (dict(scale=float("inf")), BAD),
+             (dict(scale=0.0), UNSUPPORTED), (dict(scale=-0.5), UNSUPPORTED), (dict(q=None), BAD),
+             (dict(q=FAKE + 2), BAD)]
+WINDOW = [(dict(window=0), BAD), (dict(window=-3), BAD), (dict(sinks=-1), BAD), (dict(out=None), BAD)]
+SCORING = [(dict(score_pool=None), BAD), (dict(score_pool=FAKE + 4), BAD), (dict(score_from=None), BAD),
+           (dict(decay=-0.1), BAD), (dict(decay=1.1), BAD), (dict(decay=float("nan")), BAD)]
+REFUSALS = {
+    "prefill": COMMON + ATTENTION + WINDOW + [(dict(max_q_len=41), BAD), (dict(total_q=-1), BAD),
+                                              (dict(workspace_bytes=-1), BAD), (dict(out=FAKE + 8), BAD)],
+    "decode": COMMON + ATTENTION + WINDOW + [(dict(num_q_heads=34), UNSUPPORTED), (dict(max_seq_len=0), BAD),
+                                             (dict(workspace_bytes=-1), BAD)],
+    "scores": COMMON + ATTENTION + SCORING + [(dict(num_q_heads=34), UNSUPPORTED), (dict(max_scored_len=49), BAD),
+                                              (dict(max_scored_len=-1), BAD), (dict(out=None), BAD)],
+    "prompt": COMMON + ATTENTION + SCORING + [(dict(rows=0), BAD), (dict(max_q_len=41), BAD),
+                                              (dict(total_q=-1), BAD), (dict(workspace_bytes=-1), BAD)],
+    "evict": COMMON + [(dict(budget=0), BAD), (dict(trigger=7), BAD), (dict(recent=9), BAD), (dict(recent=-1), BAD),
+                       (dict(kept=None), BAD), (dict(new_lens=None), BAD), (dict(keep_from=None), BAD),
+                       (dict(seq_lens=None), BAD), (dict(score_pool=FAKE + 8), BAD), (dict(max_seq_len=-1), BAD),
+                       (dict(batch=2 ** 30, num_kv_heads=8), BAD)],
+}
+
+
+@pytest.mark.parametrize("name,kw,status", [(n, kw, st) for n, cases in REFUSALS.items() for kw, st in cases])
+def test_bad_arguments_are_refused(name, kw, status):
+    assert call(name, **kw) == status
+    assert ops.last_error() != ""
+
+
+@pytest.mark.parametrize("name,kw", [(n, dict(batch=0)) for n in CALLS] + [
+    ("prefill", dict(total_q=0)), ("prefill", dict(max_q_len=0)), ("prompt", dict(total_q=0)),
+    ("prompt", dict(max_q_len=0)), ("decode", dict(batch=0, q=None, out=None)),
+    ("evict", dict(batch=0, kept=None, score_pool=None))])
+def test_empty_work_is_a_noop(name, kw):
+    assert call(name, **kw) == ops.CS_OK
+    assert ops.last_error() == ""
+
+
+def test_window_workspaces_follow_what_is_in_sight():
+    cu = 256
+    # 16 tokens on 6000: key parts over the whole length, over a long window, none over a short one
+    full = ops.prefill_workspace_bytes(1, 16, 16, 6016, 32, 8, 128, cu)
+    assert ops.prefill_window_workspace_bytes(1, 16, 16, 6016, 32, 8, 128, 6016, 0, cu) == full > 0
+    assert 0 < ops.prefill_window_workspace_bytes(1, 16, 16, 6016, 32, 8, 128, 1200, 4, cu) < full
+    assert ops.prefill_window_workspace_bytes(1, 16, 16, 6016, 32, 8, 128, 500, 4, cu) == 0
+    plain = ops.paged_decode_workspace_bytes(3, 6000, 32, 8, 128, cu)
+    assert ops.decode_window_workspace_bytes(3, 6000, 32, 8, 128, 1000, 4, cu) == plain > 0
+    assert ops.decode_window_workspace_bytes(3, 6000, 32, 8, 128, 60, 4, cu) == 0      # 126 keys at most
+    assert ops.decode_window_workspace_bytes(3, 6000, 32, 8, 128, 2 ** 31 - 1, 2 ** 31 - 1, cu) == plain
+    for bad in (dict(window=0), dict(sinks=-1)):
+        assert ops.decode_window_workspace_bytes(3, 6000, 32, 8, 128, **{"window": 5, "sinks": 0, **bad}, num_cus=cu) < 0
+        assert ops.prefill_window_workspace_bytes(1, 16, 16, 6016, 32, 8, 128, **{"window": 5, "sinks": 0, **bad},
+                                                  num_cus=cu) < 0
+
+
+def test_scores_workspace_holds_the_logits_of_the_scored_units():
+    cu = 256
+    ranges = ops.paged_decode_workspace_bytes(3, 6000, 32, 8, 128, cu)
+    for n in (1, 2, 31, 32, 33, 4000, 6000):
+        # a sequence of n scored keys spans at most this many units of 32, wherever it starts
+        units = max((start + n - 1) // 32 - start // 32 + 1 for start in range(32))
+        assert ops.decode_scores_workspace_bytes(3, 6000, n, 32, 8, 128, cu) == ranges + 3 * 32 * units * 32 * 4
+    assert ops.decode_scores_workspace_bytes(3, 6000, 0, 32, 8, 128, cu) == ranges
+    assert ops.decode_scores_workspace_bytes(3, 6000, 6001, 32, 8, 128, cu) < 0
+    assert ops.decode_scores_workspace_bytes(3, 100, -1, 32, 8, 128, cu) < 0
+    assert ops.decode_scores_workspace_bytes(3, 100, 10, 32, 5, 128, cu) < 0
+
+
+def test_prompt_scores_workspace():
+    cu = 256
+    one = ops.prefill_scores_workspace_bytes(32, 2000, 5000, 2000, 32, 8, cu)
+    assert one == 32 * 32 * 2000 * 8                       # a row's statistics, in one part
+    assert ops.prefill_scores_workspace_bytes(32, 2000, 5000, 10 ** 9, 32, 8, cu) == one
+    few = ops.prefill_scores_workspace_bytes(1, 500, 5000, 32, 32, 8, cu)
+    assert few % (32 * 32 * 8) == 0 and few > 32 * 32 * 8   # several parts
+    assert ops.prefill_scores_workspace_bytes(0, 500, 5000, 32, 32, 8, cu) == 0
+    assert ops.prefill_scores_workspace_bytes(1, 500, 5000, 0, 32, 8, cu) < 0
+    assert ops.prefill_scores_workspace_bytes(1, 500, 5000, 3, 32, 5, cu) < 0
+
+
+def test_binding_checks_tensors():
+    import torch
+    k = torch.zeros(4, 2, 16, 64, dtype=torch.bfloat16)
+    i = torch.zeros(2, dtype=torch.int32)
+    t = torch.zeros(2, 2, dtype=torch.int32)
+    q = torch.zeros(2, 8, 64, dtype=torch.bfloat16)
+    s = torch.zeros(4, 2, 16)
+    for fn in (lambda: ops.cs_decode_window_attn(q, k, k, t, i, q, max_seq_len=32, window=4, sinks=0, scale=0.1),
+               lambda: ops.cs_prefill_window_attn(q, k, k, t, i, i, q, max_q_len=2, max_kv_len=32, window=4, sinks=0,
+                                                  scale=0.1),
+               lambda: ops.cs_decode_attn_scores(q, k, k, t, i, i, s, q, max_seq_len=32, max_scored_len=3, scale=0.1),
+               lambda: ops.cs_prefill_key_scores(q, k, t, i, i, i, s, max_q_len=2, max_kv_len=32, rows=3, scale=0.1),
+               lambda: ops.cs_kv_evict(s, k, k, t, None, i, i, t, i, max_seq_len=32, budget=4, trigger=4, recent=1)):
+        with pytest.raises(ops.CacheScoutError, match="must be on"):
+            fn()
