@@ -570,7 +570,7 @@ int64_t cs_decode_scores_workspace_bytes(int32_t batch, int32_t max_seq_len, int
  *   decay          in [0, 1], else CS_ERR_INVALID_ARG.
  *   score_pool     as in cs_decode_attn_scores.
  *   workspace      device, 16-byte aligned, caller-owned scratch of at least
- *                  cs_prefill_scores_workspace_bytes(batch, max_q_len,
+ *                  cs_prefill_scores_workspace_bytes(batch, total_q, max_q_len,
  *                  max_kv_len, rows, num_q_heads, num_kv_heads, 0) bytes; calls
  *                  that share one must be ordered on one stream.
  *   workspace_bytes  its size; smaller than required -> CS_ERR_INVALID_ARG.
@@ -588,9 +588,9 @@ int cs_prefill_key_scores(const void *q, const void *k_pool, const int32_t *bloc
 /* Workspace bytes cs_prefill_key_scores needs.  num_cus: compute units to size
  * for, 0 = the current device's (-1 if there is none).  -1 for a negative size,
  * rows below 1 or bad head counts. */
-int64_t cs_prefill_scores_workspace_bytes(int32_t batch, int32_t max_q_len, int32_t max_kv_len,
-                                          int32_t rows, int32_t num_q_heads, int32_t num_kv_heads,
-                                          int32_t num_cus);
+int64_t cs_prefill_scores_workspace_bytes(int32_t batch, int32_t total_q, int32_t max_q_len,
+                                          int32_t max_kv_len, int32_t rows, int32_t num_q_heads,
+                                          int32_t num_kv_heads, int32_t num_cus);
 
 /*
  * Eviction within sequences by accumulated attention weight.

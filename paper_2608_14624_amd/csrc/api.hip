@@ -866,14 +866,18 @@ int cs_prefill_key_scores(const void* q, const void* k_pool, const int32_t* bloc
   hipError_t e = cs::current_device_cus(&cus);
   if (e != hipSuccess) return hip_fail(e, "compute-unit count of the current device");
   cs::KeyScoreLaunch a;
-  a.geo = cs::key_score_geometry(batch, max_q_len, max_kv_len, rows, num_q_heads, num_kv_heads, cus);
+  a.geo = cs::key_score_geometry(batch, total_q, max_q_len, max_kv_len, rows, num_q_heads, num_kv_heads, cus);
   if (a.geo.stat_grid > 0x7fffffffLL || a.geo.weight_grid > 0x7fffffffLL)
     return fail(CS_ERR_INVALID_ARG, "launch too large");
+  // (rows are divided by the group with a 32-bit reciprocal)
+  const long long group = num_q_heads / num_kv_heads;
+  if (a.geo.max_rows * group * group > 0xffffffffLL)
+    return fail(CS_ERR_UNSUPPORTED, "%d rows of %lld query heads per KV head", a.geo.max_rows, group);
   if (!workspace || !aligned16(workspace))
     return fail(CS_ERR_INVALID_ARG, "workspace must be a 16-byte aligned device buffer");
-  if (workspace_bytes < a.geo.stat_bytes)
+  if (workspace_bytes < a.geo.bytes)
     return fail(CS_ERR_INVALID_ARG, "workspace_bytes %lld < %lld required", (long long)workspace_bytes,
-                (long long)a.geo.stat_bytes);
+                (long long)a.geo.bytes);
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   if (debug_checks_enabled()) {
     int st = debug_check_attn(block_tables, prefix_lens, cu_q_lens, batch, total_q, max_q_len, max_kv_len,
@@ -908,15 +912,17 @@ int cs_prefill_key_scores(const void* q, const void* k_pool, const int32_t* bloc
   return ok();
 }
 
-int64_t cs_prefill_scores_workspace_bytes(int32_t batch, int32_t max_q_len, int32_t max_kv_len, int32_t rows,
-                                          int32_t num_q_heads, int32_t num_kv_heads, int32_t num_cus) {
-  if (batch < 0 || max_q_len < 0 || max_kv_len < 0 || rows < 1 || num_cus < 0 || num_q_heads <= 0 ||
+int64_t cs_prefill_scores_workspace_bytes(int32_t batch, int32_t total_q, int32_t max_q_len, int32_t max_kv_len,
+                                          int32_t rows, int32_t num_q_heads, int32_t num_kv_heads,
+                                          int32_t num_cus) {
+  if (batch < 0 || total_q < 0 || max_q_len < 0 || max_kv_len < 0 || rows < 1 || num_cus < 0 || num_q_heads <= 0 ||
       num_kv_heads <= 0 || num_q_heads % num_kv_heads != 0)
     return -1;
-  if (batch == 0 || max_q_len == 0) return 0;
+  if (batch == 0 || total_q == 0 || max_q_len == 0) return 0;
   int cus = num_cus;
   if (cus == 0 && cs::current_device_cus(&cus) != hipSuccess) return -1;
-  return cs::key_score_geometry(batch, max_q_len, max_kv_len, rows, num_q_heads, num_kv_heads, cus).stat_bytes;
+  return cs::key_score_geometry(batch, total_q, max_q_len, max_kv_len, rows, num_q_heads, num_kv_heads, cus)
+      .bytes;
 }
 
 int cs_kv_evict(float* score_pool, void* k_pool, void* v_pool, const int32_t* block_tables,

@@ -165,13 +165,16 @@ struct KeyScoreGeometry {
   int max_rows;             // observed rows of any invocation
   int parts;                // key parts of the row statistics
   long long row_tiles;      // statistics work-groups per (invocation, KV head) and part
-  long long key_tiles;      // weights work-groups per (invocation, KV head)
+  long long key_tiles;      // key tiles of the longest invocation
+  long long weight_groups;  // weights work-groups per (invocation, KV head)
+  bool splits_rows;         // some key tile's rows may be split over several of them
   long long stat_grid;
   long long weight_grid;
-  long long stat_bytes;     // workspace
+  long long stat_bytes;     // workspace of the statistics, and all of it
+  long long bytes;
 };
-KeyScoreGeometry key_score_geometry(int batch, int max_q_len, int max_kv_len, int rows, int num_q_heads,
-                                    int num_kv_heads, int cus);
+KeyScoreGeometry key_score_geometry(int batch, int total_q, int max_q_len, int max_kv_len, int rows,
+                                    int num_q_heads, int num_kv_heads, int cus);
 
 struct KeyScoreLaunch {
   const uint16_t* q;

@@ -67,6 +67,7 @@
 // l) to a workspace instead of the output.  The other half (each sequence's
 // own keys) and the log-sum-exp merge run in the decode kernel.  This kernel
 // stages K and V through registers into a double-buffered LDS tile.
+#include "direct_lds.h"
 #include "internal.h"
 #include "wave_ops.h"
 
@@ -148,50 +149,6 @@ struct Lds {
   uint16_t k[2][kBN * kStride];               // K of steps j (even/odd buffer)
   uint16_t v[2][kBN * vStride];               // V of steps j
 };
-
-// Direct-to-LDS staging (the ppd kernels).  buffer_load_dwordx4 with the
-// LDS flag writes lane i's 16 bytes at the instruction's LDS address + 16 i,
-// so one load moves 1 KB of a (block, head) tile: four 256-byte rows at
-// D = 128, eight 128-byte rows at D = 64 (a "group").  Which 16-byte chunk
-// each lane fetches is free, so the layout inside a group is any
-// permutation of its chunks.  A buffer holds one 64-key step as 16 (D = 128)
-// or 8 (D = 64) groups.
-//   D = 128: groups 4 D + 8 elements apart (16 bytes of padding); chunk s of
-//            row d holds the row's chunk s ^ 4d.
-//   D = 64:  groups 8 D + 16 elements apart (32 bytes); chunk s of row d
-//            holds the row's chunk s ^ y(d), y(d) = 4 ((d / 2) % 2) + d / 4.
-// The K operand reads (ds_read_b128: 16 lanes, one chunk of 16 rows, per
-// pass) and the transposing V reads (32 lanes, 64 bytes of 4 rows, per pass)
-// are then free of bank conflicts at 64 banks (checked element by element,
-// with the bank of every access, in the host layout test), and every
-// per-lane address is one register plus a constant.  Buffer loads rather
-// than global_load_lds: the compiler's wait insertion counts a global load
-// into LDS as a flat access and then makes every LDS read wait for all loads
-// in flight; with buffer loads it keeps exact counts.
-template <int D>
-struct DirectLayout;
-template <>
-struct DirectLayout<128> {
-  static constexpr int kRows = 4;                 // rows per 1 KB group
-  static constexpr int kGrp = 4 * 128 + 8;        // elements from group to group
-  static __device__ __forceinline__ int swz(int d) { return 4 * d; }
-};
-template <>
-struct DirectLayout<64> {
-  static constexpr int kRows = 8;
-  static constexpr int kGrp = 8 * 64 + 16;
-  static __device__ __forceinline__ int swz(int d) { return 4 * ((d >> 1) & 1) + (d >> 2); }
-};
-//
-// Word 3 of a raw buffer descriptor on gfx9-family parts: 32-bit data format
-// (DATA_FORMAT = 4), no swizzle, no index stride.
-constexpr int kRawBufferWord3 = 0x00020000;
-// s_waitcnt immediates (gfx9 layout: vmcnt[3:0], expcnt[6:4], lgkmcnt[11:8],
-// vmcnt[5:4] at [15:14]; a field at its maximum does not wait)
-constexpr int kWaitVmcnt0 = 0x0F70;
-constexpr int kWaitVmcnt2 = 0x0F72;
-constexpr int kWaitVmcnt4 = 0x0F74;
-constexpr int kWaitLgkmcnt0 = 0xC07F;
 
 __device__ __forceinline__ bf16x8 as_bf16x8(uint4 v) { return __builtin_bit_cast(bf16x8, v); }
 

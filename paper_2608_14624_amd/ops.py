@@ -136,7 +136,7 @@ def _load():
         "cs_decode_scores_workspace_bytes": ([i32] * 7, i64),
         "cs_prefill_key_scores": ([vp] * 6 + [i32] * 10 + [f32, i32, f32, vp, vp, i64, vp],
                                   ctypes.c_int),
-        "cs_prefill_scores_workspace_bytes": ([i32] * 7, i64),
+        "cs_prefill_scores_workspace_bytes": ([i32] * 8, i64),
         "cs_kv_evict": ([vp] * 7 + [i32] * 10 + [vp, vp, vp], ctypes.c_int),
     }
     for name, (args, res) in sigs.items():
@@ -797,12 +797,12 @@ def cs_prefill_key_scores_raw(q, k_pool, block_tables, prefix_lens, cu_q_lens, s
                                       workspace, workspace_bytes, stream)
 
 
-def prefill_scores_workspace_bytes(batch, max_q_len, max_kv_len, rows, num_q_heads, num_kv_heads,
+def prefill_scores_workspace_bytes(batch, total_q, max_q_len, max_kv_len, rows, num_q_heads, num_kv_heads,
                                    num_cus=0):
     """Bytes of workspace ``cs_prefill_key_scores`` takes (negative: bad arguments, or no GPU to
     size for)."""
-    return int(_lib.cs_prefill_scores_workspace_bytes(batch, max_q_len, max_kv_len, rows, num_q_heads,
-                                                      num_kv_heads, num_cus))
+    return int(_lib.cs_prefill_scores_workspace_bytes(batch, total_q, max_q_len, max_kv_len, rows,
+                                                      num_q_heads, num_kv_heads, num_cus))
 
 
 def cs_prefill_key_scores(q, k_pool, block_tables, prefix_lens, cu_q_lens, score_from, score_pool, *,
@@ -827,8 +827,8 @@ def cs_prefill_key_scores(q, k_pool, block_tables, prefix_lens, cu_q_lens, score
              "prefix_lens and score_from must have B entries and cu_q_lens B + 1")
     _require_scores(score_pool, k_pool, dev)
     max_q_len, max_kv_len, rows = int(max_q_len), int(max_kv_len), int(rows)
-    ws = _workspace(workspace, prefill_scores_workspace_bytes(batch, max_q_len, max_kv_len, rows, hq, hkv),
-                    stream, dev)
+    ws = _workspace(workspace, prefill_scores_workspace_bytes(batch, total_q, max_q_len, max_kv_len, rows, hq,
+                                                              hkv), stream, dev)
     _check(_lib.cs_prefill_key_scores(_ptr(q), _ptr(k_pool), _ptr(block_tables), _ptr(prefix_lens),
                                       _ptr(cu_q_lens), _ptr(score_from), batch, total_q, max_q_len,
                                       max_kv_len, block_tables.shape[1], num_blocks, hq, hkv, d, bs,

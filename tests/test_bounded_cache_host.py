@@ -112,14 +112,18 @@ def test_scores_workspace_holds_the_logits_of_the_scored_units():
 
 def test_prompt_scores_workspace():
     cu = 256
-    one = ops.prefill_scores_workspace_bytes(32, 2000, 5000, 2000, 32, 8, cu)
-    assert one == 32 * 32 * 2000 * 8                       # a row's statistics, in one part
-    assert ops.prefill_scores_workspace_bytes(32, 2000, 5000, 10 ** 9, 32, 8, cu) == one
-    few = ops.prefill_scores_workspace_bytes(1, 500, 5000, 32, 32, 8, cu)
-    assert few % (32 * 32 * 8) == 0 and few > 32 * 32 * 8   # several parts
-    assert ops.prefill_scores_workspace_bytes(0, 500, 5000, 32, 32, 8, cu) == 0
-    assert ops.prefill_scores_workspace_bytes(1, 500, 5000, 0, 32, 8, cu) < 0
-    assert ops.prefill_scores_workspace_bytes(1, 500, 5000, 3, 32, 5, cu) < 0
+
+    def need(batch, total_q, max_q, max_kv, rows):
+        return ops.prefill_scores_workspace_bytes(batch, total_q, max_q, max_kv, rows, 32, 8, cu)
+    many = need(32, 64000, 2000, 5000, 2000)
+    # every row's statistics in one part, and a sum per key of every key tile of 128
+    assert many == 32 * 32 * 2000 * 8 + 32 * 8 * 40 * 128 * 4
+    assert need(32, 64000, 2000, 5000, 10 ** 9) == many
+    few = need(1, 500, 500, 5000, 32)
+    assert few == 9 * 32 * 32 * 8                            # key parts of 8 or 9 steps; no rows are split
+    assert need(0, 500, 500, 5000, 32) == need(1, 0, 500, 5000, 32) == need(1, 500, 0, 5000, 32) == 0
+    assert need(1, 500, 500, 5000, 0) < 0 and need(1, -1, 500, 5000, 32) < 0
+    assert ops.prefill_scores_workspace_bytes(1, 500, 500, 5000, 3, 32, 5, cu) < 0
 
 
 def test_binding_checks_tensors():
