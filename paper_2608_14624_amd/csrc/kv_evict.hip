@@ -201,10 +201,10 @@ __device__ __forceinline__ void store_new_len(const EvictParams& p, int r, bool 
 
 // Rows i = -lead .. budget - 1 of a sequence and KV head into other blocks, where lead
 // keys before keep_from lie in its block and come along.  HBM bound: a third of the rows
-// of scattered 4 KiB tiles is read, in 256-byte pieces.  48 sequences to 2048 of 3000-9000
-// keys, 8 heads of 128 (830 MB in all), with the selection: 205.6 us with 64 rows per
+// of scattered 4 KiB tiles is read, in 256-byte pieces.  52 sequences to 2048 of 3000-9000
+// keys, 8 heads of 128 (870 MB), with the selection: 205.6 us with 64 rows per
 // work-group and ordinary stores, 202.0 with 32 rows, 200.6 with 64 and non-temporal
-// stores, 197.1 with both (of which 175 are the copy, 4.7 TB/s); non-temporal loads too
+// stores, 197.1 with both (of which 175 are the copy, 5.0 TB/s); non-temporal loads too
 // 194.0, but 14.3 us for 3 sequences to 1024 keys instead of 13.7.
 template <int D>
 __global__ __launch_bounds__(kCopyThreads) void evict_copy_kernel(EvictParams p) {
