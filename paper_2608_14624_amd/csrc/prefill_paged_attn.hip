@@ -218,31 +218,30 @@ __device__ __forceinline__ bool even_tile(const Params& p, int wg, TileAt& t) {
 }
 
 // What the rows of a tile at positions qlo .. kv_end - 1 see under a window: the keys
-// below `sinks` and those from `lo` on.  The 64-key steps that hold none of them are
-// left out, so the tile's step j is the sequence's step j, or (j past the sinks)
-// j + skip; without a window nothing is left out.  A pool block in a step that no row
+// below `sinks` and those from `lo` on.  Steps of 64 keys cover the sinks, and others,
+// from lo's block on, the window: the first key of step j is start(j); without a window,
+// or where the two meet, the steps cover everything.  A pool block in a step that no row
 // sees is never read (its table entry may name a recycled block, or none), and V rows of
 // keys that no row sees are zeroed as those past the sequence's end are: a probability
 // of 0 times a NaN there would not be 0.
 template <bool kWindow>
 struct Visible {
-  int sinks, lo, sink_steps, skip;
+  int sinks, lo, sink_steps, gap;       // gap: keys left out between the two
   __device__ __forceinline__ Visible(const Params& p, int qlo, int kv_end) {
     if constexpr (kWindow) {
       sinks = min(p.sinks, kv_end);
       lo = max(0, qlo - p.window + 1);
       sink_steps = ceil_div(sinks, kBN);
-      skip = max(0, lo / kBN - sink_steps);
+      gap = max(0, lo / kBlock * kBlock - sink_steps * kBN);
     }
   }
-  __device__ __forceinline__ int step(int j) const {
-    if constexpr (kWindow) return j < sink_steps ? j : j + skip;
-    else return j;
+  __device__ __forceinline__ int start(int j) const {
+    if constexpr (kWindow) return j < sink_steps ? j * kBN : j * kBN + gap;
+    else return j * kBN;
   }
   __device__ __forceinline__ int steps(int kv_end) const {
-    const int all = (kv_end + kBN - 1) / kBN;
-    if constexpr (kWindow) return all - skip;
-    else return all;
+    if constexpr (kWindow) return (kv_end - gap + kBN - 1) / kBN;
+    else return (kv_end + kBN - 1) / kBN;
   }
   __device__ __forceinline__ bool block(int lb) const {
     if constexpr (kWindow) return lb * kBlock < sinks || (lb + 1) * kBlock > lo;
@@ -260,23 +259,40 @@ struct Visible {
 };
 
 // The logits of a windowed step for a wave whose rows are at positions qmin .. qmax
-// (its lane's at qpos): keys the row does not see become -inf.  Steps that every row
-// sees whole are passed by.
+// (its lane's at qpos): keys the row does not see become -inf.  Most steps are seen
+// whole; of the others nearly all are cut by one edge alone, the diagonal, the window's
+// or the sinks', and at head_dim 128 take one comparison per key instead of three (32
+// ragged invocations, window 1024: 1010 -> 976 us).  At 64, where registers are short, the
+// code of the four cases costs the loop more than they save (46.2 us in one, 47.5 in four).
+template <int D>
 __device__ __forceinline__ void mask_window(const Params& p, int sinks, int kstart, int qmin, int qmax, int qpos,
                                             int half, f32x16 (&s)[2]) {
-  if (kstart + kBN - 1 <= qmin && (kstart > qmax - p.window || kstart + kBN <= sinks)) return;
-  // in the step, the lane's key of constant offset o is visible if o <= last and o > old or o < sink
+  const bool causal = kstart + kBN - 1 > qmin;                  // some row does not reach some key
+  const bool old = kstart <= qmax - p.window;                    // some row's window has left some key
+  const bool gone = kstart + kBN - 1 <= qmin - p.window;         // all rows' have left all keys
+  // in the step, the lane's key of constant offset o is visible if o <= last and
+  // (o > first or o < sink)
   const int last = qpos - kstart - 4 * half;
-  const int old = last - p.window;
+  const int first = last - p.window;
   const int sink = sinks - kstart - 4 * half;
+  auto keep = [&](auto visible) __attribute__((always_inline)) {
 #pragma unroll
-  for (int mt = 0; mt < 2; ++mt) {
+    for (int mt = 0; mt < 2; ++mt)
 #pragma unroll
-    for (int rr = 0; rr < 16; ++rr) {
-      const int o = mt * 32 + 8 * (rr >> 2) + (rr & 3);
-      s[mt][rr] = (o <= last && (o > old || o < sink)) ? s[mt][rr] : -INFINITY;
-    }
-  }
+      for (int rr = 0; rr < 16; ++rr)
+        s[mt][rr] = visible(mt * 32 + 8 * (rr >> 2) + (rr & 3)) ? s[mt][rr] : -INFINITY;
+  };
+  if (!causal && (!old || kstart + kBN <= sinks)) return;
+  if (D == 64)
+    keep([&](int o) { return o <= last && (o > first || o < sink); });
+  else if (!old || kstart + kBN <= sinks)
+    keep([&](int o) { return o <= last; });
+  else if (!causal && gone)
+    keep([&](int o) { return o < sink; });
+  else if (!causal && kstart >= sinks)
+    keep([&](int o) { return o > first; });
+  else
+    keep([&](int o) { return o <= last && (o > first || o < sink); });
 }
 
 // The same in any other batch; false: no tile is left for the work-group.
@@ -754,7 +770,7 @@ __device__ __forceinline__ void ppd_split_tile(const Params& p, const int wg, co
   const __attribute__((address_space(4))) int32_t* bt_c =
       (const __attribute__((address_space(4))) int32_t*)bt;
   auto block_id = [&](int step) __attribute__((always_inline)) -> int {
-    const int lb = vis.step(j0 + step) * (kBN / kBlock) + slot_u;
+    const int lb = vis.start(j0 + step) / kBlock + slot_u;
     return (step < n_steps && lb < n_blk && vis.block(lb)) ? bt_c[lb] : -1;   // -1: past the end, or out of sight
   };
   // staging and operand addressing as in the ppd kernel (DirectLayout<D>)
@@ -821,7 +837,7 @@ __device__ __forceinline__ void ppd_split_tile(const Params& p, const int wg, co
 
   // logits, mask, online softmax and PV product of step j
   auto step = [&](const int j, const uint16_t* kbuf, const uint16_t* vbuf) __attribute__((always_inline)) {
-    const int kstart = vis.step(j0 + j) * kBN;
+    const int kstart = vis.start(j0 + j);
     f32x16 s_cur[2];
     s_cur[0] = f32x16{};
     s_cur[1] = f32x16{};
@@ -846,7 +862,7 @@ __device__ __forceinline__ void ppd_split_tile(const Params& p, const int wg, co
     // accumulator register rr of tile mt holds key
     //   kstart + 32*mt + 8*(rr/4) + 4*half + rr%4   for query qi
     if constexpr (kWindow) {
-      mask_window(p, vis.sinks, kstart, wave_qmin, min(wave_qmin + kNQ - 1, L - 1), qpos, half, s_cur);
+      mask_window<D>(p, vis.sinks, kstart, wave_qmin, min(wave_qmin + kNQ - 1, L - 1), qpos, half, s_cur);
     } else if (kstart + kBN - 1 > wave_qmin) {
       // key kj <= qpos  <=>  its constant offset in the step <= lim
       const int lim = qpos - kstart - 4 * half;
@@ -924,7 +940,7 @@ __device__ __forceinline__ void ppd_split_tile(const Params& p, const int wg, co
     auto iteration = [&](const int j, uint16_t* kcur, uint16_t* vcur, uint16_t* knext,
                          uint16_t* vnext) __attribute__((always_inline)) {
       __builtin_amdgcn_s_waitcnt(kWaitVmcnt0);
-      if (j < n_steps) zero_tail(vcur, vis.step(j0 + j) * kBN + slot_u * kBlock);
+      if (j < n_steps) zero_tail(vcur, vis.start(j0 + j) + slot_u * kBlock);
       __builtin_amdgcn_s_waitcnt(kWaitLgkmcnt0);
       asm volatile("s_barrier" ::: "memory");
       if (j + 1 < n_steps) {
@@ -1100,7 +1116,7 @@ __global__ __launch_bounds__(kPPThreads, D == 64 ? 4 : 2) void prefill_paged_att
   const __attribute__((address_space(4))) int32_t* bt_c =
       (const __attribute__((address_space(4))) int32_t*)bt;
   auto block_id = [&](int step) __attribute__((always_inline)) -> int {
-    const int lb = vis.step(step) * (kBN / kBlock) + slot_u;
+    const int lb = vis.start(step) / kBlock + slot_u;
     return (step < n_steps && lb < n_blk && vis.block(lb)) ? bt_c[lb] : -1;   // -1: past the end, or out of sight
   };
   // lane i of a load: row d = i / (D / 8) of the group, stored chunk
@@ -1236,11 +1252,11 @@ __global__ __launch_bounds__(kPPThreads, D == 64 ? 4 : 2) void prefill_paged_att
     // V phase for step x: mask, online softmax, P_x in bf16, row sums
     auto valu_phase = [&](int x) __attribute__((always_inline)) {
       if (x < 0 || x >= n_steps) return;
-      const int kstart = vis.step(x) * kBN;
+      const int kstart = vis.start(x);
       // accumulator register rr of tile mt holds key
       //   kstart + 32*mt + 8*(rr/4) + 4*half + rr%4   for query qi
       if constexpr (kWindow) {
-        mask_window(p, vis.sinks, kstart, wave_qmin, min(wave_qmin + kNQ - 1, L - 1), qpos, half, s_acc);
+        mask_window<D>(p, vis.sinks, kstart, wave_qmin, min(wave_qmin + kNQ - 1, L - 1), qpos, half, s_acc);
       } else if (kstart + kBN - 1 > wave_qmin) {
         // key kj <= qpos  <=>  its constant offset in the step <= lim
         const int lim = qpos - kstart - 4 * half;
@@ -1309,7 +1325,7 @@ __global__ __launch_bounds__(kPPThreads, D == 64 ? 4 : 2) void prefill_paged_att
       // loads issued two iterations back have landed (vmcnt <= kLoads); the
       // V block read in this iteration gets its tail zeroed; then the barrier
       __builtin_amdgcn_s_waitcnt(D == 128 ? kWaitVmcnt4 : kWaitVmcnt2);
-      if (kB && j >= 1) zero_tail(vprev, vis.step(j - 1) * kBN + slot_u * kBlock);
+      if (kB && j >= 1) zero_tail(vprev, vis.start(j - 1) + slot_u * kBlock);
       __builtin_amdgcn_s_waitcnt(kWaitLgkmcnt0);
       asm volatile("s_barrier" ::: "memory");
       const int id = id_next;
