@@ -181,7 +181,7 @@ __global__ __launch_bounds__(kThreads, 4) void key_stats_kernel(ScoreParams p) {
   const uint16_t* kbase = p.k_pool + (size_t)g * tile_elems;
   const __attribute__((address_space(4))) int32_t* bt =
       (const __attribute__((address_space(4))) int32_t*)(p.block_tables + (size_t)ob.r * p.max_blocks_per_seq);
-  const int last_blk = (ob.len - 1) / kBlock;
+  const int last_blk = uniform((ob.len - 1) / kBlock);
   auto block_id = [&](int step) { return uniform(bt[min(step * (kStep / kBlock) + wave, last_blk)]); };
   const Staging<D> lane_at(lane);
   const int dma_off = lane_at.row * D + lane_at.elem;
@@ -246,7 +246,9 @@ __global__ __launch_bounds__(kThreads, 4) void key_stats_kernel(ScoreParams p) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) l[e] = sum[e];
   };
-  // step j: its K has landed; the loads of step j + 1 go into the other buffer, read last in step j - 1
+  // step j: its K has landed; the loads of step j + 1 go into the other buffer, read last
+  // in step j - 1 (rings of three and four buffers, with their loads further ahead, gain
+  // nothing: 198 us with two, 200 and 206 with three and four, for work-groups fewer to a CU)
   auto run_step = [&](int j, uint16_t* cur, uint16_t* next, int& id) __attribute__((always_inline)) {
     __builtin_amdgcn_s_waitcnt(kWaitVmcnt0);
     asm volatile("s_barrier" ::: "memory");
@@ -341,7 +343,7 @@ __global__ __launch_bounds__(kThreads, 4) void key_weights_kernel(ScoreParams p)
   const size_t tile_elems = (size_t)kBlock * D;
   const size_t slot_elems = (size_t)p.num_kv_heads * tile_elems;
   const int32_t* bt = p.block_tables + (size_t)ob.r * p.max_blocks_per_seq;
-  const int last_blk = (ob.len - 1) / kBlock;
+  const int last_blk = uniform((ob.len - 1) / kBlock);
   bf16x8 kreg[KS];
   {
     const int key = wkey + qi;

@@ -8,6 +8,7 @@ missing or fails to load, importing this module raises.
 """
 
 import ctypes
+import functools
 import os
 
 import torch
@@ -247,7 +248,7 @@ def _require_tensors(dev, index, *tensors):
     made for every tensor of every call they were most of a small call's
     host time."""
     for name, t, dt in tensors:
-        if t.get_device() != index or t.dtype != dt or not t.is_contiguous() or not t.is_cuda:
+        if t.get_device() != index or t.dtype is not dt or not t.is_contiguous() or not t.is_cuda:
             _require(t.device == dev and t.is_cuda, f"{name} must be on {dev}")
             _require(t.dtype == dt, f"{name} must be {dt}")
             _require(t.is_contiguous(), f"{name} must be contiguous")
@@ -646,11 +647,23 @@ def prefill_window_workspace_bytes(batch, total_q, max_q_len, max_kv_len, num_q_
                                                       num_kv_heads, head_dim, window, sinks, num_cus))
 
 
+# index of the current device, without the check that CUDA is initialised: the tensors are on it
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+
+
+@functools.lru_cache(maxsize=1024)
+def _bytes_on(index, fn, *sizes):
+    """Workspace bytes ``fn(*sizes)`` on the current device ``index``: asked of the library
+    once for each combination (1 us a call), like every size a function of its arguments."""
+    need = fn(*sizes)
+    _require(need >= 0, "no workspace size for these arguments")
+    return need
+
+
 def _workspace(workspace, need, stream, dev):
     """The workspace of a call that needs ``need`` bytes, as a tensor or None: ``workspace``
     itself, or ("auto") a new one for work on ``stream``.  On the per-thread stream, which has
     no pool of its own, it comes from the current stream's, and the caller orders the two."""
-    _require(need >= 0, "no workspace size for these arguments")
     if isinstance(workspace, str) and workspace == "auto":
         if need == 0:
             return None
@@ -675,8 +688,13 @@ def cs_prefill_window_attn(q, k_pool, v_pool, block_tables, prefix_lens, cu_q_le
                                     max_q_len, max_kv_len, scale)
     window, sinks = int(window), int(sinks)
     _require(window >= 1 and sinks >= 0, "window must be positive and sinks not negative")
-    ws = _workspace(workspace, prefill_window_workspace_bytes(args[6], args[7], args[8], args[9], args[12],
-                                                              args[13], args[14], window, sinks), stream, dev)
+    if _current_device() != dev.index:
+        with torch.cuda.device(dev):
+            return cs_prefill_window_attn(q, k_pool, v_pool, block_tables, prefix_lens, cu_q_lens, out,
+                                          max_q_len=max_q_len, max_kv_len=max_kv_len, window=window,
+                                          sinks=sinks, scale=scale, workspace=workspace, stream=stream)
+    need = _bytes_on(dev.index, prefill_window_workspace_bytes, *args[6:10], *args[12:15], window, sinks)
+    ws = _workspace(workspace, need, stream, dev)
     _check(_lib.cs_prefill_window_attn(*args, window, sinks, _ptr(ws), _nbytes(ws), outp,
                                        _stream_handle(stream, dev)))
 
@@ -726,12 +744,17 @@ def cs_decode_window_attn(q, k_pool, v_pool, block_tables, seq_lens, out, *, max
                                                                  out, max_seq_len)
     window, sinks, max_seq_len = int(window), int(sinks), int(max_seq_len)
     _require(window >= 1 and sinks >= 0, "window must be positive and sinks not negative")
-    ws = _workspace(workspace, decode_window_workspace_bytes(batch, max_seq_len, hq, hkv, d, window, sinks),
-                    stream, dev)
-    _check(_lib.cs_decode_window_attn(_ptr(q), _ptr(k_pool), _ptr(v_pool), _ptr(block_tables), _ptr(seq_lens),
-                                      batch, max_seq_len, width, num_blocks, hq, hkv, d, bs,
-                                      ctypes.c_float(scale), window, sinks, _ptr(ws), _nbytes(ws), _ptr(out),
-                                      _stream_handle(stream, dev)))
+    if _current_device() != dev.index:
+        with torch.cuda.device(dev):
+            return cs_decode_window_attn(q, k_pool, v_pool, block_tables, seq_lens, out,
+                                         max_seq_len=max_seq_len, window=window, sinks=sinks, scale=scale,
+                                         workspace=workspace, stream=stream)
+    need = _bytes_on(dev.index, decode_window_workspace_bytes, batch, max_seq_len, hq, hkv, d, window, sinks)
+    ws = _workspace(workspace, need, stream, dev)
+    _check(_lib.cs_decode_window_attn(q.data_ptr(), k_pool.data_ptr(), v_pool.data_ptr(),
+                                      block_tables.data_ptr(), seq_lens.data_ptr(), batch, max_seq_len, width,
+                                      num_blocks, hq, hkv, d, bs, scale, window, sinks, _ptr(ws), _nbytes(ws),
+                                      out.data_ptr(), _stream_handle(stream, dev)))
 
 
 _F32 = torch.float32
@@ -776,12 +799,17 @@ def cs_decode_attn_scores(q, k_pool, v_pool, block_tables, seq_lens, score_from,
     _require(score_from.numel() == batch, "score_from must have B entries")
     _require_scores(score_pool, k_pool, dev)
     max_seq_len, max_scored_len = int(max_seq_len), int(max_scored_len)
-    ws = _workspace(workspace, decode_scores_workspace_bytes(batch, max_seq_len, max_scored_len, hq, hkv, d),
-                    stream, dev)
-    _check(_lib.cs_decode_attn_scores(_ptr(q), _ptr(k_pool), _ptr(v_pool), _ptr(block_tables), _ptr(seq_lens),
-                                      _ptr(score_from), batch, max_seq_len, max_scored_len, width, num_blocks,
-                                      hq, hkv, d, bs, ctypes.c_float(scale), ctypes.c_float(decay),
-                                      _ptr(score_pool), _ptr(ws), _nbytes(ws), _ptr(out),
+    if _current_device() != dev.index:
+        with torch.cuda.device(dev):
+            return cs_decode_attn_scores(q, k_pool, v_pool, block_tables, seq_lens, score_from, score_pool, out,
+                                         max_seq_len=max_seq_len, max_scored_len=max_scored_len, scale=scale,
+                                         decay=decay, workspace=workspace, stream=stream)
+    need = _bytes_on(dev.index, decode_scores_workspace_bytes, batch, max_seq_len, max_scored_len, hq, hkv, d)
+    ws = _workspace(workspace, need, stream, dev)
+    _check(_lib.cs_decode_attn_scores(q.data_ptr(), k_pool.data_ptr(), v_pool.data_ptr(),
+                                      block_tables.data_ptr(), seq_lens.data_ptr(), score_from.data_ptr(), batch,
+                                      max_seq_len, max_scored_len, width, num_blocks, hq, hkv, d, bs, scale,
+                                      decay, score_pool.data_ptr(), _ptr(ws), _nbytes(ws), out.data_ptr(),
                                       _stream_handle(stream, dev)))
 
 
@@ -827,13 +855,18 @@ def cs_prefill_key_scores(q, k_pool, block_tables, prefix_lens, cu_q_lens, score
              "prefix_lens and score_from must have B entries and cu_q_lens B + 1")
     _require_scores(score_pool, k_pool, dev)
     max_q_len, max_kv_len, rows = int(max_q_len), int(max_kv_len), int(rows)
-    ws = _workspace(workspace, prefill_scores_workspace_bytes(batch, total_q, max_q_len, max_kv_len, rows, hq,
-                                                              hkv), stream, dev)
-    _check(_lib.cs_prefill_key_scores(_ptr(q), _ptr(k_pool), _ptr(block_tables), _ptr(prefix_lens),
-                                      _ptr(cu_q_lens), _ptr(score_from), batch, total_q, max_q_len,
-                                      max_kv_len, block_tables.shape[1], num_blocks, hq, hkv, d, bs,
-                                      ctypes.c_float(scale), rows, ctypes.c_float(decay), _ptr(score_pool),
-                                      _ptr(ws), _nbytes(ws), _stream_handle(stream, dev)))
+    if _current_device() != dev.index:
+        with torch.cuda.device(dev):
+            return cs_prefill_key_scores(q, k_pool, block_tables, prefix_lens, cu_q_lens, score_from, score_pool,
+                                         max_q_len=max_q_len, max_kv_len=max_kv_len, rows=rows, scale=scale,
+                                         decay=decay, workspace=workspace, stream=stream)
+    need = _bytes_on(dev.index, prefill_scores_workspace_bytes, batch, total_q, max_q_len, max_kv_len, rows, hq, hkv)
+    ws = _workspace(workspace, need, stream, dev)
+    _check(_lib.cs_prefill_key_scores(q.data_ptr(), k_pool.data_ptr(), block_tables.data_ptr(),
+                                      prefix_lens.data_ptr(), cu_q_lens.data_ptr(), score_from.data_ptr(), batch,
+                                      total_q, max_q_len, max_kv_len, block_tables.shape[1], num_blocks, hq, hkv,
+                                      d, bs, scale, rows, decay, score_pool.data_ptr(), _ptr(ws), _nbytes(ws),
+                                      _stream_handle(stream, dev)))
 
 
 def cs_kv_evict_raw(score_pool, k_pool, v_pool, block_tables, dst_block_tables, seq_lens, keep_from, batch,
@@ -855,12 +888,11 @@ def cs_kv_evict(score_pool, k_pool, v_pool, block_tables, dst_block_tables, seq_
     positions.  ``kept`` int32 ``[B, Hkv, budget]`` gets the kept keys (a first entry of -1:
     nothing was evicted), ``new_lens`` int32 ``[B]`` the new lengths (it may be ``seq_lens``)."""
     dev = k_pool.device
-    tensors = [("k_pool", k_pool, _BF16), ("v_pool", v_pool, _BF16), ("block_tables", block_tables, _I32),
-               ("seq_lens", seq_lens, _I32), ("keep_from", keep_from, _I32), ("kept", kept, _I32),
-               ("new_lens", new_lens, _I32)]
+    _require_tensors(dev, k_pool.get_device(), ("k_pool", k_pool, _BF16), ("v_pool", v_pool, _BF16),
+                     ("block_tables", block_tables, _I32), ("seq_lens", seq_lens, _I32),
+                     ("keep_from", keep_from, _I32), ("kept", kept, _I32), ("new_lens", new_lens, _I32))
     if dst_block_tables is not None:
-        tensors.append(("dst_block_tables", dst_block_tables, _I32))
-    _require_tensors(dev, k_pool.get_device(), *tensors)
+        _require_tensors(dev, k_pool.get_device(), ("dst_block_tables", dst_block_tables, _I32))
     _require(k_pool.shape == v_pool.shape and k_pool.dim() == 4, "pools must match")
     _require_scores(score_pool, k_pool, dev)
     _require(block_tables.dim() == 2, "block_tables must be [B, max_blocks]")
@@ -871,10 +903,15 @@ def cs_kv_evict(score_pool, k_pool, v_pool, block_tables, dst_block_tables, seq_
     _require(seq_lens.numel() == batch and keep_from.numel() == batch and new_lens.numel() == batch,
              "seq_lens, keep_from and new_lens must have B entries")
     _require(tuple(kept.shape) == (batch, hkv, budget), "kept must be [B, Hkv, budget]")
-    _check(_lib.cs_kv_evict(_ptr(score_pool), _ptr(k_pool), _ptr(v_pool), _ptr(block_tables),
-                            _ptr(dst_block_tables), _ptr(seq_lens), _ptr(keep_from), batch,
+    if _current_device() != dev.index:
+        with torch.cuda.device(dev):
+            return cs_kv_evict(score_pool, k_pool, v_pool, block_tables, dst_block_tables, seq_lens, keep_from,
+                               kept, new_lens, max_seq_len=max_seq_len, budget=budget, trigger=trigger,
+                               recent=recent, stream=stream)
+    _check(_lib.cs_kv_evict(score_pool.data_ptr(), k_pool.data_ptr(), v_pool.data_ptr(), block_tables.data_ptr(),
+                            _ptr(dst_block_tables), seq_lens.data_ptr(), keep_from.data_ptr(), batch,
                             int(max_seq_len), block_tables.shape[1], num_blocks, hkv, d, bs, budget,
-                            int(trigger), int(recent), _ptr(kept), _ptr(new_lens),
+                            int(trigger), int(recent), kept.data_ptr(), new_lens.data_ptr(),
                             _stream_handle(stream, dev)))
 
 
