@@ -669,9 +669,17 @@ def _workspace(workspace, need, stream, dev):
             return None
         ws = _scratch(need, stream, dev)
         return _scratch(need, None, dev) if ws is None else ws
+    _require(isinstance(workspace, torch.Tensor), 'workspace must be "auto" or a tensor')
     _require(workspace.is_cuda and workspace.device == dev, f"workspace must be on {dev}")
     _require(workspace.is_contiguous(), "workspace must be contiguous")
     return workspace
+
+
+def _window(window, sinks, max_len):
+    """A window and its sinks as the C calls take them: one of at least ``max_len`` keys, however
+    large, hides nothing."""
+    _require(window >= 1 and sinks >= 0, "window must be positive and sinks not negative")
+    return int(min(window, max(max_len, 1))), int(min(sinks, max(max_len, 0)))
 
 
 def _nbytes(ws):
@@ -686,8 +694,7 @@ def cs_prefill_window_attn(q, k_pool, v_pool, block_tables, prefix_lens, cu_q_le
     one) or a uint8 GPU tensor of :func:`prefill_window_workspace_bytes`."""
     args, outp, dev = _prefill_args(q, k_pool, v_pool, block_tables, prefix_lens, cu_q_lens, out,
                                     max_q_len, max_kv_len, scale)
-    window, sinks = int(window), int(sinks)
-    _require(window >= 1 and sinks >= 0, "window must be positive and sinks not negative")
+    window, sinks = _window(window, sinks, args[9])
     if _current_device() != dev.index:
         with torch.cuda.device(dev):
             return cs_prefill_window_attn(q, k_pool, v_pool, block_tables, prefix_lens, cu_q_lens, out,
@@ -742,8 +749,8 @@ def cs_decode_window_attn(q, k_pool, v_pool, block_tables, seq_lens, out, *, max
     (allocated here) or a uint8 GPU tensor of :func:`decode_window_workspace_bytes`."""
     batch, hq, hkv, d, num_blocks, bs, width, dev = _decode_args(q, k_pool, v_pool, block_tables, seq_lens,
                                                                  out, max_seq_len)
-    window, sinks, max_seq_len = int(window), int(sinks), int(max_seq_len)
-    _require(window >= 1 and sinks >= 0, "window must be positive and sinks not negative")
+    max_seq_len = int(max_seq_len)
+    window, sinks = _window(window, sinks, max_seq_len)
     if _current_device() != dev.index:
         with torch.cuda.device(dev):
             return cs_decode_window_attn(q, k_pool, v_pool, block_tables, seq_lens, out,
@@ -854,7 +861,8 @@ def cs_prefill_key_scores(q, k_pool, block_tables, prefix_lens, cu_q_lens, score
     _require(prefix_lens.numel() == batch and cu_q_lens.numel() == batch + 1 and score_from.numel() == batch,
              "prefix_lens and score_from must have B entries and cu_q_lens B + 1")
     _require_scores(score_pool, k_pool, dev)
-    max_q_len, max_kv_len, rows = int(max_q_len), int(max_kv_len), int(rows)
+    max_q_len, max_kv_len = int(max_q_len), int(max_kv_len)
+    rows = int(min(rows, max(max_q_len, 1)))
     if _current_device() != dev.index:
         with torch.cuda.device(dev):
             return cs_prefill_key_scores(q, k_pool, block_tables, prefix_lens, cu_q_lens, score_from, score_pool,
@@ -911,7 +919,7 @@ def cs_kv_evict(score_pool, k_pool, v_pool, block_tables, dst_block_tables, seq_
     _check(_lib.cs_kv_evict(score_pool.data_ptr(), k_pool.data_ptr(), v_pool.data_ptr(), block_tables.data_ptr(),
                             _ptr(dst_block_tables), seq_lens.data_ptr(), keep_from.data_ptr(), batch,
                             int(max_seq_len), block_tables.shape[1], num_blocks, hkv, d, bs, budget,
-                            int(trigger), int(recent), kept.data_ptr(), new_lens.data_ptr(),
+                            int(min(trigger, 2 ** 31 - 1)), int(recent), kept.data_ptr(), new_lens.data_ptr(),
                             _stream_handle(stream, dev)))
 
 
