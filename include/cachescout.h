@@ -537,11 +537,12 @@ int cs_decode_attn_scores(const void *q, const void *k_pool, const void *v_pool,
                           int32_t block_size, float scale, float decay, float *score_pool,
                           void *workspace, int64_t workspace_bytes, void *out, cs_stream_t stream);
 
-/* Workspace bytes cs_decode_attn_scores needs: those of
- * cs_paged_decode_attn_ws, and 128 * batch * num_q_heads *
- * floor((max_scored_len + 62) / 32) (0 for max_scored_len 0).  num_cus as there;
- * -1 for a negative size, bad head counts, a head_dim other than 64 or 128, or
- * max_scored_len above max_seq_len. */
+/* Workspace bytes cs_decode_attn_scores needs: 128 * batch * num_q_heads *
+ * floor((max_scored_len + 62) / 32) (0 for max_scored_len 0), and those of
+ * cs_paged_decode_attn_ws unless it takes one work-group per sequence and KV head
+ * (at least as many as compute units, and max_scored_len at least three quarters
+ * of max_seq_len).  num_cus as there; -1 for a negative size, bad head counts, a
+ * head_dim other than 64 or 128, or max_scored_len above max_seq_len. */
 int64_t cs_decode_scores_workspace_bytes(int32_t batch, int32_t max_seq_len, int32_t max_scored_len,
                                          int32_t num_q_heads, int32_t num_kv_heads,
                                          int32_t head_dim, int32_t num_cus);

@@ -363,6 +363,19 @@ int64_t scored_units(int32_t max_scored_len) {
   return max_scored_len > 0 ? ((int64_t)max_scored_len + 62) / 32 : 0;
 }
 
+// The launch of a decode that adds scores: ranges as any other's, or none, i.e. one
+// work-group per (sequence, KV head), which keeps the logits on the CU.  The latter from one
+// pair per compute unit on, unless more than a quarter of the keys may be a shared prefix
+// (which ranges read once).  us a call in ranges and by pairs, 32 / 8 heads of 128: 32 sequences
+// of 3000-9000 keys 174 and 172, 48 254 and 231, 64 347 and 295, 128 of 4200-10000 748 and 612,
+// 160 of 300-900 98 and 96; of 64 128 of 3000-6000 287 and 256; 8 / 1 heads, 160 (0.6 pairs a
+// CU) of 500-5000 52 and 73.
+cs::DecodeGeometry scored_geometry(int32_t batch, int32_t max_seq_len, int32_t max_scored_len, int32_t num_kv_heads,
+                                   int32_t head_dim, int cus) {
+  if ((long long)batch * num_kv_heads >= cus && 4LL * max_scored_len >= 3LL * max_seq_len) return {};
+  return cs::decode_geometry(batch, max_seq_len, num_kv_heads, head_dim, cus);
+}
+
 // Workspace bytes of the kept logits
 int64_t logit_bytes(int32_t batch, int32_t max_scored_len, int32_t num_q_heads) {
   return (int64_t)batch * num_q_heads * scored_units(max_scored_len) * 32 * (int64_t)sizeof(float);
@@ -389,7 +402,9 @@ int paged_decode(const void* q, const void* k_pool, const void* v_pool,
     int cus = 0;
     hipError_t ecu = cs::current_device_cus(&cus);
     if (ecu != hipSuccess) return hip_fail(ecu, "compute-unit count of the current device");
-    geo = cs::decode_geometry(batch, extra.win.visible(max_seq_len, 1, 32), num_kv_heads, head_dim, cus);
+    geo = extra.score_pool ? scored_geometry(batch, max_seq_len, extra.max_scored_len, num_kv_heads, head_dim, cus)
+                           : cs::decode_geometry(batch, extra.win.visible(max_seq_len, 1, 32), num_kv_heads, head_dim,
+                                                 cus);
     const int64_t need = logits + decode_range_bytes(geo, num_q_heads, head_dim);
     if (need > 0) {
       if (!workspace || !aligned16(workspace))
@@ -826,10 +841,15 @@ int cs_decode_attn_scores(const void* q, const void* k_pool, const void* v_pool,
 int64_t cs_decode_scores_workspace_bytes(int32_t batch, int32_t max_seq_len, int32_t max_scored_len,
                                          int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim,
                                          int32_t num_cus) {
-  if (max_scored_len < 0 || max_scored_len > max_seq_len) return -1;
-  const int64_t ranges = cs_paged_decode_workspace_bytes(batch, max_seq_len, num_q_heads, num_kv_heads, head_dim,
-                                                         num_cus);
-  return ranges < 0 ? -1 : ranges + logit_bytes(batch, max_scored_len, num_q_heads);
+  if (batch < 0 || max_scored_len < 0 || max_scored_len > max_seq_len || num_cus < 0 || num_q_heads <= 0 ||
+      num_kv_heads <= 0 || num_q_heads % num_kv_heads != 0 || (head_dim != 64 && head_dim != 128))
+    return -1;
+  if (batch == 0) return 0;
+  int cus = num_cus;
+  if (cus == 0 && cs::current_device_cus(&cus) != hipSuccess) return -1;
+  return decode_range_bytes(scored_geometry(batch, max_seq_len, max_scored_len, num_kv_heads, head_dim, cus),
+                            num_q_heads, head_dim) +
+         logit_bytes(batch, max_scored_len, num_q_heads);
 }
 
 int cs_prefill_key_scores(const void* q, const void* k_pool, const int32_t* block_tables,

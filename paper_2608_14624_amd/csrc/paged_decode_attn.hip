@@ -100,6 +100,7 @@ struct DecParams {
   float decay;
   float* logits;
   int logit_units;
+  int lds_units;                // of these, the ones that decode_scores_pair_kernel keeps in LDS
 };
 
 // The units of a sequence of len keys that its query sees, as a list: under a window
@@ -167,31 +168,37 @@ __device__ __forceinline__ void keep_logits(const DecParams& p, float* unit_logi
     *reinterpret_cast<f32x4*>(unit_logits + 4 * ((4 * mt + (lane >> 4)) * p.group + (lane & 15))) = s[mt];
 }
 
-// units whose logits a wave of decode_ranges_kernel stages in LDS before it stores them
+// Units whose logits a wave of decode_ranges_kernel stages in LDS before it stores them:
+// 128 sequences of 4.2k-10k keys 806 us without, 751 with 4 units, 747 with 8, 743 with 16.
 constexpr int kStagedUnits = 8;
 
-// The weights of the four keys key .. key + 3, of the group's heads together, into their
-// scores.  stat: m c and 1 / l of every head.
-__device__ __forceinline__ void add_scores(const DecParams& p, const float2* stat, int r, int g, int key, int len, int from,
-                                           int id) {
-  const float* at = logits_at(p, r, g, key / kUnitKeys, from / kUnitKeys) + 4 * (key / 4 % 8) * p.group;
+// The weights of four keys, of the group's heads together, from their logits ([group][4]).
+// stat: m c and 1 / l of every head.
+__device__ __forceinline__ f32x4 quad_weights(const DecParams& p, const float2* stat, const float* logits) {
   f32x4 w = f32x4{};
   for (int j = 0; j < p.group; ++j) {
-    const f32x4 x = *reinterpret_cast<const f32x4*>(at + 4 * j);
+    const f32x4 x = *reinterpret_cast<const f32x4*>(logits + 4 * j);
     const float2 st = stat[j];
 #pragma unroll
     for (int e = 0; e < 4; ++e)
       w[e] = __builtin_fmaf(__builtin_amdgcn_exp2f(__builtin_fmaf(x[e], p.scale_log2, -st.x)), st.y, w[e]);
   }
-  float* score = p.score_pool + ((size_t)id * p.num_kv_heads + g) * kBlock + key % kBlock;
-  const f32x4 old = *reinterpret_cast<const f32x4*>(score);
+  return w;
+}
+
+// The scores of the keys key .. key + 3 with the weights added; those not scored as they
+// were.  The query's own key is new in this step: what its slot held is another key's.
+__device__ __forceinline__ f32x4 quad_scores(const DecParams& p, f32x4 old, f32x4 w, int key, int from, int len) {
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
-    // the query's own key is new in this step: what its slot held is another key's
     const float kept = key + e == len - 1 ? 0.f : p.decay * old[e];
     w[e] = key + e >= from && key + e < len ? kept + w[e] : old[e];
   }
-  *reinterpret_cast<f32x4*>(score) = w;
+  return w;
+}
+
+__device__ __forceinline__ float* score_at(const DecParams& p, int id, int g, int key) {
+  return p.score_pool + ((size_t)id * p.num_kv_heads + g) * kBlock + key % kBlock;
 }
 
 // first key of sequence r that its group does not share
@@ -382,10 +389,6 @@ __global__ __launch_bounds__(64 * (kKeys == Keys::kCascade ? kCascadeWaves : kDe
         s[mt][rr] = (key < end && key >= start && seen.key(key)) ? s[mt][rr] : -INFINITY;
         mloc = fmaxf(mloc, s[mt][rr]);
       }
-    if constexpr (kKeys == Keys::kScored) {
-      float* keep = logits_at(p, r, g, ch, max(0, p.score_from[r]) / kUnitKeys);
-      if (keep != nullptr && head_valid) keep_logits(p, keep, lane, s);
-    }
     mloc = fmaxf(mloc, __shfl_xor(mloc, 16));
     mloc = fmaxf(mloc, __shfl_xor(mloc, 32));
     const float m_new = fmaxf(m_run, mloc);
@@ -402,8 +405,7 @@ __global__ __launch_bounds__(64 * (kKeys == Keys::kCascade ? kCascadeWaves : kDe
       for (int rr = 0; rr < 4; ++rr) {
         const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s[mt][rr], c, -mc));
         pb[4 * mt + rr] = (__bf16)e;
-        // (scores are sums of fp32 weights, which are normalised by a sum of such)
-        l_run += kKeys == Keys::kScored ? e : (float)pb[4 * mt + rr];
+        l_run += (float)pb[4 * mt + rr];
       }
     // O^T += V^T P^T
 #pragma unroll
@@ -453,23 +455,6 @@ __global__ __launch_bounds__(64 * (kKeys == Keys::kCascade ? kCascadeWaves : kDe
       // a row of an empty sequence (a padded batch) is zero
       p.out[row * D + d] = __builtin_bit_cast(uint16_t, (__bf16)(L > 0 ? num / den : 0.f));
     }
-  }
-  if constexpr (kKeys == Keys::kScored) {
-    __shared__ float2 stat[kMaxGroup];
-    if ((int)threadIdx.x < p.group) {
-      const int hj = threadIdx.x;
-      float mx = -INFINITY, den = 0.f;
-      for (int w = 0; w < kWaves; ++w) mx = fmaxf(mx, sm.merge.m[w][hj]);
-      for (int w = 0; w < kWaves; ++w) den += __builtin_amdgcn_exp2f((sm.merge.m[w][hj] - mx) * c) * sm.merge.l[w][hj];
-      stat[hj] = make_float2(mx * c, 1.f / den);
-    }
-    __syncthreads();
-    // the logits that the work-group's waves kept (at most logit_units of them)
-    const int from = max(0, p.score_from[r]);
-    const int first = from / 4 * 4;
-    const int last = (int)min((long long)L, (long long)(from / kUnitKeys + p.logit_units) * kUnitKeys);
-    for (int key = first + 4 * threadIdx.x; key < last; key += 4 * kWGThreads)
-      add_scores(p, stat, r, g, key, L, from, bt[key / kBlock]);
   }
 }
 
@@ -849,7 +834,8 @@ __global__ __launch_bounds__(64) void decode_ranges_kernel(DecParams p) {
         for (int dc = 0; dc < DC; ++dc)
           s[mt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kreg[mt][dc], qreg[dc], s[mt], 0, 0, 0);
       // Staged logits go out ahead of the next unit's loads: these are waited for in order,
-      // so behind them the stores' way to memory would be waited for on top of theirs.
+      // so behind them the stores' way to memory would be waited for on top of theirs (747
+      // us behind, 741 ahead).
       if constexpr (kScored) {
         if (n_staged == kStagedUnits || (n_staged > 0 && piece_begins)) store_staged();
       }
@@ -1037,7 +1023,204 @@ __global__ __launch_bounds__(kMergeThreads) void decode_scores_kernel(DecParams 
   __syncthreads();
   const int key = first + 4 * threadIdx.x;
   if (key + 3 < from || key >= len || (key - from / kUnitKeys * kUnitKeys) / kUnitKeys >= p.logit_units) return;
-  add_scores(p, stat, r, g, key, len, from, p.block_tables[(size_t)r * p.max_blocks_per_seq + key / kBlock]);
+  f32x4* score = reinterpret_cast<f32x4*>(
+      score_at(p, p.block_tables[(size_t)r * p.max_blocks_per_seq + key / kBlock], g, key));
+  const f32x4 old = *score;
+  const float* logits = logits_at(p, r, g, key / kUnitKeys, from / kUnitKeys) + 4 * (key / 4 % 8) * p.group;
+  *score = quad_scores(p, old, quad_weights(p, stat, logits), key, from, len);
+}
+
+// Decode with scores, one work-group of four waves per (sequence, KV head): the waves take
+// the sequence's units in turn and keep the logits of its scored keys in LDS (those past
+// p.lds_units units in the workspace), so that its weights need no memory but the scores.
+// Ranges have to write all logits, since a sequence's softmax is known only when all of
+// its pieces are done, and the writes cost the stream of reads far more than their bytes:
+// 128 sequences of 4.2k-10k keys, 32 / 8 heads of 128, 3.3 GB of K and V and 100 MB of logits,
+// 748 us in ranges, 612 here (5.5 TB/s; five, six and eight waves 617, 625 and 638: what is
+// read ahead is enough, and the V tiles of more waves leave the logits less room).
+constexpr int kScoreWaves = 4;
+constexpr int kScoreThreads = 64 * kScoreWaves;
+constexpr int kScoreBatch = 256;        // longest sequence first up to this many
+constexpr int kScoreQuads = 8;          // quads of keys per thread whose scores are loaded together
+template <int D>
+__global__ __launch_bounds__(kScoreThreads) void decode_scores_pair_kernel(DecParams p) {
+  constexpr int DC = D / 32;
+  constexpr int DT = D / 16;
+  constexpr int kVLoads = kChunk * D / 8 / 64;
+  __shared__ DecLds<D, kScoreWaves> sm;
+  __shared__ float2 stat[kMaxGroup];
+  __shared__ int lens[kScoreBatch];
+  __shared__ int pick;
+  extern __shared__ __attribute__((aligned(16))) float kept_logits[];     // [lds_units][8][group][4]
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int j = lane & 15;
+  const int qd = lane >> 4;
+  const int g = blockIdx.x % p.num_kv_heads;
+  int r = blockIdx.x / p.num_kv_heads;
+  if (p.batch <= kScoreBatch) {
+    // (the order of paged_decode_attn_kernel)
+    for (int s = threadIdx.x; s < p.batch; s += kScoreThreads) lens[s] = p.seq_lens[s];
+    __syncthreads();
+    for (int s = threadIdx.x; s < p.batch; s += kScoreThreads) {
+      const int mine = lens[s];
+      int rank = 0;
+      for (int t = 0; t < p.batch; ++t) rank += (lens[t] > mine) || (lens[t] == mine && t < s);
+      if (rank == r) pick = s;
+    }
+    __syncthreads();
+    r = pick;
+  }
+  r = __builtin_amdgcn_readfirstlane(r);
+  const ScalarInts bt = (ScalarInts)(p.block_tables + (size_t)r * p.max_blocks_per_seq);
+  const int len = __builtin_amdgcn_readfirstlane(p.seq_lens[r]);
+  const int from = __builtin_amdgcn_readfirstlane(max(0, p.score_from[r]));
+  const int from_unit = from / kUnitKeys;
+  const int units = units_of(len);
+  const size_t tile_elems = (size_t)kBlock * D;
+  const size_t slot_elems = (size_t)p.num_kv_heads * tile_elems;
+  const uint16_t* kbase = p.k_pool + (size_t)g * tile_elems;
+  const uint16_t* vbase = p.v_pool + (size_t)g * tile_elems;
+  const bool head_valid = j < p.group;
+  const int h = g * p.group + (head_valid ? j : 0);
+  const float c = p.scale_log2;
+  const float lowest = -FLT_MAX / fmaxf(c, 1.f);      // as in decode_ranges_kernel
+  bf16x8 qreg[DC];
+#pragma unroll
+  for (int dc = 0; dc < DC; ++dc) {
+    qreg[dc] = bf16x8{};
+    if (head_valid)
+      qreg[dc] = *reinterpret_cast<const bf16x8*>(p.q + ((size_t)r * p.num_q_heads + h) * D + 32 * dc + 8 * qd);
+  }
+  f32x4 oacc[DT];
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt) oacc[dt] = f32x4{};
+  float m_run = -INFINITY, l_run = 0.f;
+  const int last_blk = (len - 1) / kBlock;
+  int id0 = 0, id1 = 0;
+  auto ids_of = [&](int x) {
+    id0 = bt[min(x * kUnitBlocks, last_blk)];
+    id1 = bt[min(x * kUnitBlocks + 1, last_blk)];
+  };
+  bf16x8 kreg[2][DC];
+  bf16x8 vreg[kVLoads];
+  uint16_t* tile = sm.v[wave];
+  if (wave < units) {
+    ids_of(wave);
+    load_chunk_tiles<D, kNonTemporal>(kbase, vbase, id0, id1, slot_elems, lane, kreg, vreg);
+    ids_of(wave + kScoreWaves);
+  }
+  for (int x = wave; x < units; x += kScoreWaves) {
+    const int key0 = x * kUnitKeys;
+    store_v_tile<D>(vreg, lane, key0, len, tile);
+    f32x4 s[2] = {f32x4{}, f32x4{}};
+#pragma unroll
+    for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+      for (int dc = 0; dc < DC; ++dc)
+        s[mt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kreg[mt][dc], qreg[dc], s[mt], 0, 0, 0);
+    if (x + kScoreWaves < units) {
+      load_chunk_tiles<D, kNonTemporal>(kbase, vbase, id0, id1, slot_elems, lane, kreg, vreg);
+      ids_of(x + 2 * kScoreWaves);
+    }
+    float mloc = -INFINITY;
+#pragma unroll
+    for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+      for (int rr = 0; rr < 4; ++rr) {
+        const int key = key0 + 16 * mt + 4 * qd + rr;
+        s[mt][rr] = key < len ? s[mt][rr] : -INFINITY;
+        mloc = fmaxf(mloc, s[mt][rr]);
+      }
+    const int u = x - from_unit;
+    if (u >= 0 && u < p.lds_units) {
+      if (head_valid) keep_logits(p, kept_logits + u * kUnitKeys * p.group, lane, s);
+    } else if (float* keep = logits_at(p, r, g, x, from_unit); keep != nullptr && head_valid) {
+      keep_logits(p, keep, lane, s);
+    }
+    const float m_unit = fmaxf(quad_max(mloc), lowest);
+    const float m_new = fmaxf(m_run, m_unit);
+    const float alpha = __builtin_amdgcn_exp2f((m_run - m_new) * c);
+    const float beta = __builtin_amdgcn_exp2f((m_unit - m_new) * c);
+    m_run = m_new;
+    const float mc = m_unit * c;
+    bf16x8 pb;
+    float l_unit = 0.f;
+#pragma unroll
+    for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+      for (int rr = 0; rr < 4; ++rr) {
+        const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s[mt][rr], c, -mc));
+        pb[4 * mt + rr] = (__bf16)e;
+        l_unit += e;
+      }
+    l_run = __builtin_fmaf(l_run, alpha, l_unit * beta);
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) {
+      const f32x4 o = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v_fragment<D>(tile, lane, dt), pb, f32x4{}, 0, 0, 0);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) oacc[dt][e] = __builtin_fmaf(oacc[dt][e], alpha, o[e] * beta);
+    }
+  }
+
+  // the scores of the first quads, in flight during the merge
+  const int first = from / 4 * 4;
+  const int last = (int)min((long long)len, (long long)(from_unit + p.logit_units) * kUnitKeys);
+  f32x4* at[kScoreQuads];
+  f32x4 old[kScoreQuads];
+  auto load_scores = [&](int key0) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < kScoreQuads; ++i) {
+      const int key = key0 + 4 * ((int)threadIdx.x + i * kScoreThreads);
+      at[i] = reinterpret_cast<f32x4*>(score_at(p, p.block_tables[(size_t)r * p.max_blocks_per_seq + min(key, last - 1) / kBlock],
+                                                g, key));
+    }
+#pragma unroll
+    for (int i = 0; i < kScoreQuads; ++i) old[i] = *at[i];
+  };
+  if (first < last) load_scores(first);
+  l_run = quad_sum(l_run);
+  __syncthreads();                     // every wave is done with its V tile
+  if (qd == 0) {
+    sm.merge.m[wave][j] = m_run;
+    sm.merge.l[wave][j] = l_run;
+  }
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+    for (int rr = 0; rr < 4; ++rr) sm.merge.o[wave][j][16 * dt + 4 * qd + rr] = oacc[dt][rr];
+  __syncthreads();
+  for (int idx = threadIdx.x; idx < p.group * D; idx += kScoreThreads) {
+    const int hj = idx / D;
+    const int d = idx % D;
+    float mx = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < kScoreWaves; ++w) mx = fmaxf(mx, sm.merge.m[w][hj]);
+    float num = 0.f, den = 0.f;
+#pragma unroll
+    for (int w = 0; w < kScoreWaves; ++w) {
+      const float wt = __builtin_amdgcn_exp2f((sm.merge.m[w][hj] - mx) * c);   // 0 for idle waves
+      num += wt * sm.merge.o[w][hj][d];
+      den += wt * sm.merge.l[w][hj];
+    }
+    // a row of an empty sequence (a padded batch) is zero
+    p.out[((size_t)r * p.num_q_heads + g * p.group + hj) * D + d] =
+        __builtin_bit_cast(uint16_t, (__bf16)(len > 0 ? num / den : 0.f));
+    if (d == 0) stat[hj] = make_float2(mx * c, 1.f / den);
+  }
+  __syncthreads();
+  for (int key0 = first; key0 < last; key0 += 4 * kScoreQuads * kScoreThreads) {
+    if (key0 != first) load_scores(key0);
+#pragma unroll
+    for (int i = 0; i < kScoreQuads; ++i) {
+      const int key = key0 + 4 * ((int)threadIdx.x + i * kScoreThreads);
+      if (key >= last) break;
+      const int u = key / kUnitKeys - from_unit;
+      const float* logits = u < p.lds_units ? kept_logits + u * kUnitKeys * p.group
+                                            : logits_at(p, r, g, key / kUnitKeys, from_unit);
+      *at[i] = quad_scores(p, old[i], quad_weights(p, stat, logits + 4 * (key / 4 % 8) * p.group), key, from, len);
+    }
+  }
 }
 
 // One work-group per (sequence, KV head): the final output of cascade decode
@@ -1127,10 +1310,26 @@ DecodeGeometry decode_geometry(int batch, int max_seq_len, int num_kv_heads, int
 
 namespace {
 
+// LDS of a compute unit, and of decode_scores_pair_kernel without the logits
+constexpr int kLdsBytes = 160 * 1024;
+constexpr int pair_lds_bytes(int head_dim) {
+  return (head_dim == 128 ? (int)sizeof(DecLds<128, kScoreWaves>) : (int)sizeof(DecLds<64, kScoreWaves>)) +
+         kMaxGroup * (int)sizeof(float2) + kScoreBatch * (int)sizeof(int) + 256;
+}
+
 template <int D, Keys kKeys>
 void launch_decode(const DecodeLaunch& a, const DecParams& p, hipStream_t stream) {
   const unsigned rows = (unsigned)((long long)a.batch * a.num_kv_heads);
-  if (a.ranges == 0) {
+  if constexpr (kKeys == Keys::kScored) {
+    if (a.ranges == 0) {
+      DecParams pair = p;
+      const int unit_bytes = kUnitKeys * p.group * (int)sizeof(float);
+      pair.lds_units = std::min(a.logit_units, (kLdsBytes - pair_lds_bytes(D)) / unit_bytes);
+      hipLaunchKernelGGL(decode_scores_pair_kernel<D>, dim3(rows), dim3(kScoreThreads),
+                         (size_t)pair.lds_units * unit_bytes, stream, pair);
+      return;
+    }
+  } else if (a.ranges == 0) {
     hipLaunchKernelGGL((paged_decode_attn_kernel<D, kKeys>), dim3(rows), dim3(64 * kDecodeWaves), 0, stream, p);
     return;
   }

@@ -105,6 +105,11 @@ def test_scores_workspace_holds_the_logits_of_the_scored_units():
         units = max((start + n - 1) // 32 - start // 32 + 1 for start in range(32))
         assert ops.decode_scores_workspace_bytes(3, 6000, n, 32, 8, 128, cu) == ranges + 3 * 32 * units * 32 * 4
     assert ops.decode_scores_workspace_bytes(3, 6000, 0, 32, 8, 128, cu) == ranges
+    # from one (sequence, KV head) per compute unit on, the logits alone, unless much may be shared
+    many = ops.paged_decode_workspace_bytes(32, 6000, 32, 8, 128, cu)
+    assert ops.decode_scores_workspace_bytes(32, 6000, 4500, 32, 8, 128, cu) == 32 * 32 * 142 * 32 * 4
+    assert ops.decode_scores_workspace_bytes(32, 6000, 4499, 32, 8, 128, cu) == 32 * 32 * 142 * 32 * 4 + many
+    assert ops.decode_scores_workspace_bytes(31, 6000, 4500, 32, 8, 128, cu) > 31 * 32 * 142 * 32 * 4
     assert ops.decode_scores_workspace_bytes(3, 6000, 6001, 32, 8, 128, cu) < 0
     assert ops.decode_scores_workspace_bytes(3, 100, -1, 32, 8, 128, cu) < 0
     assert ops.decode_scores_workspace_bytes(3, 100, 10, 32, 5, 128, cu) < 0

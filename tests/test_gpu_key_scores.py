@@ -100,6 +100,25 @@ def test_decode_full_batch_on_a_shared_anchor():
     check_decode(36, 32, 8, 128, lens, [960] * 64, shared=60, rows=[0, 1, 40, 63], decay=0.97)
 
 
+@pytest.mark.parametrize("hq,hkv,d,batch", [(32, 8, 128, 41), (32, 8, 64, 33), (40, 8, 128, 32), (16, 16, 64, 20)])
+def test_decode_a_work_group_per_pair(hq, hkv, d, batch):
+    """At least as many sequences and KV heads as compute units."""
+    lens = [(397 * i) % 1300 for i in range(batch)]
+    check_decode(46, hq, hkv, d, lens, [(5 * i) % 200 for i in range(batch)], decay=0.7, rows=[0, 1, 2, batch // 2, batch - 1])
+
+
+def test_decode_more_logits_than_a_compute_unit_holds():
+    """16 query heads per KV head: past about 1900 scored keys their logits go to the workspace."""
+    lens = [4000, 2500, 1800, 0] + [60] * 29
+    check_decode(47, 128, 8, 128, lens, [33, 0, 5, 0] + [0] * 29, rows=[0, 1, 2, 32])
+
+
+def test_decode_batch_in_its_own_order():
+    """More sequences than are ordered by length, one work-group per sequence and KV head."""
+    lens = [(61 * i) % 250 + 1 for i in range(300)]
+    check_decode(48, 8, 1, 64, lens, [0] * 300, rows=[0, 7, 299])
+
+
 def test_decode_nothing_scored():
     check_decode(37, 8, 2, 128, [300, 40], [300, 100])
 
