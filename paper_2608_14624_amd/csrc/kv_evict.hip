@@ -33,7 +33,6 @@ constexpr int kBlock = 16;
 constexpr int kSelectThreads = 1024;
 constexpr int kSelectWaves = kSelectThreads / 64;
 constexpr int kBins = 2 * kSelectThreads;   // 11 bits
-constexpr int kXcds = 8;
 constexpr int kCopyThreads = 256;
 constexpr int kCopyRows = 32;          // rows of a copy work-group
 constexpr int kCompactVecs = 4;        // 16-byte vectors of a row per work-group (64 bytes)
@@ -86,15 +85,10 @@ __device__ __forceinline__ int block_scan(int mine, int lane, int wave, int* sum
 __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(EvictParams p) {
   __shared__ unsigned hist[kBins];
   __shared__ int sums[2][kSelectWaves];
-  __shared__ uint16_t chosen[kSelectThreads * kBlock];
   __shared__ unsigned found[3];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  // Work-groups are dealt to the XCDs in turn: all heads of a sequence on one XCD, whose L2
-  // then fetches a block's scores (512 bytes at 8 heads, of which a head takes 64) once.
-  const int turn = blockIdx.x / kXcds;
-  const int r = turn / p.num_kv_heads * kXcds + blockIdx.x % kXcds;
-  const int g = turn % p.num_kv_heads;
-  if (r >= p.batch) return;
+  const int g = blockIdx.x % p.num_kv_heads;
+  const int r = blockIdx.x / p.num_kv_heads;
   const int len = p.seq_lens[r];
   const int from = max(0, p.keep_from[r]);
   int32_t* kept = p.kept + ((size_t)r * p.num_kv_heads + g) * p.budget;
@@ -111,14 +105,9 @@ __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(EvictParam
   // those that do not compete (at least `want` do, so they are never chosen)
   const int first = from / kBlock;
   const int blocks = ceil_div(end, kBlock) - first;
-  // (a wave without any of a chunk's keys passes its work by: there are more waves on a CU than
-  // it can run at once, and a sequence of 6000 keys has work for 6 of 16)
-  const int wave_u = __builtin_amdgcn_readfirstlane(wave);
-  auto busy = [&](int chunk) { return (first + chunk * kSelectThreads + 64 * wave_u) * kBlock < end; };
   unsigned rank[kBlock];
   auto load = [&](int chunk) __attribute__((always_inline)) {
     const int b = first + chunk * kSelectThreads + tid;
-    if (!busy(chunk)) return;
 #pragma unroll
     for (int e = 0; e < kBlock; ++e) rank[e] = 0;
     if (b * kBlock >= end) return;
@@ -149,7 +138,6 @@ __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(EvictParam
     const int above = pass == 1 ? 21 : 10;        // bits that the passes before have found
     for (int c = 0; c < chunks; ++c) {
       if (chunks > 1) load(c);
-      if (!busy(c)) continue;
 #pragma unroll
       for (int e = 0; e < kBlock; ++e)
         if (pass == 0 ? rank[e] != 0 : rank[e] >> above == prefix >> above)
@@ -180,38 +168,29 @@ __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(EvictParam
       break;
     }
   }
-  // In ascending order: all keys above the rank, and the first `need` at it.  A chunk's are
-  // collected in LDS (as offsets from its first key) and stored together.
+  // in ascending order: all keys above the rank, and the first `need` at it
   int above = 0, at = 0;                          // before this chunk
   for (int c = 0; c < chunks; ++c) {
     if (chunks > 1) load(c);
     int n_above = 0, n_at = 0;
-    if (busy(c)) {
 #pragma unroll
-      for (int e = 0; e < kBlock; ++e) {
-        n_above += rank[e] > prefix;
-        n_at += rank[e] == prefix;
-      }
+    for (int e = 0; e < kBlock; ++e) {
+      n_above += rank[e] > prefix;
+      n_at += rank[e] == prefix;
     }
     int all;
     const int before = block_scan(n_above | n_at << 16, lane, wave, sums[c & 1], all);
     int a = above + (before & 0xffff), t = at + (int)((unsigned)before >> 16);
-    const int out = above + min(at, need);         // the chunk's first
+    const int key = (first + c * kSelectThreads + tid) * kBlock;
+#pragma unroll
+    for (int e = 0; e < kBlock; ++e) {
+      const bool is_above = rank[e] > prefix, is_at = rank[e] == prefix;
+      if (is_above || (is_at && t < need)) kept[a + min(t, need)] = key + e;
+      a += is_above;
+      t += is_at;
+    }
     above += all & 0xffff;
     at += (int)((unsigned)all >> 16);
-    const int n = above + min(at, need) - out;
-    if (busy(c)) {
-#pragma unroll
-      for (int e = 0; e < kBlock; ++e) {
-        const bool is_above = rank[e] > prefix, is_at = rank[e] == prefix;
-        if (is_above || (is_at && t < need)) chosen[a + min(t, need) - out] = (uint16_t)(tid * kBlock + e);
-        a += is_above;
-        t += is_at;
-      }
-    }
-    __syncthreads();
-    const int key0 = (first + c * kSelectThreads) * kBlock;
-    for (int i = tid; i < n; i += kSelectThreads) kept[out + i] = key0 + chosen[i];
     __syncthreads();
   }
 }
@@ -365,8 +344,7 @@ hipError_t launch_kv_evict(const EvictLaunch& a, hipStream_t stream) {
   p.trigger = a.trigger;
   p.recent = a.recent;
   const unsigned pairs = (unsigned)((long long)a.batch * a.num_kv_heads);
-  const unsigned all = (unsigned)((a.batch + kXcds - 1) / kXcds * kXcds) * (unsigned)a.num_kv_heads;
-  hipLaunchKernelGGL(evict_select_kernel, dim3(all), dim3(kSelectThreads), 0, stream, p);
+  hipLaunchKernelGGL(evict_select_kernel, dim3(pairs), dim3(kSelectThreads), 0, stream, p);
   if (a.dst_tables != nullptr) {
     const unsigned chunks = (unsigned)((a.budget + kBlock - 1 + kCopyRows - 1) / kCopyRows);
     if (a.head_dim == 128)
