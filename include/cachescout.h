@@ -513,7 +513,8 @@ int64_t cs_decode_window_workspace_bytes(int32_t batch, int32_t max_seq_len, int
  * they move with the blocks.  Weights and their sums are fp32.  Keys before
  * score_from[r] are attended but not scored: a shared anchor's blocks belong to
  * several sequences.  Every block that holds scored keys must belong to one
- * sequence of the call alone.  Nothing else in score_pool is changed.
+ * sequence of the call alone, and stand once in its table.  Nothing else in
+ * score_pool is changed.
  *
  * Arguments as in cs_paged_decode_attn_ws, except
  *   seq_lens       each in [0, max_seq_len]; a row with L = 0 gets zeros and scores
@@ -566,7 +567,8 @@ int64_t cs_decode_scores_workspace_bytes(int32_t batch, int32_t max_seq_len, int
  *
  * Arguments as in cs_prefill_paged_attn, plus
  *   score_from     device, int32 [batch], each >= 0.  The blocks that hold scored
- *                  keys must belong to one invocation of the call alone.
+ *                  keys must belong to one invocation of the call alone, and
+ *                  stand once in its table.
  *   rows           >= 1: how many of the last suffix rows count; S or more: all.
  *   decay          in [0, 1], else CS_ERR_INVALID_ARG.
  *   score_pool     as in cs_decode_attn_scores.
