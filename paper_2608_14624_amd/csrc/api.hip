@@ -968,10 +968,10 @@ int cs_kv_evict(float* score_pool, void* k_pool, void* v_pool, const int32_t* bl
     return fail(CS_ERR_INVALID_ARG, "max_blocks_per_seq * block_size < max_seq_len");
   if (!aligned16(score_pool) || !aligned16(k_pool) || !aligned16(v_pool))
     return fail(CS_ERR_INVALID_ARG, "the pools must be 16-byte aligned");
-  if ((long long)batch * num_kv_heads * ((budget + 15LL + 63) / 64 + 33) > 0x7fffffffLL)
+  if (dst_block_tables == block_tables) dst_block_tables = nullptr;
+  if (cs::evict_threads(batch, num_kv_heads, head_dim, budget, dst_block_tables != nullptr) > (double)0xffffffffu)
     return fail(CS_ERR_INVALID_ARG, "launch too large");
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
-  if (dst_block_tables == block_tables) dst_block_tables = nullptr;
   if (debug_checks_enabled()) {
     int st = debug_check_evict(block_tables, dst_block_tables, seq_lens, keep_from, batch, max_seq_len,
                                max_blocks_per_seq, num_blocks, budget, trigger, s);

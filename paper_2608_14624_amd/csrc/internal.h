@@ -217,6 +217,8 @@ struct EvictLaunch {
   int recent;
 };
 hipError_t launch_kv_evict(const EvictLaunch& a, hipStream_t stream);
+// threads of its largest launch (a launch has fewer than 2^32); moving: into other blocks
+double evict_threads(int batch, int num_kv_heads, int head_dim, int budget, bool moving);
 
 // Cascade decode: the shared prefix of each group of sequences is attended
 // once with the group's queries stacked (shared_prefix_partials_kernel), in

@@ -323,7 +323,15 @@ __global__ __launch_bounds__(kCopyThreads) void evict_compact_kernel(EvictParams
   }
 }
 
+unsigned copy_chunks(int budget) { return ((unsigned)budget + kBlock - 1 + kCopyRows - 1) / kCopyRows; }
+unsigned compact_columns(int head_dim) { return 2 * (head_dim / 8 / kCompactVecs) + 1; }
+
 }  // namespace
+
+double evict_threads(int batch, int num_kv_heads, int head_dim, int budget, bool moving) {
+  const double second = moving ? copy_chunks(budget) : compact_columns(head_dim);
+  return (double)batch * num_kv_heads * std::max((double)kSelectThreads, second * kCopyThreads);
+}
 
 hipError_t launch_kv_evict(const EvictLaunch& a, hipStream_t stream) {
   EvictParams p;
@@ -346,13 +354,13 @@ hipError_t launch_kv_evict(const EvictLaunch& a, hipStream_t stream) {
   const unsigned pairs = (unsigned)((long long)a.batch * a.num_kv_heads);
   hipLaunchKernelGGL(evict_select_kernel, dim3(pairs), dim3(kSelectThreads), 0, stream, p);
   if (a.dst_tables != nullptr) {
-    const unsigned chunks = (unsigned)((a.budget + kBlock - 1 + kCopyRows - 1) / kCopyRows);
+    const unsigned chunks = copy_chunks(a.budget);
     if (a.head_dim == 128)
       hipLaunchKernelGGL(evict_copy_kernel<128>, dim3(pairs * chunks), dim3(kCopyThreads), 0, stream, p);
     else
       hipLaunchKernelGGL(evict_copy_kernel<64>, dim3(pairs * chunks), dim3(kCopyThreads), 0, stream, p);
   } else {
-    const unsigned columns = (unsigned)(2 * (p.vecs / kCompactVecs) + 1);
+    const unsigned columns = compact_columns(a.head_dim);
     hipLaunchKernelGGL(evict_compact_kernel, dim3(pairs * columns), dim3(kCopyThreads), 0, stream, p);
   }
   return hipGetLastError();

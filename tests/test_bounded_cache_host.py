@@ -61,7 +61,15 @@ REFUSALS = {
     "evict": COMMON + [(dict(budget=0), BAD), (dict(trigger=7), BAD), (dict(recent=9), BAD), (dict(recent=-1), BAD),
                        (dict(kept=None), BAD), (dict(new_lens=None), BAD), (dict(keep_from=None), BAD),
                        (dict(seq_lens=None), BAD), (dict(score_pool=FAKE + 8), BAD), (dict(max_seq_len=-1), BAD),
-                       (dict(batch=2 ** 30, num_kv_heads=8), BAD)],
+                       (dict(batch=2 ** 30, num_kv_heads=8), BAD),
+                       # 2^32 threads or more: of the selection, of the copy, of the moves within blocks
+                       (dict(batch=2 ** 21), BAD),
+                       (dict(batch=2 ** 16, dst_block_tables=FAKE + 16, budget=4096, trigger=4096), BAD),
+                       (dict(batch=2 ** 20, head_dim=128, num_kv_heads=1, dst_block_tables=FAKE + 16,
+                             budget=2 ** 31 - 1, trigger=2 ** 31 - 1), BAD),
+                       (dict(batch=1, num_kv_heads=256, dst_block_tables=FAKE + 16, budget=2 ** 31 - 1,
+                             trigger=2 ** 31 - 1), BAD),
+                       (dict(batch=2 ** 20, num_kv_heads=2, head_dim=128), BAD)],
 }
 
 
