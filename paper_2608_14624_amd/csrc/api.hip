@@ -181,7 +181,8 @@ int debug_check_decode(const int32_t* block_tables, const int32_t* seq_lens, int
 // Every key from keep[r] on lies in a block of one sequence alone (scores are added
 // without atomics, and an eviction moves keys).
 int debug_check_private(const int32_t* block_tables, const std::vector<int32_t>& lens, const int32_t* keep_d,
-                        const char* what, int batch, int max_blocks_per_seq, int num_blocks, hipStream_t stream) {
+                        const char* what, int batch, int max_blocks_per_seq, int num_blocks, hipStream_t stream,
+                        bool may_share = false) {
   std::vector<int32_t> from, bt;
   hipError_t e = copy_to_host(from, keep_d, (size_t)batch, stream);
   if (e == hipSuccess) e = copy_to_host(bt, block_tables, (size_t)batch * max_blocks_per_seq, stream);
@@ -193,7 +194,7 @@ int debug_check_private(const int32_t* block_tables, const std::vector<int32_t>&
       const int32_t slot = bt[(size_t)r * max_blocks_per_seq + b];
       if (slot < 0 || slot >= num_blocks)
         return fail(CS_ERR_INVALID_ARG, "block_tables[%d][%d] = %d outside [0, %d)", r, b, slot, num_blocks);
-      if (seen[slot])
+      if (seen[slot] && !may_share)
         return fail(CS_ERR_INVALID_ARG, "block %d holds keys past %s of two places (sequence %d)", slot, what, r);
       seen[slot] = 1;
     }
@@ -212,7 +213,9 @@ int debug_check_evict(const int32_t* block_tables, const int32_t* dst_tables, co
   for (int r = 0; r < batch; ++r)
     if (sl[r] < 0 || sl[r] > max_seq_len)
       return fail(CS_ERR_INVALID_ARG, "seq_lens[%d] = %d outside [0, %d]", r, sl[r], max_seq_len);
-  int st = debug_check_private(block_tables, sl, keep_from, "keep_from", batch, max_blocks_per_seq, num_blocks, stream);
+  // (blocks that are only read may be several sequences')
+  int st = debug_check_private(block_tables, sl, keep_from, "keep_from", batch, max_blocks_per_seq, num_blocks, stream,
+                               dst_tables != nullptr);
   if (st != CS_OK || !dst_tables) return st;
   // the new blocks: different, and none that a sequence's keys past keep_from lie in
   std::vector<int32_t> bt;

@@ -410,5 +410,6 @@ def test_debug_checks(monkeypatch):
     window(tables=outside)                             # out of sight
     window(lens=i32(0, 300))
     evicts(good)
+    evicts(good, tables=shared)                        # old blocks are only read
     evicts(None)
     torch.cuda.synchronize()
