@@ -199,7 +199,7 @@ __global__ __launch_bounds__(kThreads, 4) void key_stats_kernel(ScoreParams p) {
 
   const float c = p.scale_log2;
   // finite, so that keys a row does not see weigh 0 and not NaN
-  float m = -FLT_MAX / fmaxf(c, 1.f);
+  float m = lowest_reference(c);
   float l[4] = {0.f, 0.f, 0.f, 0.f};
   auto compute = [&](int step, const uint16_t* buf) __attribute__((always_inline)) {
     f32x16 s[2] = {f32x16{}, f32x16{}};

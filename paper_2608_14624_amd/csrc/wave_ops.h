@@ -3,6 +3,8 @@
 
 #include <hip/hip_runtime.h>
 
+#include <math.h>
+
 namespace cs {
 namespace {
 
@@ -30,6 +32,13 @@ __device__ __forceinline__ int wave_max(int x) {
   x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false));
   return __builtin_amdgcn_readlane(x, 63);
 }
+
+// A reference for the logits of a row that has seen no key, in softmaxes of exp2(c (s - m)) with
+// c > 0: about the lowest m for which m and m c are finite, so that masked logits (-inf) weigh 0
+// and not NaN.  -FLT_MAX / c itself will not do: it is rounded, and times c it is infinite for one
+// c in seven above 1.  Both roundings are off by at most 2^-24 of the value, and the number here is
+// about 2^-21 (eight times that) below FLT_MAX.
+__host__ __device__ inline float lowest_reference(float c) { return -0x1.fffffp127f / fmaxf(c, 1.f); }
 
 }  // namespace
 }  // namespace cs
