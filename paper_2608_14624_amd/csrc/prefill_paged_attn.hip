@@ -71,7 +71,6 @@
 #include "internal.h"
 #include "wave_ops.h"
 
-#include <float.h>
 #include <math.h>
 
 #include <algorithm>
@@ -1201,7 +1200,7 @@ __global__ __launch_bounds__(kPPThreads, D == 64 ? 4 : 2) void prefill_paged_att
     const float c = p.scale_log2;
     // running max of the raw (unscaled) logits; under a window a row may see none of
     // the first steps' keys: finite, so that those weigh 0 and not NaN
-    float m_run = kWindow ? -FLT_MAX / fmaxf(c, 1.f) : -INFINITY;
+    float m_run = kWindow ? lowest_reference(c) : -INFINITY;
     float l_part[4] = {0.f, 0.f, 0.f, 0.f};
 
     // M phase of iteration j: S_j = K_j Q^T, then O += P_{j-1} V_{j-1} (the

@@ -4,8 +4,9 @@ multiplied by it again, has to stay finite: rows that see none of the first keys
 import numpy as np
 import pytest
 
-from bounded_cache_util import Paged, bf16_bits, to_gpu, weight_bound
-from oracle import add_key_scores, bf16_bits_to_f64
+from bounded_cache_util import Paged, attention_bound, bf16_bits, to_gpu, weight_bound
+from oracle import add_key_scores, bf16_bits_to_f64, window_attention
+from test_gpu_window_attention import prefill_batch, run_prefill
 
 pytestmark = pytest.mark.gpu
 
@@ -47,3 +48,27 @@ def test_prompt_scores(scale, hq, hkv, d, invs, rows):
         add_key_scores(want, q[cu[r + 1] - n:cu[r + 1]], pg.k, pg.tables[r], p + s - n, p, 0, hq, hkv, scale, 1.0)
     assert np.isfinite(got).all(), f"{(~np.isfinite(got)).sum()} scores are not finite"
     assert (np.abs(got - want) <= weight_bound(want)).all(), np.abs(got - want).max()
+
+
+@pytest.mark.parametrize("scale", SCALES)
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("invs", [[(700, 1100), (0, 1100)],
+                                  [(500, 900), (0, 1300), (80, 3), (0, 0), (1200, 700), (33, 65), (0, 640)],
+                                  [(300, 70), (0, 130), (517, 1)]])
+@pytest.mark.parametrize("window,sinks", [(1, 0), (37, 9)])
+def test_window_prefill(scale, d, invs, window, sinks):
+    """Equal and ragged ping-pong tiles and split tiles under a window that leaves a tile's later rows
+    nothing of its first step."""
+    scale, hq, hkv, heads = float(np.float32(scale)), 32, 8, [5, 30]
+    print(f"[case] window prefill at scale {scale}, heads of {d}, {invs}, window {window}, sinks {sinks}", flush=True)
+    pg, _ = prefill_batch(72, hq, hkv, d, invs, window, sinks)
+    q = small_queries(pg.rng, sum(s for _, s in invs), hq, d)
+    got, cu = run_prefill(pg, q, invs, window, sinks, scale)
+    for r, (p, s) in enumerate(invs):
+        if s == 0:
+            continue
+        out, mag = window_attention(q[cu[r]:cu[r + 1]], pg.k, pg.v, pg.tables[r], p, hq, hkv, scale, window, sinks,
+                                    heads)
+        err = np.abs(got[cu[r]:cu[r + 1]][:, heads] - out)
+        assert np.isfinite(err).all(), f"invocation {r}: {(~np.isfinite(err)).sum()} elements are not finite"
+        assert (err <= attention_bound(out, mag)).all(), f"invocation {r}: {err.max()}"
