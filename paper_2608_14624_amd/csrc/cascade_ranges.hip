@@ -37,7 +37,6 @@
 #include "decode_common.h"
 #include "internal.h"
 
-#include <float.h>
 #include <math.h>
 
 #include <algorithm>
@@ -303,7 +302,7 @@ __global__ __launch_bounds__(64, D == 64 ? 2 : 1) void cascade_ranges_kernel(Cas
   const float c = p.scale_log2;
   const float drop = 8.f / c;
   // a unit whose logits are all -inf weighs 0 relative to this, not NaN
-  const float lowest = -FLT_MAX / fmaxf(c, 1.f);
+  const float lowest = lowest_reference(c);
 
   bf16x8 kreg[2][DC];
   bf16x8 vreg[kVLoads];

@@ -37,7 +37,6 @@
 #include "decode_common.h"
 #include "internal.h"
 
-#include <float.h>
 #include <math.h>
 
 #include <algorithm>
@@ -756,7 +755,7 @@ __global__ __launch_bounds__(64) void decode_ranges_kernel(DecParams p) {
   const int h = g * p.group + (head_valid ? j : 0);
   const float c = p.scale_log2;
   // a unit whose logits are all -inf weighs 0 relative to this, not NaN
-  const float lowest = -FLT_MAX / fmaxf(c, 1.f);
+  const float lowest = lowest_reference(c);
 
   bf16x8 kreg[2][DC];
   bf16x8 vreg[kVLoads];
@@ -1084,7 +1083,7 @@ __global__ __launch_bounds__(kScoreThreads) void decode_scores_pair_kernel(DecPa
   const bool head_valid = j < p.group;
   const int h = g * p.group + (head_valid ? j : 0);
   const float c = p.scale_log2;
-  const float lowest = -FLT_MAX / fmaxf(c, 1.f);      // as in decode_ranges_kernel
+  const float lowest = lowest_reference(c);      // as in decode_ranges_kernel
   bf16x8 qreg[DC];
 #pragma unroll
   for (int dc = 0; dc < DC; ++dc) {
