@@ -301,6 +301,12 @@ __global__ __launch_bounds__(64) void key_stats_merge_kernel(ScoreParams p) {
   if (at < all) p.stats[at] = merged_stats(p, p.stats + at, all);
 }
 
+// The first scored key of an invocation, its length if there is none (score_from may be any
+// number from 0 on, and what follows adds to it).
+__device__ __forceinline__ int first_scored(const ScoreParams& p, const Observed& ob) {
+  return min(max(0, p.score_from[ob.r]), ob.len);
+}
+
 // How the scored keys of an invocation are dealt to its p.tiles work-groups: kWeightKeys
 // each, and, where work-groups are left (the longest invocation, scored from its first
 // key on, has one per key tile), with their rows in parts of at least kPartTiles tiles.
@@ -308,7 +314,7 @@ __global__ __launch_bounds__(64) void key_stats_merge_kernel(ScoreParams p) {
 struct Dealt {
   int key_tiles, row_tiles, parts;
   __device__ __forceinline__ Dealt(const ScoreParams& p, const Observed& ob, int from) {
-    key_tiles = max(0, ceil_div(ob.len - from / kBlock * kBlock, kWeightKeys));
+    key_tiles = from < ob.len ? ceil_div(ob.len - from / kBlock * kBlock, kWeightKeys) : 0;
     row_tiles = ceil_div(ob.n * p.group, kTile);
     parts = key_tiles == 0 ? 0 : max(1, min(p.tiles / key_tiles, ceil_div(row_tiles, kPartTiles)));
   }
@@ -341,7 +347,7 @@ __global__ __launch_bounds__(kThreads, 4) void key_weights_kernel(ScoreParams p)
   const int g = rest % p.num_kv_heads;
   rest /= p.num_kv_heads;
   const Observed ob(p, rest / p.tiles, g);
-  const int from = max(0, uniform(p.score_from[ob.r]));
+  const int from = uniform(first_scored(p, ob));
   const int n_rows = ob.n * p.group;
   const Dealt dealt(p, ob, from);
   const int wg = rest % p.tiles;
@@ -487,7 +493,7 @@ __global__ __launch_bounds__(kWeightKeys) void key_weights_merge_kernel(ScorePar
   rest /= p.num_kv_heads;
   const int tile = rest % p.key_tiles;
   const Observed ob(p, rest / p.key_tiles, g);
-  const int from = max(0, p.score_from[ob.r]);
+  const int from = first_scored(p, ob);
   const Dealt dealt(p, ob, from);
   const int key = from / kBlock * kBlock + tile * kWeightKeys + threadIdx.x;
   if (ob.n == 0 || dealt.parts <= 1 || key < from || key >= ob.len) return;

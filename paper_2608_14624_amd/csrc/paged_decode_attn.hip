@@ -196,6 +196,12 @@ __device__ __forceinline__ f32x4 quad_scores(const DecParams& p, f32x4 old, f32x
   return w;
 }
 
+// The first scored key of sequence r, its length if there is none (score_from may be any number
+// from 0 on, and what follows adds to it).
+__device__ __forceinline__ int first_scored(const DecParams& p, int r, int len) {
+  return min(max(0, p.score_from[r]), len);
+}
+
 __device__ __forceinline__ float* score_at(const DecParams& p, int id, int g, int key) {
   return p.score_pool + ((size_t)id * p.num_kv_heads + g) * kBlock + key % kBlock;
 }
@@ -616,7 +622,7 @@ __global__ __launch_bounds__(64) void decode_ranges_kernel(DecParams p) {
     total += wave_total(n_of[i]);
     if constexpr (kScored) {
       const int s = 64 * i + lane;
-      unscored += wave_total(s < p.batch ? min(n_of[i], units_of(p.score_from[s])) : 0);
+      unscored += wave_total(s < p.batch ? units_of(min(p.score_from[s], n_of[i] * kUnitKeys)) : 0);
     }
     longest = max(longest, wave_max(n_of[i]));
   });
@@ -996,9 +1002,9 @@ __global__ __launch_bounds__(kMergeThreads) void decode_scores_kernel(DecParams 
   }
   const int chunk = blockIdx.x / pairs - 1;
   const int len = p.seq_lens[r];
-  const int from = max(0, p.score_from[r]);
-  const int first = from / kUnitKeys * kUnitKeys + chunk * kScoreKeys;
-  if (first >= len) return;
+  const int from = first_scored(p, r, len);
+  const long long first = from / kUnitKeys * kUnitKeys + (long long)chunk * kScoreKeys;
+  if (from >= len || first >= len) return;
   const int2 piece = pieces_of<Keys::kScored>(p, r, lane);
   __shared__ float2 stat[kMaxGroup];
   const float c = p.scale_log2;
@@ -1020,7 +1026,7 @@ __global__ __launch_bounds__(kMergeThreads) void decode_scores_kernel(DecParams 
     if (lane == 0) stat[j] = make_float2(m_all * c, 1.f / l);
   }
   __syncthreads();
-  const int key = first + 4 * threadIdx.x;
+  const int key = (int)first + 4 * threadIdx.x;
   if (key + 3 < from || key >= len || (key - from / kUnitKeys * kUnitKeys) / kUnitKeys >= p.logit_units) return;
   f32x4* score = reinterpret_cast<f32x4*>(
       score_at(p, p.block_tables[(size_t)r * p.max_blocks_per_seq + key / kBlock], g, key));
@@ -1073,7 +1079,7 @@ __global__ __launch_bounds__(kScoreThreads) void decode_scores_pair_kernel(DecPa
   r = __builtin_amdgcn_readfirstlane(r);
   const ScalarInts bt = (ScalarInts)(p.block_tables + (size_t)r * p.max_blocks_per_seq);
   const int len = __builtin_amdgcn_readfirstlane(p.seq_lens[r]);
-  const int from = __builtin_amdgcn_readfirstlane(max(0, p.score_from[r]));
+  const int from = __builtin_amdgcn_readfirstlane(first_scored(p, r, len));
   const int from_unit = from / kUnitKeys;
   const int units = units_of(len);
   const size_t tile_elems = (size_t)kBlock * D;
@@ -1164,7 +1170,7 @@ __global__ __launch_bounds__(kScoreThreads) void decode_scores_pair_kernel(DecPa
 
   // the scores of the first quads, in flight during the merge
   const int first = from / 4 * 4;
-  const int last = (int)min((long long)len, (long long)(from_unit + p.logit_units) * kUnitKeys);
+  const int last = from < len ? (int)min((long long)len, (long long)(from_unit + p.logit_units) * kUnitKeys) : 0;
   f32x4* at[kScoreQuads];
   f32x4 old[kScoreQuads];
   auto load_scores = [&](int key0) __attribute__((always_inline)) {

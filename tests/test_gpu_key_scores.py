@@ -219,3 +219,18 @@ def test_prefill_of_one_token_is_the_decode():
                               max_kv_len=n, rows=1, scale=0.09, decay=0.5)
     torch.cuda.synchronize()
     np.testing.assert_allclose(sd.cpu().numpy(), by_decode, rtol=1e-4, atol=1e-7, equal_nan=True)
+
+
+@pytest.mark.parametrize("lens", [[3000, 45], [1501 + i for i in range(130)]])
+@pytest.mark.parametrize("beyond", [0, 1, 3, 2 ** 31 - 1])
+def test_decode_scored_from_its_end_or_beyond(lens, beyond):
+    """Nothing of the first sequence is scored, however far past its end score_from lies, in ranges
+    and by pairs; the others are as ever."""
+    froms = [min(lens[0] + beyond, 2 ** 31 - 1)] + [7] * (len(lens) - 1)
+    check_decode(49, 8, 2, 128, lens, froms, max_scored=max(lens), rows=[0, 1])
+
+
+@pytest.mark.parametrize("rows", [5, 400])
+@pytest.mark.parametrize("beyond", [0, 1, 2 ** 31 - 1])
+def test_prefill_scored_from_its_end_or_beyond(rows, beyond):
+    check_prefill(50, 32, 8, 128, [(1700, 405), (0, 390)], [min(2105 + beyond, 2 ** 31 - 1), 3], rows)
