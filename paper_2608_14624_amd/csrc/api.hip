@@ -910,7 +910,8 @@ int cs_prefill_key_scores(const void* q, const void* k_pool, const int32_t* bloc
     e = copy_to_host(cu, cu_q_lens, (size_t)batch + 1, s);
     if (e == hipSuccess) e = copy_to_host(lens, prefix_lens, (size_t)batch, s);
     if (e != hipSuccess) return hip_fail(e, "CS_DEBUG_CHECK metadata copy");
-    for (int r = 0; r < batch; ++r) lens[r] += cu[r + 1] - cu[r];
+    // (an invocation without rows scores nothing: its blocks may be another's)
+    for (int r = 0; r < batch; ++r) lens[r] = cu[r + 1] > cu[r] ? lens[r] + cu[r + 1] - cu[r] : 0;
     st = debug_check_private(block_tables, lens, score_from, "score_from", batch, max_blocks_per_seq, num_blocks, s);
     if (st != CS_OK) return st;
   }

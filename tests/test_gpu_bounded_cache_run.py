@@ -413,3 +413,27 @@ def test_debug_checks(monkeypatch):
     evicts(good, tables=shared)                        # old blocks are only read
     evicts(None)
     torch.cuda.synchronize()
+
+
+def test_debug_checks_leave_invocations_without_rows_alone(monkeypatch):
+    """An invocation without suffix rows changes no score, so its blocks may be another's."""
+    from paper_2608_14624_amd import ops
+    monkeypatch.setenv("CS_DEBUG_CHECK", "1")
+    pg = Paged(67, [200, 300], HKV, D)
+    tables = np.concatenate([pg.tables[1:], pg.tables[1:], pg.tables[:1]])
+    sd = to_gpu(np.zeros((pg.num_blocks, HKV, 16), dtype=np.float32))
+    q = bf16_bits(pg.rng, 3, HQ, D)
+    print("[case] debug checks of prompt scores with an invocation without rows", flush=True)
+    run = lambda cu: ops.cs_prefill_key_scores(to_gpu(q), to_gpu(pg.k), to_gpu(tables), i32(298, 298, 199),
+                                               i32(*cu), i32(0, 0, 0), sd, max_q_len=2, max_kv_len=300, rows=3,
+                                               scale=SCALE)
+    run([0, 0, 2, 3])
+    run([0, 2, 2, 3])
+    with pytest.raises(ops.CacheScoutError, match="CS_ERR_INVALID_ARG"):
+        run([0, 1, 2, 3])
+    torch.cuda.synchronize()
+    want = np.zeros((pg.num_blocks, HKV, 16))
+    for _ in range(2):
+        add_key_scores(want, q[:2], pg.k, tables[0], 298, 298, 0, HQ, HKV, SCALE, 1.0)
+        add_key_scores(want, q[2:], pg.k, tables[2], 199, 199, 0, HQ, HKV, SCALE, 1.0)
+    check_scores(sd, want, tables[[0, 2]], [300, 200], 0)
