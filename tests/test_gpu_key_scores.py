@@ -234,3 +234,9 @@ def test_decode_scored_from_its_end_or_beyond(lens, beyond):
 @pytest.mark.parametrize("beyond", [0, 1, 2 ** 31 - 1])
 def test_prefill_scored_from_its_end_or_beyond(rows, beyond):
     check_prefill(50, 32, 8, 128, [(1700, 405), (0, 390)], [min(2105 + beyond, 2 ** 31 - 1), 3], rows)
+
+
+@pytest.mark.parametrize("lens", [[9000] + [40 + i for i in range(31)], [6144 - i for i in range(32)]])
+def test_decode_of_a_batch_that_one_sequence_may_dominate(lens):
+    """Both sides of the bound on the longest sequence up to which a work-group takes a whole one."""
+    check_decode(52, 16, 8, 128, lens, [3] * 32, rows=[0, 31], decay=0.8)
