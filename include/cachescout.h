@@ -546,7 +546,7 @@ int cs_decode_attn_scores(const void *q, const void *k_pool, const void *v_pool,
  * (at least as many as compute units, max_seq_len at most 6144 times as many as there
  * are per compute unit, and max_scored_len at least three quarters of max_seq_len).
  * num_cus as there; -1 for a negative size, bad head counts, a head_dim other than 64
- * or 128, or max_scored_len above max_seq_len. */
+ * or 128, max_scored_len above max_seq_len, or a launch too large (2^32 threads). */
 int64_t cs_decode_scores_workspace_bytes(int32_t batch, int32_t max_seq_len, int32_t max_scored_len,
                                          int32_t num_q_heads, int32_t num_kv_heads,
                                          int32_t head_dim, int32_t num_cus);
@@ -593,7 +593,7 @@ int cs_prefill_key_scores(const void *q, const void *k_pool, const int32_t *bloc
 
 /* Workspace bytes cs_prefill_key_scores needs.  num_cus: compute units to size
  * for, 0 = the current device's (-1 if there is none).  -1 for a negative size,
- * rows below 1 or bad head counts. */
+ * rows below 1, bad head counts, or a launch too large (2^32 threads). */
 int64_t cs_prefill_scores_workspace_bytes(int32_t batch, int32_t total_q, int32_t max_q_len,
                                           int32_t max_kv_len, int32_t rows, int32_t num_q_heads,
                                           int32_t num_kv_heads, int32_t num_cus);

@@ -334,7 +334,8 @@ int validate_decode(const void* q, const void* k_pool, const void* v_pool,
     return fail(CS_ERR_INVALID_ARG, "max_blocks_per_seq * block_size < max_seq_len");
   if (!aligned16(q) || !aligned16(k_pool) || !aligned16(v_pool))
     return fail(CS_ERR_INVALID_ARG, "q, k_pool and v_pool must be 16-byte aligned");
-  if ((long long)batch * num_kv_heads > 0x7fffffffLL) return fail(CS_ERR_INVALID_ARG, "launch too large");
+  // (every form of the decode has a work-group of 256 threads or more for each)
+  if (!cs::launch_fits((double)batch * num_kv_heads, 256)) return fail(CS_ERR_INVALID_ARG, "launch too large");
   return CS_OK;
 }
 
@@ -428,6 +429,8 @@ int paged_decode(const void* q, const void* k_pool, const void* v_pool,
       if (!aligned16(out)) geo = {};   // the range kernels store eight bytes at a time
     }
   }
+  if (!cs::decode_fits(geo, batch, num_kv_heads, extra.score_pool ? scored_units(extra.max_scored_len) : -1))
+    return fail(CS_ERR_INVALID_ARG, "launch too large");
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   if (debug_checks_enabled()) {
     int st = debug_check_decode(block_tables, seq_lens, batch, max_seq_len, max_blocks_per_seq,
@@ -838,9 +841,6 @@ int cs_decode_attn_scores(const void* q, const void* k_pool, const void* v_pool,
   if (!(decay >= 0.f && decay <= 1.f)) return fail(CS_ERR_INVALID_ARG, "decay %g outside [0, 1]", (double)decay);
   if (batch > 0 && (!score_from || !score_pool)) return fail(CS_ERR_INVALID_ARG, "null pointer argument");
   if (!aligned16(score_pool)) return fail(CS_ERR_INVALID_ARG, "score_pool must be 16-byte aligned");
-  if (num_q_heads > 0 && num_kv_heads > 0 &&
-      (long long)batch * num_kv_heads * (1 + (scored_units(max_scored_len) + 63) / 64) > 0x7fffffffLL)
-    return fail(CS_ERR_INVALID_ARG, "launch too large");
   DecodeExtras extra;
   extra.score_from = score_from;
   extra.score_pool = score_pool;
@@ -860,9 +860,9 @@ int64_t cs_decode_scores_workspace_bytes(int32_t batch, int32_t max_seq_len, int
   if (batch == 0) return 0;
   int cus = num_cus;
   if (cus == 0 && cs::current_device_cus(&cus) != hipSuccess) return -1;
-  return decode_range_bytes(scored_geometry(batch, max_seq_len, max_scored_len, num_kv_heads, head_dim, cus),
-                            num_q_heads, head_dim) +
-         logit_bytes(batch, max_scored_len, num_q_heads);
+  const cs::DecodeGeometry geo = scored_geometry(batch, max_seq_len, max_scored_len, num_kv_heads, head_dim, cus);
+  if (!cs::decode_fits(geo, batch, num_kv_heads, scored_units(max_scored_len))) return -1;
+  return decode_range_bytes(geo, num_q_heads, head_dim) + logit_bytes(batch, max_scored_len, num_q_heads);
 }
 
 int cs_prefill_key_scores(const void* q, const void* k_pool, const int32_t* block_tables,
@@ -895,13 +895,15 @@ int cs_prefill_key_scores(const void* q, const void* k_pool, const int32_t* bloc
     return fail(CS_ERR_INVALID_ARG, "max_blocks_per_seq * block_size < max_kv_len");
   if (!aligned16(q) || !aligned16(k_pool) || !aligned16(score_pool))
     return fail(CS_ERR_INVALID_ARG, "q, k_pool and score_pool must be 16-byte aligned");
+  // (more compute units take no fewer work-groups)
+  if (!cs::key_score_geometry(batch, total_q, max_q_len, max_kv_len, rows, num_q_heads, num_kv_heads, 1).fits)
+    return fail(CS_ERR_INVALID_ARG, "launch too large");
   int cus = 0;
   hipError_t e = cs::current_device_cus(&cus);
   if (e != hipSuccess) return hip_fail(e, "compute-unit count of the current device");
   cs::KeyScoreLaunch a;
   a.geo = cs::key_score_geometry(batch, total_q, max_q_len, max_kv_len, rows, num_q_heads, num_kv_heads, cus);
-  if (a.geo.stat_grid > 0x7fffffffLL || a.geo.weight_grid > 0x7fffffffLL)
-    return fail(CS_ERR_INVALID_ARG, "launch too large");
+  if (!a.geo.fits) return fail(CS_ERR_INVALID_ARG, "launch too large");
   // (rows are divided by the group with a 32-bit reciprocal)
   const long long group = num_q_heads / num_kv_heads;
   if (a.geo.max_rows * group * group > 0xffffffffLL)
@@ -955,8 +957,9 @@ int64_t cs_prefill_scores_workspace_bytes(int32_t batch, int32_t total_q, int32_
   if (batch == 0 || total_q == 0 || max_q_len == 0) return 0;
   int cus = num_cus;
   if (cus == 0 && cs::current_device_cus(&cus) != hipSuccess) return -1;
-  return cs::key_score_geometry(batch, total_q, max_q_len, max_kv_len, rows, num_q_heads, num_kv_heads, cus)
-      .bytes;
+  const cs::KeyScoreGeometry geo =
+      cs::key_score_geometry(batch, total_q, max_q_len, max_kv_len, rows, num_q_heads, num_kv_heads, cus);
+  return geo.fits ? geo.bytes : -1;
 }
 
 int cs_kv_evict(float* score_pool, void* k_pool, void* v_pool, const int32_t* block_tables,
@@ -983,7 +986,7 @@ int cs_kv_evict(float* score_pool, void* k_pool, void* v_pool, const int32_t* bl
   if (!aligned16(score_pool) || !aligned16(k_pool) || !aligned16(v_pool))
     return fail(CS_ERR_INVALID_ARG, "the pools must be 16-byte aligned");
   if (dst_block_tables == block_tables) dst_block_tables = nullptr;
-  if (cs::evict_threads(batch, num_kv_heads, head_dim, budget, dst_block_tables != nullptr) > (double)0xffffffffu)
+  if (!cs::evict_fits(batch, num_kv_heads, head_dim, budget, dst_block_tables != nullptr))
     return fail(CS_ERR_INVALID_ARG, "launch too large");
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   if (debug_checks_enabled()) {

@@ -21,6 +21,9 @@ struct Window {
   bool hides(long long key, long long p) const { return size > 0 && key >= sinks && key + 15 <= p - size; }
 };
 
+// A launch has fewer than 2^32 threads.  Calls of several launches check all before the first.
+inline bool launch_fits(double work_groups, int threads) { return work_groups * threads < 4294967296.0; }
+
 // Everything the attention kernel needs, already validated by the ABI layer.
 struct AttnLaunch {
   const uint16_t* q;
@@ -158,6 +161,8 @@ struct DecodeGeometry {
 constexpr int kRangeMaxBatch = 1024;
 
 DecodeGeometry decode_geometry(int batch, int max_seq_len, int num_kv_heads, int head_dim, int cus);
+// Whether the launches of a decode fit; logit_units: of one that adds scores, else -1
+bool decode_fits(const DecodeGeometry& geo, int batch, int num_kv_heads, long long logit_units);
 hipError_t launch_paged_decode_attn(const DecodeLaunch& a, hipStream_t stream);
 
 // Attention weights of a prompt's last rows into the keys' scores (key_scores.hip).
@@ -172,6 +177,7 @@ struct KeyScoreGeometry {
   long long weight_grid;
   long long stat_bytes;     // workspace of the statistics, and all of it
   long long bytes;
+  bool fits;                // every launch does; if not, the rest is not set
 };
 KeyScoreGeometry key_score_geometry(int batch, int total_q, int max_q_len, int max_kv_len, int rows,
                                     int num_q_heads, int num_kv_heads, int cus);
@@ -217,8 +223,8 @@ struct EvictLaunch {
   int recent;
 };
 hipError_t launch_kv_evict(const EvictLaunch& a, hipStream_t stream);
-// threads of its largest launch (a launch has fewer than 2^32); moving: into other blocks
-double evict_threads(int batch, int num_kv_heads, int head_dim, int budget, bool moving);
+// whether its launches fit; moving: into other blocks
+bool evict_fits(int batch, int num_kv_heads, int head_dim, int budget, bool moving);
 
 // Cascade decode: the shared prefix of each group of sequences is attended
 // once with the group's queries stacked (shared_prefix_partials_kernel), in

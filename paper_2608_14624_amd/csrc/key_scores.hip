@@ -507,11 +507,14 @@ __global__ __launch_bounds__(kWeightKeys) void key_weights_merge_kernel(ScorePar
 
 KeyScoreGeometry key_score_geometry(int batch, int total_q, int max_q_len, int max_kv_len, int rows,
                                     int num_q_heads, int num_kv_heads, int cus) {
-  KeyScoreGeometry geo;
+  KeyScoreGeometry geo = {};
   geo.max_rows = std::min(rows, max_q_len);
   const long long stacked = (long long)geo.max_rows * (num_q_heads / num_kv_heads);
   geo.row_tiles = (stacked + kStatRows - 1) / kStatRows;
   geo.key_tiles = ((long long)max_kv_len + kWeightKeys - 1) / kWeightKeys;
+  // (in one part each; so far this also bounds the products below)
+  geo.fits = launch_fits((double)batch * num_kv_heads * std::max(geo.row_tiles, geo.key_tiles), kThreads);
+  if (!geo.fits) return geo;
   const long long pairs = (long long)batch * num_kv_heads;
   // room to split the rows of key tiles that have many, in launches that leave CUs idle
   const long long row_parts = std::min((stacked + kTile * kPartTiles - 1) / (kTile * kPartTiles),
@@ -527,6 +530,8 @@ KeyScoreGeometry key_score_geometry(int batch, int total_q, int max_q_len, int m
   geo.parts = (int)std::max(1LL, std::min({parts, steps / 8, 32LL}));
   geo.stat_grid = pairs * geo.row_tiles * geo.parts;
   geo.weight_grid = pairs * geo.weight_groups;
+  // (the merges have no more threads)
+  geo.fits = launch_fits((double)geo.stat_grid, kThreads) && launch_fits((double)geo.weight_grid, kThreads);
   geo.stat_bytes = geo.parts * pairs * stacked * (long long)sizeof(float2);
   // (the partial sums of the split launches: any invocation may have as few scored keys as
   // to be split)

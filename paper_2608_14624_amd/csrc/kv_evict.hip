@@ -22,8 +22,6 @@
 #include "internal.h"
 #include "wave_ops.h"
 
-#include <algorithm>
-
 namespace cs {
 namespace {
 
@@ -328,9 +326,10 @@ unsigned compact_columns(int head_dim) { return 2 * (head_dim / 8 / kCompactVecs
 
 }  // namespace
 
-double evict_threads(int batch, int num_kv_heads, int head_dim, int budget, bool moving) {
+bool evict_fits(int batch, int num_kv_heads, int head_dim, int budget, bool moving) {
+  const double pairs = (double)batch * num_kv_heads;
   const double second = moving ? copy_chunks(budget) : compact_columns(head_dim);
-  return (double)batch * num_kv_heads * std::max((double)kSelectThreads, second * kCopyThreads);
+  return launch_fits(pairs, kSelectThreads) && launch_fits(pairs * second, kCopyThreads);
 }
 
 hipError_t launch_kv_evict(const EvictLaunch& a, hipStream_t stream) {

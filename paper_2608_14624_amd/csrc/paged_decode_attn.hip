@@ -1322,6 +1322,9 @@ constexpr int pair_lds_bytes(int head_dim) {
          kMaxGroup * (int)sizeof(float2) + kScoreBatch * (int)sizeof(int) + 256;
 }
 
+// work-groups of decode_scores_kernel per (sequence, KV head) that turn logits into weights
+long long score_chunks(long long logit_units) { return (logit_units * kUnitKeys + kScoreKeys - 1) / kScoreKeys; }
+
 template <int D, Keys kKeys>
 void launch_decode(const DecodeLaunch& a, const DecParams& p, hipStream_t stream) {
   const unsigned rows = (unsigned)((long long)a.batch * a.num_kv_heads);
@@ -1342,7 +1345,7 @@ void launch_decode(const DecodeLaunch& a, const DecParams& p, hipStream_t stream
   const size_t staged = kKeys == Keys::kScored ? kStagedUnits * kUnitKeys * p.group * sizeof(float) : 0;
   hipLaunchKernelGGL((decode_ranges_kernel<D, kKeys>), grid, block, staged, stream, p);
   if constexpr (kKeys == Keys::kScored) {
-    const unsigned chunks = (unsigned)(((long long)a.logit_units * kUnitKeys + kScoreKeys - 1) / kScoreKeys);
+    const unsigned chunks = (unsigned)score_chunks(a.logit_units);
     hipLaunchKernelGGL(decode_scores_kernel<D>, dim3(rows * (1 + chunks)), dim3(kMergeThreads), 0, stream, p);
   } else {
     hipLaunchKernelGGL((decode_ranges_merge_kernel<D, kKeys>), dim3(rows), dim3(kMergeThreads), 0, stream, p);
@@ -1360,6 +1363,13 @@ void launch_decode(const DecodeLaunch& a, const DecParams& p, hipStream_t stream
 }
 
 }  // namespace
+
+bool decode_fits(const DecodeGeometry& geo, int batch, int num_kv_heads, long long logit_units) {
+  const double pairs = (double)batch * num_kv_heads;
+  if (geo.ranges == 0) return launch_fits(pairs, logit_units < 0 ? 64 * kDecodeWaves : kScoreThreads);
+  return launch_fits((double)std::max(geo.ranges, geo.aligned_ranges) * num_kv_heads, 64) &&
+         launch_fits(pairs * (1 + (logit_units < 0 ? 0 : score_chunks(logit_units))), kMergeThreads);
+}
 
 hipError_t launch_paged_decode_attn(const DecodeLaunch& a, hipStream_t stream) {
   DecParams p = {};

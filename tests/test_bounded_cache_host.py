@@ -167,3 +167,32 @@ def test_scores_of_a_batch_that_one_sequence_may_dominate_go_in_ranges():
             logits = batch * 4 * hkv * ((keys + 62) // 32) * 128
             need = ops.decode_scores_workspace_bytes(batch, keys, keys, 4 * hkv, hkv, 128, cu)
             assert need == logits + (ranges if keys > 6144 * pairs else 0), (batch, hkv, keys)
+
+
+@pytest.mark.parametrize("name,kw", [
+    # a work-group of 256 threads for every sequence and KV head at the least
+    ("decode", dict(batch=2 ** 23)), ("scores", dict(batch=2 ** 23)), ("prompt", dict(batch=2 ** 23)),
+    ("scores", dict(batch=2 ** 30, num_kv_heads=8)), ("prompt", dict(batch=2 ** 30, num_kv_heads=2 ** 30,
+                                                                     num_q_heads=2 ** 30)),
+    # for every 128 rows and heads, and every 128 keys
+    ("prompt", dict(batch=2 ** 14, num_q_heads=1024, num_kv_heads=1, total_q=2 ** 27, max_q_len=2 ** 7, rows=2 ** 7,
+                    max_kv_len=2 ** 7, max_blocks_per_seq=8)),
+    ("prompt", dict(batch=2 ** 14, num_q_heads=1, num_kv_heads=1, max_kv_len=2 ** 17, max_blocks_per_seq=2 ** 13))])
+def test_launches_of_2_to_the_32_threads_are_refused(name, kw):
+    assert call(name, **{"workspace": FAKE, "workspace_bytes": 2 ** 62, **kw}) == BAD
+    assert "launch too large" in ops.last_error()
+
+
+def test_workspaces_of_launches_of_2_to_the_32_threads():
+    cu = 256
+    # 512 threads for every 2048 scored keys of 8192 sequences and KV heads, and one more for each of these
+    fits = 1023 * 2048 - 62
+    assert ops.decode_scores_workspace_bytes(1024, fits - 2048, fits - 2048, 32, 8, 128, cu) > 0
+    assert ops.decode_scores_workspace_bytes(1024, fits + 2048, fits + 2048, 32, 8, 128, cu) == -1
+    # 256 threads for every 128 of 2^24 rows, of 2^23 keys of 256 sequences, or one for each of 2^24 sequences
+    assert ops.prefill_scores_workspace_bytes(2 ** 14, 2 ** 26, 2 ** 7, 2 ** 7, 2 ** 7, 512, 1, cu) > 0
+    assert ops.prefill_scores_workspace_bytes(2 ** 14, 2 ** 27, 2 ** 7, 2 ** 7, 2 ** 7, 1024, 1, cu) == -1
+    assert ops.prefill_scores_workspace_bytes(256, 256, 1, 2 ** 22, 1, 1, 1, cu) > 0
+    assert ops.prefill_scores_workspace_bytes(256, 256, 1, 2 ** 23, 1, 1, 1, cu) == -1
+    assert ops.prefill_scores_workspace_bytes(2 ** 24, 2 ** 24, 1, 1, 1, 1, 1, cu) == -1
+    assert ops.prefill_scores_workspace_bytes(2 ** 30, 2 ** 30, 1, 2 ** 30, 1, 2 ** 30, 2 ** 30, cu) == -1
