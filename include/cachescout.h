@@ -573,6 +573,8 @@ int64_t cs_decode_scores_workspace_bytes(int32_t batch, int32_t max_seq_len, int
  *                  keys must belong to one invocation of the call alone, and
  *                  stand once in its table.
  *   rows           >= 1: how many of the last suffix rows count; S or more: all.
+ *                  min(rows, max_q_len) * Hq / Hkv must be below 2^28, and below 2^32
+ *                  times Hq / Hkv once more, else CS_ERR_UNSUPPORTED.
  *   decay          in [0, 1], else CS_ERR_INVALID_ARG.
  *   score_pool     as in cs_decode_attn_scores.
  *   workspace      device, 16-byte aligned, caller-owned scratch of at least

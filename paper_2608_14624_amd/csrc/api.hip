@@ -895,6 +895,12 @@ int cs_prefill_key_scores(const void* q, const void* k_pool, const int32_t* bloc
     return fail(CS_ERR_INVALID_ARG, "max_blocks_per_seq * block_size < max_kv_len");
   if (!aligned16(q) || !aligned16(k_pool) || !aligned16(score_pool))
     return fail(CS_ERR_INVALID_ARG, "q, k_pool and score_pool must be 16-byte aligned");
+  // (rows are divided by the group with a 32-bit reciprocal, and their statistics, 8 bytes each, have
+  // 31-bit offsets)
+  const long long group = num_q_heads / num_kv_heads;
+  const long long max_rows = rows < max_q_len ? rows : max_q_len;
+  if (max_rows * group > 0xfffffffLL || max_rows * group * group > 0xffffffffLL)
+    return fail(CS_ERR_UNSUPPORTED, "%lld rows of %lld query heads per KV head", max_rows, group);
   // (more compute units take no fewer work-groups)
   if (!cs::key_score_geometry(batch, total_q, max_q_len, max_kv_len, rows, num_q_heads, num_kv_heads, 1).fits)
     return fail(CS_ERR_INVALID_ARG, "launch too large");
@@ -904,10 +910,6 @@ int cs_prefill_key_scores(const void* q, const void* k_pool, const int32_t* bloc
   cs::KeyScoreLaunch a;
   a.geo = cs::key_score_geometry(batch, total_q, max_q_len, max_kv_len, rows, num_q_heads, num_kv_heads, cus);
   if (!a.geo.fits) return fail(CS_ERR_INVALID_ARG, "launch too large");
-  // (rows are divided by the group with a 32-bit reciprocal)
-  const long long group = num_q_heads / num_kv_heads;
-  if (a.geo.max_rows * group * group > 0xffffffffLL)
-    return fail(CS_ERR_UNSUPPORTED, "%d rows of %lld query heads per KV head", a.geo.max_rows, group);
   if (!workspace || !aligned16(workspace))
     return fail(CS_ERR_INVALID_ARG, "workspace must be a 16-byte aligned device buffer");
   if (workspace_bytes < a.geo.bytes)

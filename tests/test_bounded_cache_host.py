@@ -196,3 +196,12 @@ def test_workspaces_of_launches_of_2_to_the_32_threads():
     assert ops.prefill_scores_workspace_bytes(256, 256, 1, 2 ** 23, 1, 1, 1, cu) == -1
     assert ops.prefill_scores_workspace_bytes(2 ** 24, 2 ** 24, 1, 1, 1, 1, 1, cu) == -1
     assert ops.prefill_scores_workspace_bytes(2 ** 30, 2 ** 30, 1, 2 ** 30, 1, 2 ** 30, 2 ** 30, cu) == -1
+
+
+@pytest.mark.parametrize("group,rows", [(1, 2 ** 28), (2, 2 ** 27), (16, 2 ** 24), (64, 2 ** 20), (2 ** 10, 2 ** 12)])
+def test_more_rows_than_their_statistics_have_offsets_for_are_refused(group, rows):
+    kw = dict(batch=1, num_kv_heads=1, num_q_heads=group, total_q=rows, max_q_len=rows, max_kv_len=rows,
+              max_blocks_per_seq=rows // 16, workspace=FAKE, workspace_bytes=2 ** 62)
+    assert call("prompt", rows=rows, **kw) == UNSUPPORTED
+    assert f"{rows} rows of {group} query heads" in ops.last_error()
+    assert call("prompt", rows=2 ** 31 - 1, **kw) == UNSUPPORTED
