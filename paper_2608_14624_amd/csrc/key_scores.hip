@@ -85,6 +85,15 @@ __device__ __forceinline__ void pair_swap(float x, float& a, float& b) {
 // and descriptors that depend on it a loop over the lanes)
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 
+// Between two steps: the wave's loads into one buffer have landed and its reads of the other are
+// done (the products that take them need not be, and the barrier alone does not wait for reads), and
+// so are all waves'.
+__device__ __forceinline__ void buffers_ready() {
+  __builtin_amdgcn_s_waitcnt(kWaitVmcnt0);
+  __builtin_amdgcn_s_waitcnt(kWaitLgkmcnt0);
+  asm volatile("s_barrier" ::: "memory");
+}
+
 // An invocation: its observed rows are the stacked rows 0 .. n * group - 1 of a KV head;
 // row rho is head rho % group of the token at position pos0 + rho / group.
 struct Observed {
@@ -251,8 +260,7 @@ __global__ __launch_bounds__(kThreads, 4) void key_stats_kernel(ScoreParams p) {
   // in step j - 1 (rings of three and four buffers, with their loads further ahead, gain
   // nothing: 198 us with two, 200 and 206 with three and four, for work-groups fewer to a CU)
   auto run_step = [&](int j, uint16_t* cur, uint16_t* next, int& id) __attribute__((always_inline)) {
-    __builtin_amdgcn_s_waitcnt(kWaitVmcnt0);
-    asm volatile("s_barrier" ::: "memory");
+    buffers_ready();
     if (j + 1 < s1) dma(next, id);
     id = block_id(j + 2);
     compute(j, cur);
@@ -446,8 +454,7 @@ __global__ __launch_bounds__(kThreads, 4) void key_weights_kernel(ScoreParams p)
   };
   // stage t: its Q has landed; the loads of the next one go into the other buffer
   auto stage = [&](int t, uint16_t* cur, Stats& st, uint16_t* next, Stats& st_next) __attribute__((always_inline)) {
-    __builtin_amdgcn_s_waitcnt(kWaitVmcnt0);
-    asm volatile("s_barrier" ::: "memory");
+    buffers_ready();
     if (t + kTiles < tiles) {
       dma(next, t + kTiles);
       st_next = load_stats(t + kTiles);
