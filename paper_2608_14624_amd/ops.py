@@ -706,7 +706,7 @@ def cs_prefill_window_attn(q, k_pool, v_pool, block_tables, prefix_lens, cu_q_le
                                        _stream_handle(stream, dev)))
 
 
-def _decode_args(q, k_pool, v_pool, block_tables, seq_lens, out, max_seq_len):
+def _decode_args(q, k_pool, v_pool, block_tables, seq_lens, out):
     """Validate a decode call's tensors; its sizes (batch, query heads, KV heads, head_dim, blocks,
     block size, table width) and the device."""
     dev = q.device
@@ -748,7 +748,7 @@ def cs_decode_window_attn(q, k_pool, v_pool, block_tables, seq_lens, out, *, max
     :func:`cs_paged_decode_attn`; a length of 0 gives a row of zeros.  ``workspace``: "auto"
     (allocated here) or a uint8 GPU tensor of :func:`decode_window_workspace_bytes`."""
     batch, hq, hkv, d, num_blocks, bs, width, dev = _decode_args(q, k_pool, v_pool, block_tables, seq_lens,
-                                                                 out, max_seq_len)
+                                                                 out)
     max_seq_len = int(max_seq_len)
     window, sinks = _window(window, sinks, max_seq_len)
     if _current_device() != dev.index:
@@ -801,7 +801,7 @@ def cs_decode_attn_scores(q, k_pool, v_pool, block_tables, seq_lens, score_from,
     a row of zeros.  ``max_scored_len`` bounds ``seq_lens - score_from``; ``workspace``: "auto"
     (allocated here) or a uint8 GPU tensor of :func:`decode_scores_workspace_bytes`."""
     batch, hq, hkv, d, num_blocks, bs, width, dev = _decode_args(q, k_pool, v_pool, block_tables, seq_lens,
-                                                                 out, max_seq_len)
+                                                                 out)
     _require_tensors(dev, q.get_device(), ("score_from", score_from, _I32))
     _require(score_from.numel() == batch, "score_from must have B entries")
     _require_scores(score_pool, k_pool, dev)
