@@ -86,7 +86,8 @@ enum cs_status {
                                 buffer, or (debug mode) bad device metadata */
     CS_ERR_UNSUPPORTED = 2,  /* valid but not implemented: head_dim other
                                 than 64 or 128, block_size other than 16,
-                                more than 16 query heads per KV head (decode) */
+                                more than 16 query heads per KV head (decode),
+                                too many rows at once (prompt scores) */
     CS_ERR_HIP = 3           /* the HIP runtime reported an error */
 };
 
@@ -508,7 +509,9 @@ int64_t cs_decode_window_workspace_bytes(int32_t batch, int32_t max_seq_len, int
  *                 + sum over the query heads h of g of p_h(j).
  *
  * The query's own key L - 1 is new in this step, so its score starts here and
- * what its slot held before does not matter.  Scores are held in
+ * what its slot held before does not matter.  Outputs have that call's precision but
+ * not its bits: their normaliser sums the fp32 weights, and not these as rounded to
+ * bf16 for the product with V.  Scores are held in
  * score_pool[slot][g][position in the block], laid out as the pools are, so
  * they move with the blocks.  Weights and their sums are fp32.  Keys before
  * score_from[r] are attended but not scored: a shared anchor's blocks belong to

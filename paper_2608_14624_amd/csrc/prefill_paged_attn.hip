@@ -1392,9 +1392,10 @@ __global__ __launch_bounds__(kPPThreads, D == 64 ? 4 : 2) void prefill_paged_att
 // The output of a split launch with key parts: each (token, head) row
 // combines its parts' partial results with the log-sum-exp weights in base
 // 2 (the kernels' own units): w_p = 2^{(m_p - max m) c}, out = sum_p w_p O_p /
-// sum_p w_p l_p, rounded to bf16.  Part 0 holds key 0, which every row sees,
-// so the sum of weights is never empty.  D / 4 threads per row, four
-// consecutive features each.
+// sum_p w_p l_p, rounded to bf16.  Every row sees its own key, which some part
+// holds, so the sum of weights is never empty; any other part, the first among
+// them under a window, may hold no key that the row sees (m = -inf, O = 0, l = 0).
+// D / 4 threads per row, four consecutive features each.
 // The loads of kStep parts (2, 4 or 8: the fewest that hold the launch's
 // parts, so that few are read twice) are in flight together, where a loop over
 // single parts waited for each in turn: calls with 4 to 8 parts 23.1 -> 20.9 us
