@@ -533,7 +533,8 @@ int64_t cs_decode_window_workspace_bytes(int32_t batch, int32_t max_seq_len, int
  *   workspace_bytes  sized by cs_decode_scores_workspace_bytes: the logits of the
  *                  scored keys are kept there until the row's softmax is known.
  * Both bounds choose the launch and size its LDS: tight ones are faster, by up to
- * 40% for many short sequences.
+ * 40% for many short sequences.  Past 1024 sequences one work-group takes a sequence and
+ * KV head whatever its length, so the longest sets the time (about 12 ns a key).
  */
 int cs_decode_attn_scores(const void *q, const void *k_pool, const void *v_pool,
                           const int32_t *block_tables, const int32_t *seq_lens,

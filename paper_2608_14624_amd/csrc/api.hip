@@ -371,7 +371,8 @@ int64_t scored_units(int32_t max_scored_len) {
 // work-group per (sequence, KV head), which keeps the logits on the CU.  The latter
 //   * from one pair per compute unit on;
 //   * up to kPairKeys keys in the longest sequence for every pair of a compute unit: a pair is
-//     one work-group's however long, at about 12 ns a key, while ranges share a long sequence out;
+//     one work-group's however long, at about 12 ns a key, while ranges share a long sequence out
+//     (past the 1024 sequences that ranges take, whatever the longest);
 //   * unless more than a quarter of the keys may be a shared prefix, which ranges read once.  (How
 //     much it takes for them to win depends on how many share it, and a quarter is on the safe
 //     side: 128 sequences of up to 8000 keys, 8 agents with 2000 shared 500 and 612, with 4800 436 and
