@@ -35,6 +35,12 @@
  *   cs_kv_evict            - the attention weight that every cached key has
  *                            received, added up per key, and the eviction of
  *                            a sequence's least attended keys.
+ *   cs_kv_write_quant,
+ *   cs_kv_quantize,
+ *   cs_kv_dequantize       - a KV pool in 4 or 8 bits: new tokens written into
+ *                            it, blocks of a bf16 pool moved to it and back.
+ *   cs_decode_quant_attn,
+ *   cs_prefill_quant_attn  - both kinds of attention over such a pool.
  *
  * Conventions shared by all calls
  *   - Every pointer is caller-owned.  The GPU calls allocate no device or
@@ -86,6 +92,7 @@ enum cs_status {
                                 buffer, or (debug mode) bad device metadata */
     CS_ERR_UNSUPPORTED = 2,  /* valid but not implemented: head_dim other
                                 than 64 or 128, block_size other than 16,
+                                bits other than 4 or 8,
                                 more than 16 query heads per KV head (decode),
                                 too many rows at once (prompt scores) */
     CS_ERR_HIP = 3           /* the HIP runtime reported an error */
@@ -700,6 +707,135 @@ int cs_kv_offload(const int32_t *src_block_ids, int32_t n, const void *k_pool,
                   const void *v_pool, int32_t num_blocks, void *host_k_blocks,
                   void *host_v_blocks, int32_t num_kv_heads, int32_t head_dim,
                   int32_t block_size, cs_stream_t stream);
+
+/* ------------------------------------------------------------------------
+ * A KV pool in 4 or 8 bits (not in the paper, which keeps every block in the model's type: a
+ * block that is read many times and written once is worth fewer bits, and at 4 a pool holds
+ * 3.8 times the tokens).
+ *
+ * Format.  The 32 features 32 i .. 32 i + 31 of a K or V row share a scale 2^e; each is held as
+ * the nearest number (ties to even) of x / 2^e among
+ *   bits 4   +-{0, .5, 1, 1.5, 2, 3, 4, 6}          (E2M1)
+ *   bits 8   E4M3: +-m 2^k with 4-bit m, up to 448, subnormals included,
+ * e being the smallest exponent for which the largest magnitude of the 32 does not round beyond
+ * 6 or 448, but at least -125 (4 bits) or -117 (8 bits), where smaller rows lose bits, and at
+ * most 125 or 119, where larger numbers become the largest.  What is held, a number times 2^e,
+ * is exact in bf16.  A group with a NaN or an infinity is NaN as a whole.
+ *
+ * A quantised pool is [num_blocks][num_kv_heads][cs_kv_quant_tile_bytes(head_dim, bits)] bytes,
+ * 16-byte aligned; the tile of a (block, KV head) holds 16 tokens, K and V:
+ *   K codes   [16 tokens][head_dim]
+ *   V codes   [16][16 tokens][head_dim / 16]: feature f of token t at [f / (head_dim / 16)][t]
+ *             [f % (head_dim / 16)]
+ *   K scales  [16 tokens][head_dim / 32], V scales [head_dim / 32][16 tokens]: a byte e + 127
+ *             each, or 255 for NaN
+ * with two codes in a byte at 4 bits, the lower feature in the low half.  Blocks may be copied as
+ * bytes.  The calls take the same block ids, tables and slots as those on bf16 pools.
+ * ------------------------------------------------------------------------ */
+
+/* Bytes of a (block, KV head) tile: head_dim * bits * 4 + head_dim (2176 at 128 and 4 bits); -1 for
+ * a head_dim other than 64 or 128 or bits other than 4 or 8. */
+int64_t cs_kv_quant_tile_bytes(int32_t head_dim, int32_t bits);
+
+/*
+ * KV write-back into a quantised pool: cs_kv_write, the rows quantised as they are stored.
+ * Tokens with a negative slot are skipped; nothing else in the pool changes.
+ *
+ * Arguments as in cs_kv_write, except
+ *   quant_pool     device, as above.
+ *   bits           4 or 8.
+ */
+int cs_kv_write_quant(const void *k_new, const void *v_new, const int32_t *slot_mapping,
+                      int32_t num_tokens, void *quant_pool, int32_t num_blocks,
+                      int32_t num_kv_heads, int32_t head_dim, int32_t block_size, int32_t bits,
+                      cs_stream_t stream);
+
+/*
+ * Blocks of a bf16 pool into a quantised pool, e.g. an agent's anchor that goes cold: block
+ * src_block_ids[i] of k_pool and v_pool becomes block dst_block_ids[i] of quant_pool, for every
+ * i < n.
+ *
+ * Arguments
+ *   k_pool, v_pool device, bf16 [num_blocks][num_kv_heads][block_size][head_dim], 16-byte aligned.
+ *   src_block_ids  device, int32 [n], each in [0, num_blocks); repeats allowed.
+ *   dst_block_ids  device, int32 [n], distinct, each in [0, num_quant_blocks).
+ *   n              at most num_quant_blocks; 0 is a no-op returning CS_OK.
+ *   quant_pool     device, as above, of num_quant_blocks blocks.
+ * What a block holds behind its sequence's last token is quantised as well (each token by
+ * itself, so it changes no other).
+ */
+int cs_kv_quantize(const void *k_pool, const void *v_pool, const int32_t *src_block_ids,
+                   const int32_t *dst_block_ids, int32_t n, void *quant_pool, int32_t num_blocks,
+                   int32_t num_quant_blocks, int32_t num_kv_heads, int32_t head_dim,
+                   int32_t block_size, int32_t bits, cs_stream_t stream);
+
+/*
+ * The way back, e.g. the predicted agent's anchor on a side stream: block src_block_ids[i] of
+ * quant_pool becomes block dst_block_ids[i] of k_pool and v_pool, exactly the values it holds.
+ *
+ * Arguments as in cs_kv_quantize, except that src_block_ids (repeats allowed) name blocks of
+ * quant_pool, dst_block_ids (distinct) of the bf16 pools, and n <= num_blocks.
+ */
+int cs_kv_dequantize(const void *quant_pool, const int32_t *src_block_ids,
+                     const int32_t *dst_block_ids, int32_t n, void *k_pool, void *v_pool,
+                     int32_t num_blocks, int32_t num_quant_blocks, int32_t num_kv_heads,
+                     int32_t head_dim, int32_t block_size, int32_t bits, cs_stream_t stream);
+
+/*
+ * Decode attention over a quantised pool: cs_paged_decode_attn_ws with K and V the values that
+ * quant_pool holds.  The token's own K/V must already be there (cs_kv_write_quant).
+ *
+ * Arithmetic: fp32 logits, of bf16 products, or at 4 bits of the query's products with the codes:
+ * a query feature is there held as two 8-bit numbers, exact unless it is more than 2^14 times
+ * smaller than the largest of its group of 32, and then off by at most 2^-22 of that one.  (Query
+ * features from 1.8125 * 2^127 on count as infinite.)  Probabilities are rounded to bf16 for the
+ * product with V, the output to nearest-even bf16.  A row's low bits may change with the rest of
+ * the batch, as there; the result is the same from run to run.
+ *
+ * Arguments as in cs_paged_decode_attn_ws, except
+ *   quant_pool     device, as above, of num_blocks blocks of `bits` (4 or 8) bits.
+ *   seq_lens       each in [0, max_seq_len]; a row with length 0 (a batch padded to a captured
+ *                  size) gets zeros, and its block table is not read.
+ *   out            16-byte aligned.
+ *   workspace,
+ *   workspace_bytes  sized by cs_decode_quant_workspace_bytes.
+ * Batches of any size share the device; what a pool holds behind a sequence's end is not used.
+ */
+int cs_decode_quant_attn(const void *q, const void *quant_pool, const int32_t *block_tables,
+                         const int32_t *seq_lens, int32_t batch, int32_t max_seq_len,
+                         int32_t max_blocks_per_seq, int32_t num_blocks, int32_t num_q_heads,
+                         int32_t num_kv_heads, int32_t head_dim, int32_t block_size, int32_t bits,
+                         float scale, void *workspace, int64_t workspace_bytes, void *out,
+                         cs_stream_t stream);
+
+/* Workspace bytes cs_decode_quant_attn needs.  num_cus: compute units to size for, 0 = the current
+ * device's (-1 if there is none).  -1 for a negative size, bad head counts, a head_dim other than
+ * 64 or 128, or a launch too large. */
+int64_t cs_decode_quant_workspace_bytes(int32_t batch, int32_t max_seq_len, int32_t num_q_heads,
+                                        int32_t num_kv_heads, int32_t head_dim, int32_t num_cus);
+
+/*
+ * Prefill attention over a quantised pool: cs_prefill_paged_attn with K and V, of the prefix and
+ * of the suffix itself, the values that quant_pool holds; arithmetic as in cs_decode_quant_attn.
+ *
+ * Arguments as in cs_prefill_paged_attn, except
+ *   quant_pool     device, as above, of num_blocks blocks of `bits` (4 or 8) bits.
+ *   workspace,
+ *   workspace_bytes  sized by cs_prefill_quant_workspace_bytes (launches too small for the device
+ *                  take their keys in parts); may be NULL and 0 when that is 0.
+ */
+int cs_prefill_quant_attn(const void *q, const void *quant_pool, const int32_t *block_tables,
+                          const int32_t *prefix_lens, const int32_t *cu_q_lens, int32_t batch,
+                          int32_t total_q, int32_t max_q_len, int32_t max_kv_len,
+                          int32_t max_blocks_per_seq, int32_t num_blocks, int32_t num_q_heads,
+                          int32_t num_kv_heads, int32_t head_dim, int32_t block_size, int32_t bits,
+                          float scale, void *workspace, int64_t workspace_bytes, void *out,
+                          cs_stream_t stream);
+
+/* Workspace bytes cs_prefill_quant_attn needs; num_cus and -1 as above. */
+int64_t cs_prefill_quant_workspace_bytes(int32_t batch, int32_t total_q, int32_t max_q_len,
+                                         int32_t max_kv_len, int32_t num_q_heads,
+                                         int32_t num_kv_heads, int32_t head_dim, int32_t num_cus);
 
 /* ------------------------------------------------------------------------
  * Control plane (host only): the agent-transition learner, the survival

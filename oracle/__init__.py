@@ -45,6 +45,10 @@ paper; ``bounded_cache.py`` evaluates their definitions in float64, pinned to
 the attention oracle and to scalar loops, with planted mistakes
 (``tests/test_bounded_cache_oracle.py``).
 
+A KV pool held in 4 or 8 bits (outside the paper too): ``quant_cache.py`` evaluates the
+format's definition in float64, pinned to exact rational arithmetic and to the layout
+element by element, with planted mistakes (``tests/test_quant_cache_oracle.py``).
+
 Every function here is pinned; none is "parity unpinned".  The full
 attention oracle is pinned by the brute force, the invariants, the closed
 forms and the golden case (``tests/test_oracle_*.py``); the row-by-row
@@ -70,4 +74,12 @@ from .bounded_cache import (  # noqa: F401
     evict,
     window_attention,
     window_weights,
+)
+from .quant_cache import (  # noqa: F401
+    pack_tiles,
+    quantise_rows,
+    row_values,
+    split_tiles,
+    to_bf16_bits,
+    unpack_tiles,
 )

@@ -148,13 +148,19 @@ int debug_check_slots(const int32_t* slots, int n, long long num_slots, hipStrea
   return CS_OK;
 }
 
-int debug_check_block_ids(const int32_t* ids_d, int n, int num_blocks, hipStream_t stream) {
+int debug_check_block_ids(const int32_t* ids_d, int n, int num_blocks, hipStream_t stream,
+                          const char* name = "src_block_ids", bool distinct = false) {
   std::vector<int32_t> ids;
   hipError_t e = copy_to_host(ids, ids_d, (size_t)n, stream);
   if (e != hipSuccess) return hip_fail(e, "CS_DEBUG_CHECK metadata copy");
-  for (int i = 0; i < n; ++i)
+  std::vector<unsigned char> seen(distinct ? (size_t)num_blocks : 0, 0);
+  for (int i = 0; i < n; ++i) {
     if (ids[i] < 0 || ids[i] >= num_blocks)
-      return fail(CS_ERR_INVALID_ARG, "src_block_ids[%d] = %d outside [0, %d)", i, ids[i], num_blocks);
+      return fail(CS_ERR_INVALID_ARG, "%s[%d] = %d outside [0, %d)", name, i, ids[i], num_blocks);
+    if (!distinct) continue;
+    if (seen[ids[i]]) return fail(CS_ERR_INVALID_ARG, "%s[%d] = %d is a duplicate", name, i, ids[i]);
+    seen[ids[i]] = 1;
+  }
   return CS_OK;
 }
 
@@ -729,6 +735,76 @@ int cascade_decode(const void* q, const void* k_pool, const void* v_pool,
 
 }  // namespace
 
+
+namespace {
+
+// Arguments shared by the calls on a quantised pool
+int validate_quant(int32_t num_blocks, int32_t num_kv_heads, int32_t head_dim, int32_t block_size, int32_t bits) {
+  if (num_blocks < 0) return fail(CS_ERR_INVALID_ARG, "negative size argument");
+  if (num_kv_heads <= 0 || head_dim <= 0 || block_size <= 0)
+    return fail(CS_ERR_INVALID_ARG, "num_kv_heads, head_dim and block_size must be positive");
+  if (head_dim != 64 && head_dim != 128)
+    return fail(CS_ERR_UNSUPPORTED, "head_dim %d (supported: 64, 128)", head_dim);
+  if (block_size != 16) return fail(CS_ERR_UNSUPPORTED, "block_size %d (supported: 16)", block_size);
+  if (bits != 4 && bits != 8) return fail(CS_ERR_UNSUPPORTED, "bits %d (supported: 4, 8)", bits);
+  return CS_OK;
+}
+
+// cs_kv_quantize and cs_kv_dequantize: whole blocks between a bf16 pool and a quantised one
+int quant_blocks(const void* k_pool, const void* v_pool, void* k_out, void* v_out, const int32_t* ids,
+                 const char* ids_name, const int32_t* pool_ids, const char* pool_ids_name, int32_t n,
+                 void* quant_pool, int32_t num_blocks, int32_t num_quant_blocks, int32_t num_kv_heads,
+                 int32_t head_dim, int32_t block_size, int32_t bits, bool write, cs_stream_t stream) {
+  if (n < 0 || num_quant_blocks < 0) return fail(CS_ERR_INVALID_ARG, "negative size argument");
+  int st = validate_quant(num_blocks, num_kv_heads, head_dim, block_size, bits);
+  if (st != CS_OK) return st;
+  if (n == 0) return ok();
+  const void* k = write ? k_pool : k_out;
+  const void* v = write ? v_pool : v_out;
+  if (!k || !v || !ids || !pool_ids || !quant_pool) return fail(CS_ERR_INVALID_ARG, "null pointer argument");
+  if (num_blocks == 0 || num_quant_blocks == 0) return fail(CS_ERR_INVALID_ARG, "a pool has no blocks");
+  if (n > (write ? num_quant_blocks : num_blocks))
+    return fail(CS_ERR_INVALID_ARG, "n = %d exceeds the %d blocks that are written to", n,
+                write ? num_quant_blocks : num_blocks);
+  if (!aligned16(k) || !aligned16(v) || !aligned16(quant_pool))
+    return fail(CS_ERR_INVALID_ARG, "the pools must be 16-byte aligned");
+  if (!cs::quant_copy_fits(n, num_kv_heads, false)) return fail(CS_ERR_INVALID_ARG, "launch too large");
+  hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+  if (debug_checks_enabled()) {
+    st = debug_check_block_ids(ids, n, num_blocks, s, ids_name, !write);
+    if (st == CS_OK) st = debug_check_block_ids(pool_ids, n, num_quant_blocks, s, pool_ids_name, write);
+    if (st != CS_OK) return st;
+  }
+  cs::QuantCopyLaunch a = {};
+  a.k = static_cast<const uint16_t*>(k_pool);
+  a.v = static_cast<const uint16_t*>(v_pool);
+  a.k_out = static_cast<uint16_t*>(k_out);
+  a.v_out = static_cast<uint16_t*>(v_out);
+  a.pool = static_cast<uint8_t*>(quant_pool);
+  a.ids = ids;
+  a.pool_ids = pool_ids;
+  a.n = n;
+  a.num_kv_heads = num_kv_heads;
+  a.head_dim = head_dim;
+  a.bits = bits;
+  hipError_t e = write ? cs::launch_kv_quantize(a, s) : cs::launch_kv_dequantize(a, s);
+  if (e != hipSuccess) return hip_fail(e, write ? "kv_quantize launch" : "kv_dequantize launch");
+  return ok();
+}
+
+// The caller's workspace, where a launch needs `need` bytes of one
+int check_workspace(const void* workspace, int64_t workspace_bytes, int64_t need) {
+  if (need == 0) return CS_OK;
+  if (!workspace || !aligned16(workspace))
+    return fail(CS_ERR_INVALID_ARG, "workspace must be a 16-byte aligned device buffer");
+  if (workspace_bytes < need)
+    return fail(CS_ERR_INVALID_ARG, "workspace_bytes %lld < %lld required", (long long)workspace_bytes,
+                (long long)need);
+  return CS_OK;
+}
+
+}  // namespace
+
 // the C ABI is the only thing the library exports (built with -fvisibility=hidden)
 #pragma GCC visibility push(default)
 extern "C" {
@@ -1229,6 +1305,196 @@ int cs_kv_offload(const int32_t* src_block_ids, int32_t n, const void* k_pool, c
   hipError_t e = cs::launch_kv_offload(a, s);
   if (e != hipSuccess) return hip_fail(e, "kv_offload launch");
   return ok();
+}
+
+int64_t cs_kv_quant_tile_bytes(int32_t head_dim, int32_t bits) {
+  if ((head_dim != 64 && head_dim != 128) || (bits != 4 && bits != 8)) return -1;
+  return cs::quant_tile_bytes(head_dim, bits);
+}
+
+int cs_kv_write_quant(const void* k_new, const void* v_new, const int32_t* slot_mapping, int32_t num_tokens,
+                      void* quant_pool, int32_t num_blocks, int32_t num_kv_heads, int32_t head_dim,
+                      int32_t block_size, int32_t bits, cs_stream_t stream) {
+  if (num_tokens < 0) return fail(CS_ERR_INVALID_ARG, "negative size argument");
+  int st = validate_quant(num_blocks, num_kv_heads, head_dim, block_size, bits);
+  if (st != CS_OK) return st;
+  if (num_tokens == 0) return ok();
+  if (!k_new || !v_new || !slot_mapping || !quant_pool) return fail(CS_ERR_INVALID_ARG, "null pointer argument");
+  if (num_blocks == 0) return fail(CS_ERR_INVALID_ARG, "num_blocks is 0");
+  if (!aligned16(k_new) || !aligned16(v_new) || !aligned16(quant_pool))
+    return fail(CS_ERR_INVALID_ARG, "k_new, v_new and the pool must be 16-byte aligned");
+  if (!cs::quant_copy_fits(num_tokens, num_kv_heads, true)) return fail(CS_ERR_INVALID_ARG, "launch too large");
+  hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+  if (debug_checks_enabled()) {
+    st = debug_check_slots(slot_mapping, num_tokens, (long long)num_blocks * block_size, s);
+    if (st != CS_OK) return st;
+  }
+  cs::QuantCopyLaunch a = {};
+  a.k = static_cast<const uint16_t*>(k_new);
+  a.v = static_cast<const uint16_t*>(v_new);
+  a.pool = static_cast<uint8_t*>(quant_pool);
+  a.ids = slot_mapping;
+  a.n = num_tokens;
+  a.num_kv_heads = num_kv_heads;
+  a.head_dim = head_dim;
+  a.bits = bits;
+  hipError_t e = cs::launch_kv_write_quant(a, s);
+  if (e != hipSuccess) return hip_fail(e, "kv_write_quant launch");
+  return ok();
+}
+
+int cs_kv_quantize(const void* k_pool, const void* v_pool, const int32_t* src_block_ids,
+                   const int32_t* dst_block_ids, int32_t n, void* quant_pool, int32_t num_blocks,
+                   int32_t num_quant_blocks, int32_t num_kv_heads, int32_t head_dim, int32_t block_size,
+                   int32_t bits, cs_stream_t stream) {
+  return quant_blocks(k_pool, v_pool, nullptr, nullptr, src_block_ids, "src_block_ids", dst_block_ids,
+                      "dst_block_ids", n, quant_pool, num_blocks, num_quant_blocks, num_kv_heads, head_dim,
+                      block_size, bits, true, stream);
+}
+
+int cs_kv_dequantize(const void* quant_pool, const int32_t* src_block_ids, const int32_t* dst_block_ids,
+                     int32_t n, void* k_pool, void* v_pool, int32_t num_blocks, int32_t num_quant_blocks,
+                     int32_t num_kv_heads, int32_t head_dim, int32_t block_size, int32_t bits,
+                     cs_stream_t stream) {
+  return quant_blocks(nullptr, nullptr, k_pool, v_pool, dst_block_ids, "dst_block_ids", src_block_ids,
+                      "src_block_ids", n, const_cast<void*>(quant_pool), num_blocks, num_quant_blocks,
+                      num_kv_heads, head_dim, block_size, bits, false, stream);
+}
+
+int cs_decode_quant_attn(const void* q, const void* quant_pool, const int32_t* block_tables,
+                         const int32_t* seq_lens, int32_t batch, int32_t max_seq_len,
+                         int32_t max_blocks_per_seq, int32_t num_blocks, int32_t num_q_heads,
+                         int32_t num_kv_heads, int32_t head_dim, int32_t block_size, int32_t bits,
+                         float scale, void* workspace, int64_t workspace_bytes, void* out,
+                         cs_stream_t stream) {
+  if (bits != 4 && bits != 8) return fail(CS_ERR_UNSUPPORTED, "bits %d (supported: 4, 8)", bits);
+  bool noop;
+  int st = validate_decode(q, quant_pool, quant_pool, block_tables, seq_lens, batch, max_seq_len,
+                           max_blocks_per_seq, num_blocks, num_q_heads, num_kv_heads, head_dim, block_size,
+                           scale, out, &noop);
+  if (st != CS_OK) return st;
+  if (workspace_bytes < 0) return fail(CS_ERR_INVALID_ARG, "negative workspace_bytes");
+  if (noop) return ok();
+  if (!aligned16(out)) return fail(CS_ERR_INVALID_ARG, "out must be 16-byte aligned");
+  int cus = 0;
+  hipError_t e = cs::current_device_cus(&cus);
+  if (e != hipSuccess) return hip_fail(e, "compute-unit count of the current device");
+  const cs::QuantDecodeGeometry geo =
+      cs::quant_decode_geometry(batch, max_seq_len, num_q_heads, num_kv_heads, head_dim, cus);
+  if (!geo.fits) return fail(CS_ERR_INVALID_ARG, "launch too large");
+  st = check_workspace(workspace, workspace_bytes, geo.bytes);
+  if (st != CS_OK) return st;
+  hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+  if (debug_checks_enabled()) {
+    st = debug_check_decode(block_tables, seq_lens, batch, max_seq_len, max_blocks_per_seq, num_blocks, 0, {}, s);
+    if (st != CS_OK) return st;
+  }
+  cs::QuantAttnLaunch a = {};
+  a.q = static_cast<const uint16_t*>(q);
+  a.pool = static_cast<const uint8_t*>(quant_pool);
+  a.block_tables = block_tables;
+  a.lens = seq_lens;
+  a.out = static_cast<uint16_t*>(out);
+  a.batch = batch;
+  a.max_blocks_per_seq = max_blocks_per_seq;
+  a.num_q_heads = num_q_heads;
+  a.num_kv_heads = num_kv_heads;
+  a.head_dim = head_dim;
+  a.bits = bits;
+  a.scale = scale;
+  a.workspace = static_cast<float*>(workspace);
+  e = cs::launch_quant_decode(a, geo, s);
+  if (e != hipSuccess) return hip_fail(e, "decode_quant_attn launch");
+  return ok();
+}
+
+int64_t cs_decode_quant_workspace_bytes(int32_t batch, int32_t max_seq_len, int32_t num_q_heads,
+                                        int32_t num_kv_heads, int32_t head_dim, int32_t num_cus) {
+  if (batch < 0 || max_seq_len < 0 || num_cus < 0 || num_q_heads <= 0 || num_kv_heads <= 0 ||
+      num_q_heads % num_kv_heads != 0 || (head_dim != 64 && head_dim != 128))
+    return -1;
+  if (batch == 0 || max_seq_len == 0) return 0;
+  int cus = num_cus;
+  if (cus == 0 && cs::current_device_cus(&cus) != hipSuccess) return -1;
+  const cs::QuantDecodeGeometry geo =
+      cs::quant_decode_geometry(batch, max_seq_len, num_q_heads, num_kv_heads, head_dim, cus);
+  return geo.fits ? geo.bytes : -1;
+}
+
+int cs_prefill_quant_attn(const void* q, const void* quant_pool, const int32_t* block_tables,
+                          const int32_t* prefix_lens, const int32_t* cu_q_lens, int32_t batch,
+                          int32_t total_q, int32_t max_q_len, int32_t max_kv_len,
+                          int32_t max_blocks_per_seq, int32_t num_blocks, int32_t num_q_heads,
+                          int32_t num_kv_heads, int32_t head_dim, int32_t block_size, int32_t bits,
+                          float scale, void* workspace, int64_t workspace_bytes, void* out,
+                          cs_stream_t stream) {
+  if (batch < 0 || total_q < 0 || max_q_len < 0 || max_kv_len < 0 || max_blocks_per_seq < 0)
+    return fail(CS_ERR_INVALID_ARG, "negative size argument");
+  int st = validate_quant(num_blocks, num_kv_heads, head_dim, block_size, bits);
+  if (st != CS_OK) return st;
+  if (num_q_heads <= 0 || num_q_heads % num_kv_heads != 0)
+    return fail(CS_ERR_INVALID_ARG, "num_q_heads %d is not a positive multiple of num_kv_heads %d", num_q_heads,
+                num_kv_heads);
+  if (!isfinite(scale)) return fail(CS_ERR_INVALID_ARG, "scale is not finite");
+  if (!(scale > 0.f)) return fail(CS_ERR_UNSUPPORTED, "scale %g (supported: > 0)", (double)scale);
+  if (workspace_bytes < 0) return fail(CS_ERR_INVALID_ARG, "negative workspace_bytes");
+  if (batch == 0 || total_q == 0 || max_q_len == 0) return ok();
+  if (!q || !quant_pool || !block_tables || !prefix_lens || !cu_q_lens || !out)
+    return fail(CS_ERR_INVALID_ARG, "null pointer argument");
+  if (num_blocks == 0) return fail(CS_ERR_INVALID_ARG, "num_blocks is 0");
+  if (max_q_len > max_kv_len) return fail(CS_ERR_INVALID_ARG, "max_q_len exceeds max_kv_len");
+  if ((long long)max_blocks_per_seq * block_size < max_kv_len)
+    return fail(CS_ERR_INVALID_ARG, "max_blocks_per_seq * block_size < max_kv_len");
+  if (!aligned16(q) || !aligned16(quant_pool) || !aligned16(out))
+    return fail(CS_ERR_INVALID_ARG, "q, quant_pool and out must be 16-byte aligned");
+  int cus = 0;
+  hipError_t e = cs::current_device_cus(&cus);
+  if (e != hipSuccess) return hip_fail(e, "compute-unit count of the current device");
+  const cs::QuantPrefillGeometry geo = cs::quant_prefill_geometry(batch, total_q, max_q_len, max_kv_len, num_q_heads,
+                                                                  num_kv_heads, head_dim, cus);
+  if (!geo.fits) return fail(CS_ERR_INVALID_ARG, "launch too large");
+  st = check_workspace(workspace, workspace_bytes, geo.bytes);
+  if (st != CS_OK) return st;
+  hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+  if (debug_checks_enabled()) {
+    st = debug_check_attn(block_tables, prefix_lens, cu_q_lens, batch, total_q, max_q_len, max_kv_len,
+                          max_blocks_per_seq, num_blocks, {}, s);
+    if (st != CS_OK) return st;
+  }
+  cs::QuantAttnLaunch a = {};
+  a.q = static_cast<const uint16_t*>(q);
+  a.pool = static_cast<const uint8_t*>(quant_pool);
+  a.block_tables = block_tables;
+  a.lens = prefix_lens;
+  a.cu_q_lens = cu_q_lens;
+  a.out = static_cast<uint16_t*>(out);
+  a.batch = batch;
+  a.total_q = total_q;
+  a.max_q_len = max_q_len;
+  a.max_blocks_per_seq = max_blocks_per_seq;
+  a.num_q_heads = num_q_heads;
+  a.num_kv_heads = num_kv_heads;
+  a.head_dim = head_dim;
+  a.bits = bits;
+  a.scale = scale;
+  a.workspace = geo.bytes > 0 ? static_cast<float*>(workspace) : nullptr;
+  e = cs::launch_quant_prefill(a, geo, s);
+  if (e != hipSuccess) return hip_fail(e, "prefill_quant_attn launch");
+  return ok();
+}
+
+int64_t cs_prefill_quant_workspace_bytes(int32_t batch, int32_t total_q, int32_t max_q_len,
+                                         int32_t max_kv_len, int32_t num_q_heads, int32_t num_kv_heads,
+                                         int32_t head_dim, int32_t num_cus) {
+  if (batch < 0 || total_q < 0 || max_q_len < 0 || max_kv_len < 0 || num_cus < 0 || num_q_heads <= 0 ||
+      num_kv_heads <= 0 || num_q_heads % num_kv_heads != 0 || (head_dim != 64 && head_dim != 128))
+    return -1;
+  if (batch == 0 || total_q == 0 || max_q_len == 0) return 0;
+  int cus = num_cus;
+  if (cus == 0 && cs::current_device_cus(&cus) != hipSuccess) return -1;
+  const cs::QuantPrefillGeometry geo = cs::quant_prefill_geometry(batch, total_q, max_q_len, max_kv_len, num_q_heads,
+                                                                  num_kv_heads, head_dim, cus);
+  return geo.fits ? geo.bytes : -1;
 }
 
 }  // extern "C"

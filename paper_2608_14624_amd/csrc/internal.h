@@ -226,6 +226,70 @@ hipError_t launch_kv_evict(const EvictLaunch& a, hipStream_t stream);
 // whether its launches fit; moving: into other blocks
 bool evict_fits(int batch, int num_kv_heads, int head_dim, int budget, bool moving);
 
+// A KV pool held in 4 or 8 bits (kv_quant.hip, quant_attn.hip; the tile: quant_tile.h).
+long long quant_tile_bytes(int head_dim, int bits);
+
+struct QuantCopyLaunch {
+  const uint16_t* k;        // new tokens [n][num_kv_heads][head_dim], or the bf16 pools
+  const uint16_t* v;
+  uint16_t* k_out;          // the bf16 pools that blocks are read back into
+  uint16_t* v_out;
+  uint8_t* pool;            // [num_blocks][num_kv_heads][quant_tile_bytes]
+  const int32_t* ids;       // the tokens' slots, or the blocks' places in the bf16 pools
+  const int32_t* pool_ids;  // the blocks' places in the quantised pool
+  int n;
+  int num_kv_heads;
+  int head_dim;
+  int bits;
+};
+bool quant_copy_fits(long long n, int num_kv_heads, bool tokens);
+hipError_t launch_kv_write_quant(const QuantCopyLaunch& a, hipStream_t stream);
+hipError_t launch_kv_quantize(const QuantCopyLaunch& a, hipStream_t stream);
+hipError_t launch_kv_dequantize(const QuantCopyLaunch& a, hipStream_t stream);
+
+struct QuantAttnLaunch {
+  const uint16_t* q;            // [total_q][num_q_heads][head_dim]
+  const uint8_t* pool;
+  const int32_t* block_tables;
+  const int32_t* lens;          // decode: sequence lengths; prefill: prefix lengths
+  const int32_t* cu_q_lens;     // prefill only
+  uint16_t* out;
+  int batch;
+  int total_q;
+  int max_q_len;
+  int max_blocks_per_seq;
+  int num_q_heads;
+  int num_kv_heads;
+  int head_dim;
+  int bits;
+  float scale;
+  float* workspace;
+};
+
+// Decode: the batch's keys, in units of 32, dealt in equal contiguous ranges to `ranges`
+// work-groups per KV head.  rows: partial results per query head in the workspace.
+struct QuantDecodeGeometry {
+  int ranges;
+  long long rows;
+  long long bytes;
+  bool fits;
+};
+QuantDecodeGeometry quant_decode_geometry(int batch, int max_seq_len, int num_q_heads, int num_kv_heads,
+                                          int head_dim, int cus);
+hipError_t launch_quant_decode(const QuantAttnLaunch& a, const QuantDecodeGeometry& geo, hipStream_t stream);
+
+// Prefill: tiles of query rows, each in `parts` parts of its keys where there are few.
+struct QuantPrefillGeometry {
+  int parts;
+  long long tiles;              // of the longest suffix, per (invocation, KV head)
+  long long grid;
+  long long bytes;
+  bool fits;
+};
+QuantPrefillGeometry quant_prefill_geometry(int batch, int total_q, int max_q_len, int max_kv_len,
+                                            int num_q_heads, int num_kv_heads, int head_dim, int cus);
+hipError_t launch_quant_prefill(const QuantAttnLaunch& a, const QuantPrefillGeometry& geo, hipStream_t stream);
+
 // Cascade decode: the shared prefix of each group of sequences is attended
 // once with the group's queries stacked (shared_prefix_partials_kernel), in
 // chunks of kCascadeChunkSteps * 64 keys whose partial results go to a

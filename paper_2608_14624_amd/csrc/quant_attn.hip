@@ -1,0 +1,791 @@
+// Attention over a KV pool held in 4 or 8 bits, for gfx950: decode (one token per sequence) and
+// prefill (suffix rows over a prefix and their own keys).
+//
+//   out = sum_j softmax_j(scale * q . K_j) V_j,   K, V the values of the pool's codes
+//
+// Both kernels are made of waves that need nothing of each other in the loop: a wave takes 16
+// or 32 query rows (token, query head of the KV head) and a run of keys, 32 at a time, and no
+// LDS.  With S^T = K Q^T and O^T = V^T P^T on 16 x 16 tiles, S^T leaves the matrix unit in the very
+// registers that P^T enters it from (a lane's keys 4q .. 4q + 3 of the two blocks), and the
+// tile's layout (quant_tile.h) gives K and V to the lanes that need them.
+//   * 4 bits: K goes into the matrix unit as it is (v_mfma_scale_f32_16x16x128_f8f6f4, codes and
+//     scales from the pool).  Its partner then has to be of 8 bits or fewer: Q is the sum of two
+//     E4M3 numbers with scales of their own, which holds bf16's 8 bits (a 4-bit head and what
+//     is left, of 4 bits again); features more than 2^14 below the largest of their group of
+//     32 are off by 2^-22 of that largest at most.  At D = 64 the two halves of the contracted
+//     index hold the head and the rest, so it is one product.
+//   * 8 bits: K is converted to bf16.  (8-bit times 8-bit products sum up with errors of 3e-5 of
+//     the largest, where 4-bit times 8-bit ones are exact to fp32's 5e-8.)
+//   * V is converted to bf16, two features of a key at a time, which two byte permutes then
+//     pair up by keys.
+// The running maximum that the exponentials are relative to follows the logits only when one is
+// above it by 2^8: P is then up to 256, which bf16 holds as well as 1, and most steps rescale
+// nothing and exchange nothing between lanes.
+#include "decode_common.h"
+#include "internal.h"
+#include "quant_tile.h"
+
+#include <math.h>
+
+namespace cs {
+namespace {
+
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
+typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
+
+constexpr int kWaves = 4;             // of a work-group, both kernels
+constexpr int kThreads = 64 * kWaves;
+constexpr float kLazy = 8.f;          // log2 of what a logit's weight may exceed 1 by
+
+struct QuantParams {
+  const uint16_t* q;
+  const uint8_t* pool;
+  const int32_t* block_tables;
+  const int32_t* lens;
+  const int32_t* cu_q_lens;
+  uint16_t* out;
+  int batch;
+  int max_blocks_per_seq;
+  int num_q_heads;
+  int num_kv_heads;
+  int group;
+  float scale_log2;
+  float* ws_o;
+  float* ws_ml;
+  int ranges;               // decode: work-groups per KV head
+  long long rows;           // partial results per query head
+  int parts;                // prefill: key parts
+  int tiles;
+  int total_q;
+};
+
+// ---------------------------------------------------------------------------
+// Query rows
+
+// 16 rows as the B operand: lane l holds row l & 15 (`row`, null: zeros), quarter l >> 4.
+template <int D, int kBits>
+struct Rows16;
+
+template <int D>
+struct Rows16<D, 8> {
+  bf16x8 q[D / 32];
+  __device__ __forceinline__ void load(const uint16_t* row, int lane) {
+    // step s of the contracted index: features (D / 4) qd + 8 s .. + 7, as K's lanes hold them
+#pragma unroll
+    for (int s = 0; s < D / 32; ++s) {
+      q[s] = bf16x8{};
+      if (row != nullptr) q[s] = *reinterpret_cast<const bf16x8*>(row + D / 4 * (lane >> 4) + 8 * s);
+    }
+  }
+};
+
+// the largest magnitude of 16 features
+__device__ __forceinline__ unsigned top_of(const u32x4 (&x)[2]) {
+  unsigned top = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const unsigned w = x[i / 4][i % 4];
+    top = max(top, max(w & 0x7fffu, (w >> 16) & 0x7fffu));
+  }
+  return top;
+}
+
+// 16 features as E4M3 heads times `scale` and what is left times scale / 16
+__device__ __forceinline__ void split16(const u32x4 (&x)[2], float scale, int* head, int* rest) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    i16_pair h = {0, 0}, r = {0, 0};
+#pragma unroll
+    for (int p = 0; p < 2; ++p) {
+      const uint32_t w = x[i / 2][2 * (i % 2) + p];
+      h = p ? __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(h, as_pair(w), scale, true)
+            : __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(h, as_pair(w), scale, false);
+      const uint32_t back = read_pair<8>(__builtin_bit_cast(uint32_t, h), scale, p);
+      const float a = __builtin_bit_cast(float, w << 16) - __builtin_bit_cast(float, back << 16);
+      const float b = __builtin_bit_cast(float, w & 0xffff0000u) - __builtin_bit_cast(float, back & 0xffff0000u);
+      r = p ? __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(r, a, b, scale * 0.0625f, true)
+            : __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(r, a, b, scale * 0.0625f, false);
+    }
+    head[i] = __builtin_bit_cast(int, h);
+    rest[i] = __builtin_bit_cast(int, r);
+  }
+}
+
+// The scale byte of a group of a query: E4M3's, with room for the rest's below it.
+__device__ __forceinline__ int query_scale(unsigned top) { return max(scale_byte<128, 8>(top), 14); }
+
+template <int D>
+struct Rows16<D, 4> {
+  // D = 128: [0] the heads, [1] the rests; D = 64: both in one
+  i32x8 q[D / 64];
+  int scale[D / 64];
+  __device__ __forceinline__ void load(const uint16_t* row, int lane) {
+    const int qd = lane >> 4;
+    // the 8-bit operand's lane holds indices 16 qd .. + 15 and 64 + 16 qd .. + 15
+    u32x4 x[D / 64][2];
+#pragma unroll
+    for (int s = 0; s < D / 64; ++s)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        x[s][i] = u32x4{};
+        if (row != nullptr) x[s][i] = *reinterpret_cast<const u32x4*>(row + 64 * s + 16 * qd + 8 * i);
+      }
+    // the group's other 16 features are lane qd ^ 1's
+    int byte[D / 64];
+#pragma unroll
+    for (int s = 0; s < D / 64; ++s) {
+      unsigned top = top_of(x[s]);
+      top = max(top, (unsigned)__shfl_xor((int)top, 16));
+      byte[s] = query_scale(top);
+    }
+#pragma unroll
+    for (int s = 0; s < D / 64; ++s) {
+      int head[4], rest[4];
+      // (a group that is not finite is NaN by its scale; its codes do not matter)
+      split16(x[s], byte[s] == kNanScale ? 1.f : scale_of(byte[s]), head, rest);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if constexpr (D == 128) {
+          q[0][4 * s + i] = head[i];
+          q[1][4 * s + i] = rest[i];
+        } else {
+          q[0][i] = head[i];
+          q[0][4 + i] = rest[i];
+        }
+      }
+    }
+    // lane qd supplies the scale of indices 32 qd .. + 31: at D = 128 of group qd, whose lanes are
+    // 2 qd and 2 qd + 1 (mod 4); at D = 64 of the heads' group qd or the rests' group qd - 2
+    const int from = (lane & 15) + 16 * (2 * qd & 3);
+    const int first = __shfl(byte[0], from);
+    if constexpr (D == 128) {
+      const int second = __shfl(byte[1], from);
+      const int b = qd < 2 ? first : second;
+      scale[0] = b;
+      scale[1] = b == kNanScale ? b : b - 4;
+    } else {
+      scale[0] = qd < 2 || first == kNanScale ? first : first - 4;
+    }
+  }
+};
+
+// ---------------------------------------------------------------------------
+// Keys
+
+// The codes and scales of 32 keys (two blocks) as a lane needs them.
+template <int D, int kBits>
+struct Unit {
+  using T = QuantTile<D, kBits>;
+  static constexpr int kKWords = kBits == 4 ? 4 : D / 16;      // a lane's codes of a block, in words
+  static constexpr int kVWords = T::kPartBytes;                // 4 keys of kPartBytes
+  uint32_t k[2][kKWords];
+  uint32_t v[2][kVWords];
+  int ks[2];
+  uint32_t vs[2];
+
+  template <int kWords>
+  __device__ __forceinline__ static void load_words(uint32_t (&to)[kWords], __amdgpu_buffer_rsrc_t rs, int off) {
+    if constexpr (kWords == 2) {
+      const u32x2 x = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(rs, off, 0, 0));
+      to[0] = x[0];
+      to[1] = x[1];
+    } else {
+#pragma unroll
+      for (int w = 0; w < kWords; w += 4) {
+        const u32x4 x = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rs, off + 4 * w, 0, 0));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) to[w + i] = x[i];
+      }
+    }
+  }
+
+  // Blocks id0 and id1 of the KV head whose tiles `base` starts at, `stride` bytes apart.  The
+  // descriptor of a negative id is empty: zeros, and nothing outside the pool is read.
+  __device__ __forceinline__ void load(const uint8_t* base, size_t stride, int id0, int id1, int lane) {
+    const int key = lane & 15, qd = lane >> 4;
+    int k_off, ks_off;
+    if constexpr (kBits == 4) {
+      const int g = D == 128 ? qd : qd & 1;      // D = 64: indices 64 .. 127 are the same keys again
+      k_off = key * T::kRowBytes + 16 * g;
+      ks_off = T::kKScales + key * T::kGroups + g;
+    } else {
+      k_off = key * T::kRowBytes + D / 4 * qd;
+      ks_off = T::kKScales + key * T::kGroups + qd * T::kGroups / 4;
+    }
+    const int v_off = T::kV + (key * 16 + 4 * qd) * T::kPartBytes;
+    const int vs_off = T::kVScales + key * T::kPart / kScaleGroup * 16 + 4 * qd;
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+      const int id = b ? id1 : id0;
+      const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(
+          (void*)(base + (size_t)id * stride), (short)0, id < 0 ? 0 : T::kBytes, kRawBufferWord3);
+      load_words(k[b], rs, k_off);
+      load_words(v[b], rs, v_off);
+      ks[b] = __builtin_amdgcn_raw_buffer_load_b8(rs, ks_off, 0, 0);
+      vs[b] = __builtin_amdgcn_raw_buffer_load_b32(rs, vs_off, 0, 0);
+    }
+  }
+
+  // What stands behind `n` keys of the unit is not the sequence's: V there becomes zero (its weights
+  // are 0, but 0 times a NaN is NaN).
+  __device__ __forceinline__ void cut_values(int n, int lane) {
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (16 * b + 4 * (lane >> 4) + i >= n) {
+          vs[b] = (vs[b] & ~(0xffu << (8 * i))) | (0x7fu << (8 * i));
+          // (key i's codes: kPartBytes of them)
+          if constexpr (T::kPartBytes == 2) {
+            v[b][i / 2] &= i % 2 ? 0x0000ffffu : 0xffff0000u;
+          } else {
+#pragma unroll
+            for (int w = 0; w < T::kPartBytes / 4; ++w) v[b][i * (T::kPartBytes / 4) + w] = 0;
+          }
+        }
+  }
+
+  // S^T of the 16 keys of block b and 16 rows: lane l has row l & 15 and keys 4 (l >> 4) .. + 3
+  __device__ __forceinline__ f32x4 logits(int b, const Rows16<D, kBits>& rows) const {
+    f32x4 s = f32x4{};
+    if constexpr (kBits == 4) {
+      const i32x8 a = {(int)k[b][0], (int)k[b][1], (int)k[b][2], (int)k[b][3], 0, 0, 0, 0};
+#pragma unroll
+      for (int i = 0; i < D / 64; ++i)
+        s = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, rows.q[i], s, 4, 0, 0, ks[b], 0, rows.scale[i]);
+    } else {
+      const float scale = scale_of(ks[b]);
+#pragma unroll
+      for (int i = 0; i < D / 32; ++i) {
+        const u32x4 a = {read_pair<8>(k[b][2 * i], scale, 0), read_pair<8>(k[b][2 * i], scale, 1),
+                         read_pair<8>(k[b][2 * i + 1], scale, 0), read_pair<8>(k[b][2 * i + 1], scale, 1)};
+        s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), rows.q[i], s, 0, 0, 0);
+      }
+    }
+    return s;
+  }
+
+  // V^T fragments of features kPart c + t, t = 2 pair and 2 pair + 1 (c = l & 15): the lane's
+  // keys 4 qd .. + 3 of both blocks
+  __device__ __forceinline__ void values(int pair, const float (&scale)[2][4], bf16x8 (&f)[2]) const {
+    uint32_t x[2][4];
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if constexpr (kBits == 4) {
+          const int byte = i * T::kPartBytes + pair;       // of the lane's codes
+          x[b][i] = read_pair<4>(v[b][byte / 4], scale[b][i], byte % 4);
+        } else {
+          const int half = i * T::kPartBytes / 2 + pair;
+          x[b][i] = read_pair<8>(v[b][half / 2], scale[b][i], half % 2);
+        }
+      }
+    u32x4 lo, hi;
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        lo[2 * b + i] = __builtin_amdgcn_perm(x[b][2 * i + 1], x[b][2 * i], 0x05040100u);
+        hi[2 * b + i] = __builtin_amdgcn_perm(x[b][2 * i + 1], x[b][2 * i], 0x07060302u);
+      }
+    f[0] = __builtin_bit_cast(bf16x8, lo);
+    f[1] = __builtin_bit_cast(bf16x8, hi);
+  }
+
+  __device__ __forceinline__ void value_scales(float (&scale)[2][4]) const {
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+      scale[b][0] = __builtin_bit_cast(float, (vs[b] & 0xffu) << 23);
+      scale[b][1] = __builtin_bit_cast(float, (vs[b] & 0xff00u) << 15);
+      scale[b][2] = __builtin_bit_cast(float, (vs[b] & 0xff0000u) << 7);
+      scale[b][3] = __builtin_bit_cast(float, (vs[b] & 0xff000000u) >> 1);
+    }
+  }
+};
+
+// ---------------------------------------------------------------------------
+// The softmax of kTiles x 16 rows over the keys seen so far: lane l holds, of row l & 15 of every
+// tile, O's features D / 4 qd + D / 16 r + t in o[t][r], and its own keys' share of l.
+template <int D, int kBits, int kTiles>
+struct Softmax {
+  f32x4 o[kTiles][D / 16];
+  float m[kTiles], l[kTiles];
+
+  __device__ __forceinline__ void reset(float lowest) {
+#pragma unroll
+    for (int x = 0; x < kTiles; ++x) {
+#pragma unroll
+      for (int t = 0; t < D / 16; ++t) o[x][t] = f32x4{};
+      m[x] = lowest;
+      l[x] = 0.f;
+    }
+  }
+
+  // The unit's 32 keys; of them a row of tile x sees the first seen[x] (masked: some row may not
+  // see all).
+  __device__ __forceinline__ void add(const Unit<D, kBits>& u, const Rows16<D, kBits> (&rows)[kTiles], float c,
+                                      bool masked, const int (&seen)[kTiles], int lane) {
+    const int qd = lane >> 4;
+    bf16x8 p[kTiles];
+#pragma unroll
+    for (int x = 0; x < kTiles; ++x) {
+      f32x4 s[2];
+#pragma unroll
+      for (int b = 0; b < 2; ++b) s[b] = u.logits(b, rows[x]);
+      if (masked) {
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) s[b][r] = 16 * b + 4 * qd + r < seen[x] ? s[b][r] : -INFINITY;
+      }
+      float top = fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3]));
+      top = fmaxf(top, fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3])));
+      if (__builtin_amdgcn_ballot_w64(__builtin_fmaf(top, c, -m[x] * c) > kLazy)) {
+        const float m_new = fmaxf(m[x], quad_max(top));
+        const float alpha = __builtin_amdgcn_exp2f((m[x] - m_new) * c);
+        m[x] = m_new;
+        l[x] *= alpha;
+#pragma unroll
+        for (int t = 0; t < D / 16; ++t) o[x][t] *= alpha;
+      }
+      const float mc = m[x] * c;
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][r], c, -mc));
+          // (rounded to bf16 for the product with V; the sum takes it unrounded)
+          p[x][4 * b + r] = (__bf16)e;
+          l[x] += e;
+        }
+    }
+    float scale[2][4];
+    u.value_scales(scale);
+#pragma unroll
+    for (int t = 0; t < D / 16; t += 2) {
+      bf16x8 f[2];
+      u.values(t / 2, scale, f);
+#pragma unroll
+      for (int x = 0; x < kTiles; ++x) {
+        o[x][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f[0], p[x], o[x][t], 0, 0, 0);
+        o[x][t + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f[1], p[x], o[x][t + 1], 0, 0, 0);
+      }
+    }
+  }
+};
+
+// 8 features of a lane's O (its r-th run of D / 16, at D = 64 two of them) as bf16
+template <int D>
+__device__ __forceinline__ bf16x8 rounded8(const f32x4 (&o)[D / 16], int i, float l) {
+  bf16x8 x;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) x[e] = (__bf16)(o[e % (D / 16)][8 * i / (D / 16) + e / (D / 16)] / l);
+  return x;
+}
+
+// ---------------------------------------------------------------------------
+// Decode.  The batch's keys are counted in units of 32 and dealt to `ranges` work-groups per KV
+// head in equal contiguous ranges.  A work-group's waves take the units of a piece (a sequence's
+// part of the range) in turn and merge in LDS; a sequence cut over several ranges leaves partial
+// results (O relative to m, m, and l) that a second kernel merges.
+
+__device__ __forceinline__ long long total_units(const QuantParams& p, int lane) {
+  long long total = 0;
+  for (int s = 0; s < p.batch; s += 64) total += wave_total(s + lane < p.batch ? units_of(p.lens[s + lane]) : 0);
+  return total;
+}
+
+__device__ __forceinline__ int units_per_range(const QuantParams& p, long long total) {
+  return max((int)((total + p.ranges - 1) / p.ranges), kWaves);
+}
+
+template <int D>
+struct DecodeLds {
+  float o[kWaves][kMaxGroup][D + 4];
+  float2 ml[kWaves][kMaxGroup];
+};
+
+template <int D, int kBits>
+__global__ __launch_bounds__(kThreads, D == 64 ? 4 : 3) void quant_decode_kernel(QuantParams p) {
+  using T = QuantTile<D, kBits>;
+  __shared__ DecodeLds<D> sm;
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int g = blockIdx.x % p.num_kv_heads;
+  const int w = blockIdx.x / p.num_kv_heads;
+  const ScalarInts lens = (ScalarInts)p.lens;
+  const long long total = total_units(p, lane);
+  const int per = units_per_range(p, total);
+  const long long u0 = (long long)w * per;
+  if (u0 >= total) return;
+  int left = (int)min((long long)per, total - u0);
+  // the sequence that holds unit u0
+  int r = 0, x = 0;
+  {
+    long long first = 0;
+    for (int s = 0;; s += 64) {
+      const int n = s + lane < p.batch ? units_of(p.lens[s + lane]) : 0;
+      const int incl = wave_scan(n);
+      const unsigned long long past = __builtin_amdgcn_ballot_w64(first + incl > u0);
+      if (past != 0) {
+        const int at = __builtin_ctzll(past);
+        r = s + at;
+        x = (int)(u0 - first - __builtin_amdgcn_readlane(incl - n, at));
+        break;
+      }
+      first += __builtin_amdgcn_readlane(incl, 63);
+    }
+  }
+  const size_t stride = (size_t)p.num_kv_heads * T::kBytes;
+  const uint8_t* base = p.pool + (size_t)g * T::kBytes;
+  const int j = lane & 15;
+  const float c = p.scale_log2;
+  const float lowest = lowest_reference(c);
+  for (;;) {
+    const int len = lens[r];
+    const int n = units_of(len);
+    const int xe = min(n, x + left);
+    const bool whole = x == 0 && xe == n;
+    left -= xe - x;
+    const ScalarInts table = (ScalarInts)(p.block_tables + (size_t)r * p.max_blocks_per_seq);
+    const int last = (len - 1) / kBlock;
+    Rows16<D, kBits> rows[1];
+    rows[0].load(j < p.group ? p.q + ((size_t)r * p.num_q_heads + g * p.group + j) * D : nullptr, lane);
+    Softmax<D, kBits, 1> soft;
+    soft.reset(lowest);
+    Unit<D, kBits> cur, nxt;
+    int y = x + wave;
+    int id0 = 0, id1 = 0;
+    auto ids_of = [&](int unit) {
+      id0 = table[kUnitBlocks * unit];
+      id1 = table[min(kUnitBlocks * unit + 1, last)];
+    };
+    if (y < xe) {
+      ids_of(y);
+      nxt.load(base, stride, id0, id1, lane);
+      if (y + kWaves < xe) ids_of(y + kWaves);
+    }
+    for (; y < xe; y += kWaves) {
+      cur = nxt;
+      if (y + kWaves < xe) {
+        nxt.load(base, stride, id0, id1, lane);
+        if (y + 2 * kWaves < xe) ids_of(y + 2 * kWaves);
+      }
+      const int seen[1] = {len - y * kUnitKeys};
+      const bool masked = seen[0] < kUnitKeys;
+      if (masked) cur.cut_values(seen[0], lane);
+      soft.add(cur, rows, c, masked, seen, lane);
+    }
+    const float l = quad_sum(soft.l[0]);
+    if (j < p.group) {
+#pragma unroll
+      for (int rr = 0; rr < 4; ++rr)
+#pragma unroll
+        for (int t = 0; t < D / 16; t += 4)
+          *reinterpret_cast<f32x4*>(&sm.o[wave][j][D / 4 * (lane >> 4) + D / 16 * rr + t]) =
+              f32x4{soft.o[0][t][rr], soft.o[0][t + 1][rr], soft.o[0][t + 2][rr], soft.o[0][t + 3][rr]};
+      if (lane < 16) sm.ml[wave][j] = make_float2(soft.m[0], l);
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < p.group * (D / 4); i += kThreads) {
+      const int hj = i / (D / 4), d = i % (D / 4) * 4;
+      float m = sm.ml[0][hj].x;
+#pragma unroll
+      for (int k = 1; k < kWaves; ++k) m = fmaxf(m, sm.ml[k][hj].x);
+      float den = 0.f;
+      f32x4 acc = f32x4{};
+#pragma unroll
+      for (int k = 0; k < kWaves; ++k) {
+        const float wt = __builtin_amdgcn_exp2f((sm.ml[k][hj].x - m) * c);
+        den = __builtin_fmaf(wt, sm.ml[k][hj].y, den);
+        const f32x4 o = *reinterpret_cast<const f32x4*>(&sm.o[k][hj][d]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[e] = __builtin_fmaf(wt, o[e], acc[e]);
+      }
+      if (whole) {
+        bf16x4 o;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] = (__bf16)(acc[e] / den);
+        *reinterpret_cast<uint2*>(p.out + ((size_t)r * p.num_q_heads + g * p.group + hj) * D + d) =
+            __builtin_bit_cast(uint2, o);
+      } else {
+        const size_t at = ((size_t)g * p.rows + r + w) * p.group + hj;
+        *reinterpret_cast<f32x4*>(p.ws_o + at * D + d) = acc;
+        if (d == 0) *reinterpret_cast<float2*>(p.ws_ml + 2 * at) = make_float2(m, den);
+      }
+    }
+    if (left <= 0) return;
+    do ++r;
+    while (lens[r] <= 0);
+    x = 0;
+    __syncthreads();
+  }
+}
+
+// One work-group per (sequence, KV head) merges what the ranges left of it.
+template <int D>
+__global__ __launch_bounds__(kMergeThreads) void quant_decode_merge_kernel(QuantParams p) {
+  const int g = blockIdx.x % p.num_kv_heads;
+  const int r = blockIdx.x / p.num_kv_heads;
+  const int lane = threadIdx.x & 63;
+  long long total = 0, before = 0;
+  for (int s = 0; s < p.batch; s += 64) {
+    const int n = s + lane < p.batch ? units_of(p.lens[s + lane]) : 0;
+    total += wave_total(n);
+    before += wave_total(s + lane < r ? n : 0);
+  }
+  const int per = units_per_range(p, total);
+  const int n = units_of(p.lens[r]);
+  const int w0 = (int)(before / per);
+  const int pieces = n == 0 ? 0 : (int)((before + n - 1) / per) - w0 + 1;
+  if (pieces == 1) return;
+  const size_t first = ((size_t)g * p.rows + r + w0) * p.group;
+  merge_pieces<D>(
+      p.ws_o, p.ws_ml, p.group, p.scale_log2, [&](int) { return pieces; },
+      [&](int hj, int k) { return first + (size_t)k * p.group + hj; },
+      [&](int hj, int d, bf16x4 o) {
+        *reinterpret_cast<uint2*>(p.out + ((size_t)r * p.num_q_heads + g * p.group + hj) * D + d) =
+            __builtin_bit_cast(uint2, pieces == 0 ? bf16x4{} : o);
+      });
+}
+
+// ---------------------------------------------------------------------------
+// Prefill.  Rows of a KV head are (token, query head of it), heads fastest; a wave takes 32 of
+// them, a work-group 128, which its waves' loads of the same keys share in the L1 cache.  Part
+// `part` of the keys that a tile's rows see is one work-group's; several leave partial results.
+
+constexpr int kRowTiles = 2;
+constexpr int kWaveRows = 16 * kRowTiles;
+constexpr int kTileRows = kWaves * kWaveRows;
+
+template <int D, int kBits>
+__global__ __launch_bounds__(kThreads, 2) void quant_prefill_kernel(QuantParams p) {
+  using T = QuantTile<D, kBits>;
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const ScalarInts prefix = (ScalarInts)p.lens;
+  const ScalarInts cu = (ScalarInts)p.cu_q_lens;
+  unsigned at = blockIdx.x;
+  const int g = at % p.num_kv_heads;
+  at /= p.num_kv_heads;
+  const int part = at % p.parts;
+  at /= p.parts;
+  const int r = at % p.batch;
+  const int tile = p.tiles - 1 - at / p.batch;      // those with the most keys first
+  const int q0 = cu[r];
+  const int tokens = cu[r + 1] - q0;
+  const long long n_rows = (long long)tokens * p.group;
+  const long long row0 = (long long)tile * kTileRows + wave * kWaveRows;
+  if (row0 >= n_rows) return;
+  const int before = prefix[r];
+  const int len = before + tokens;
+  // tokens of the wave's first and last row
+  const int t0 = (int)(row0 / p.group);
+  const int t1 = (int)(min(row0 + kWaveRows, n_rows) - 1) / p.group;
+  const int units = units_of(before + t1 + 1);
+  const int x0 = (int)((long long)units * part / p.parts);
+  const int xe = (int)((long long)units * (part + 1) / p.parts);
+
+  const size_t stride = (size_t)p.num_kv_heads * T::kBytes;
+  const uint8_t* base = p.pool + (size_t)g * T::kBytes;
+  const float c = p.scale_log2;
+  const int j = lane & 15;
+  Rows16<D, kBits> rows[kRowTiles];
+  long long q_row[kRowTiles];      // of q and out; negative: none
+  int end[kRowTiles];              // keys that the row sees
+#pragma unroll
+  for (int i = 0; i < kRowTiles; ++i) {
+    const long long row = row0 + 16 * i + j;
+    const int t = (int)(row / p.group);
+    q_row[i] = row < n_rows ? (long long)(q0 + t) * p.num_q_heads + g * p.group + (int)(row - (long long)t * p.group) : -1;
+    end[i] = before + min(t, t1) + 1;
+    rows[i].load(row < n_rows ? p.q + q_row[i] * D : nullptr, lane);
+  }
+  Softmax<D, kBits, kRowTiles> soft;
+  soft.reset(lowest_reference(c));
+  const ScalarInts table = (ScalarInts)(p.block_tables + (size_t)r * p.max_blocks_per_seq);
+  const int last = (len - 1) / kBlock;
+  int id0 = 0, id1 = 0;
+  auto ids_of = [&](int unit) {
+    id0 = table[kUnitBlocks * unit];
+    id1 = table[min(kUnitBlocks * unit + 1, last)];
+  };
+  Unit<D, kBits> cur, nxt;
+  if (x0 < xe) {
+    ids_of(x0);
+    nxt.load(base, stride, id0, id1, lane);
+    if (x0 + 1 < xe) ids_of(x0 + 1);
+  }
+  for (int x = x0; x < xe; ++x) {
+    cur = nxt;
+    if (x + 1 < xe) {
+      nxt.load(base, stride, id0, id1, lane);
+      if (x + 2 < xe) ids_of(x + 2);
+    }
+    const int key0 = x * kUnitKeys;
+    const bool masked = key0 + kUnitKeys > before + t0 + 1;
+    int seen[kRowTiles];
+#pragma unroll
+    for (int i = 0; i < kRowTiles; ++i) seen[i] = end[i] - key0;
+    if (key0 + kUnitKeys > len) cur.cut_values(len - key0, lane);
+    soft.add(cur, rows, c, masked, seen, lane);
+  }
+#pragma unroll
+  for (int i = 0; i < kRowTiles; ++i) {
+    const float l = quad_sum(soft.l[i]);
+    if (q_row[i] < 0) continue;
+    const int d0 = D / 4 * (lane >> 4);
+    if (p.parts == 1) {
+#pragma unroll
+      for (int k = 0; k < D / 32; ++k)
+        *reinterpret_cast<bf16x8*>(p.out + q_row[i] * D + d0 + 8 * k) = rounded8<D>(soft.o[i], k, l);
+    } else {
+      const size_t to = (size_t)part * p.total_q * p.num_q_heads + q_row[i];
+#pragma unroll
+      for (int rr = 0; rr < 4; ++rr)
+#pragma unroll
+        for (int t = 0; t < D / 16; t += 4)
+          *reinterpret_cast<f32x4*>(p.ws_o + to * D + d0 + D / 16 * rr + t) =
+              f32x4{soft.o[i][t][rr], soft.o[i][t + 1][rr], soft.o[i][t + 2][rr], soft.o[i][t + 3][rr]};
+      if (lane < 16) *reinterpret_cast<float2*>(p.ws_ml + 2 * to) = make_float2(soft.m[i], l);
+    }
+  }
+}
+
+// A thread merges 4 features of a (token, query head) row.
+template <int D>
+__global__ __launch_bounds__(kThreads) void quant_prefill_merge_kernel(QuantParams p) {
+  const long long i = (long long)blockIdx.x * kThreads + threadIdx.x;
+  const long long n = (long long)p.total_q * p.num_q_heads;
+  const long long row = i / (D / 4);
+  const int d = (int)(i % (D / 4)) * 4;
+  if (row >= (long long)p.cu_q_lens[p.batch] * p.num_q_heads) return;
+  float m = -INFINITY;
+  for (int k = 0; k < p.parts; ++k) m = fmaxf(m, p.ws_ml[2 * (k * n + row)]);
+  float den = 0.f;
+  f32x4 acc = f32x4{};
+  for (int k = 0; k < p.parts; ++k) {
+    const float2 ml = *reinterpret_cast<const float2*>(p.ws_ml + 2 * (k * n + row));
+    const float wt = __builtin_amdgcn_exp2f((ml.x - m) * p.scale_log2);
+    const f32x4 o = *reinterpret_cast<const f32x4*>(p.ws_o + (k * n + row) * D + d);
+    den = __builtin_fmaf(wt, ml.y, den);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) acc[e] = __builtin_fmaf(wt, o[e], acc[e]);
+  }
+  bf16x4 o;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) o[e] = (__bf16)(acc[e] / den);
+  *reinterpret_cast<uint2*>(p.out + row * D + d) = __builtin_bit_cast(uint2, o);
+}
+
+QuantParams params_of(const QuantAttnLaunch& a) {
+  QuantParams p = {};
+  p.q = a.q;
+  p.pool = a.pool;
+  p.block_tables = a.block_tables;
+  p.lens = a.lens;
+  p.cu_q_lens = a.cu_q_lens;
+  p.out = a.out;
+  p.batch = a.batch;
+  p.max_blocks_per_seq = a.max_blocks_per_seq;
+  p.num_q_heads = a.num_q_heads;
+  p.num_kv_heads = a.num_kv_heads;
+  p.group = a.num_q_heads / a.num_kv_heads;
+  p.scale_log2 = a.scale * kLog2e;
+  p.total_q = a.total_q;
+  return p;
+}
+
+template <int D, int kBits>
+hipError_t decode(const QuantParams& p, hipStream_t stream) {
+  hipLaunchKernelGGL((quant_decode_kernel<D, kBits>), dim3((unsigned)p.ranges * p.num_kv_heads), dim3(kThreads), 0,
+                     stream, p);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL(quant_decode_merge_kernel<D>, dim3((unsigned)p.batch * p.num_kv_heads), dim3(kMergeThreads), 0,
+                     stream, p);
+  return hipGetLastError();
+}
+
+template <int D, int kBits>
+hipError_t prefill(const QuantParams& p, long long grid, hipStream_t stream) {
+  hipLaunchKernelGGL((quant_prefill_kernel<D, kBits>), dim3((unsigned)grid), dim3(kThreads), 0, stream, p);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || p.parts == 1) return e;
+  const long long threads = (long long)p.total_q * p.num_q_heads * (D / 4);
+  hipLaunchKernelGGL(quant_prefill_merge_kernel<D>, dim3((unsigned)((threads + kThreads - 1) / kThreads)),
+                     dim3(kThreads), 0, stream, p);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+// Work-groups per compute unit that a decode's keys are dealt to
+constexpr int kDecodeGroupsPerCu = 4;
+
+QuantDecodeGeometry quant_decode_geometry(int batch, int max_seq_len, int num_q_heads, int num_kv_heads,
+                                          int head_dim, int cus) {
+  QuantDecodeGeometry geo = {};
+  const double units = (double)((max_seq_len + 31LL) / 32);
+  const double most = batch * units;
+  geo.ranges = (kDecodeGroupsPerCu * cus + num_kv_heads - 1) / num_kv_heads;
+  if (most < geo.ranges) geo.ranges = most < 1 ? 1 : (int)most;
+  geo.rows = (long long)geo.ranges + batch;
+  geo.bytes = geo.rows * num_q_heads * (head_dim + 2) * (long long)sizeof(float);
+  // (the units of 64 sequences, and those of a range, are counted in 32 bits)
+  geo.fits = launch_fits((double)geo.ranges * num_kv_heads, kThreads) &&
+             launch_fits((double)batch * num_kv_heads, kMergeThreads) && 64 * units < 0x1p31 &&
+             most / geo.ranges < 0x1p31;
+  return geo;
+}
+
+hipError_t launch_quant_decode(const QuantAttnLaunch& a, const QuantDecodeGeometry& geo, hipStream_t stream) {
+  QuantParams p = params_of(a);
+  p.ranges = geo.ranges;
+  p.rows = geo.rows;
+  p.ws_o = a.workspace;
+  p.ws_ml = a.workspace + geo.rows * a.num_q_heads * a.head_dim;
+  if (a.head_dim == 64) return a.bits == 4 ? decode<64, 4>(p, stream) : decode<64, 8>(p, stream);
+  return a.bits == 4 ? decode<128, 4>(p, stream) : decode<128, 8>(p, stream);
+}
+
+constexpr int kPrefillMaxParts = 16;
+// fewest units of a part
+constexpr int kPrefillPartUnits = 4;
+
+QuantPrefillGeometry quant_prefill_geometry(int batch, int total_q, int max_q_len, int max_kv_len,
+                                            int num_q_heads, int num_kv_heads, int head_dim, int cus) {
+  QuantPrefillGeometry geo = {};
+  const long long group = num_q_heads / num_kv_heads;
+  geo.tiles = (max_q_len * group + kTileRows - 1) / kTileRows;
+  // tiles there are at most: of the longest suffix, or as many as the rows of all make
+  const double bound = (double)num_kv_heads * ((double)total_q * group / kTileRows + batch);
+  double tiles = (double)geo.tiles * batch * num_kv_heads;
+  if (bound < tiles) tiles = bound;
+  long long parts = tiles > 0 ? (long long)(2 * cus / tiles) : 1;
+  const long long units = (max_kv_len + 31LL) / 32;
+  if (parts > units / kPrefillPartUnits) parts = units / kPrefillPartUnits;
+  if (parts > kPrefillMaxParts) parts = kPrefillMaxParts;
+  geo.parts = parts < 1 ? 1 : (int)parts;
+  const double grid = (double)geo.tiles * batch * num_kv_heads * geo.parts;
+  geo.fits = launch_fits(grid, kThreads) &&
+             (geo.parts == 1 || launch_fits((double)total_q * num_q_heads * (head_dim / 4) / kThreads + 1, kThreads));
+  if (!geo.fits) return geo;
+  geo.grid = (long long)grid;
+  geo.bytes = geo.parts == 1 ? 0 : (long long)geo.parts * total_q * num_q_heads * (head_dim + 2) * (long long)sizeof(float);
+  return geo;
+}
+
+hipError_t launch_quant_prefill(const QuantAttnLaunch& a, const QuantPrefillGeometry& geo, hipStream_t stream) {
+  QuantParams p = params_of(a);
+  p.parts = geo.parts;
+  p.tiles = (int)geo.tiles;
+  p.ws_o = a.workspace;
+  p.ws_ml = a.workspace + (long long)geo.parts * a.total_q * a.num_q_heads * a.head_dim;
+  if (a.head_dim == 64) return a.bits == 4 ? prefill<64, 4>(p, geo.grid, stream) : prefill<64, 8>(p, geo.grid, stream);
+  return a.bits == 4 ? prefill<128, 4>(p, geo.grid, stream) : prefill<128, 8>(p, geo.grid, stream);
+}
+
+}  // namespace cs

@@ -39,7 +39,13 @@ EXPORTED = ("cs_prefill_paged_attn", "cs_kv_prefetch", "cs_kv_write", "cs_kv_off
             "cs_prefill_window_workspace_bytes", "cs_decode_window_attn",
             "cs_decode_window_workspace_bytes", "cs_decode_attn_scores",
             "cs_decode_scores_workspace_bytes", "cs_prefill_key_scores",
-            "cs_prefill_scores_workspace_bytes", "cs_kv_evict")
+            "cs_prefill_scores_workspace_bytes", "cs_kv_evict", "cs_kv_quant_tile_bytes",
+            "cs_kv_write_quant", "cs_kv_quantize", "cs_kv_dequantize", "cs_decode_quant_attn",
+            "cs_decode_quant_workspace_bytes", "cs_prefill_quant_attn",
+            "cs_prefill_quant_workspace_bytes")
+
+# tokens of a pool block
+BLOCK_SIZE = 16
 
 # bytes of the device scratch array behind cs_cascade_decode_attn_noalloc
 NOALLOC_SCRATCH_BYTES = 32 * 1024 * 1024
@@ -139,6 +145,14 @@ def _load():
                                   ctypes.c_int),
         "cs_prefill_scores_workspace_bytes": ([i32] * 8, i64),
         "cs_kv_evict": ([vp] * 7 + [i32] * 10 + [vp, vp, vp], ctypes.c_int),
+        "cs_kv_quant_tile_bytes": ([i32, i32], i64),
+        "cs_kv_write_quant": ([vp] * 3 + [i32, vp] + [i32] * 5 + [vp], ctypes.c_int),
+        "cs_kv_quantize": ([vp] * 4 + [i32, vp] + [i32] * 6 + [vp], ctypes.c_int),
+        "cs_kv_dequantize": ([vp] * 3 + [i32, vp, vp] + [i32] * 6 + [vp], ctypes.c_int),
+        "cs_decode_quant_attn": ([vp] * 4 + [i32] * 9 + [f32, vp, i64, vp, vp], ctypes.c_int),
+        "cs_decode_quant_workspace_bytes": ([i32] * 6, i64),
+        "cs_prefill_quant_attn": ([vp] * 5 + [i32] * 11 + [f32, vp, i64, vp, vp], ctypes.c_int),
+        "cs_prefill_quant_workspace_bytes": ([i32] * 8, i64),
     }
     for name, (args, res) in sigs.items():
         fn = getattr(lib, name)
@@ -921,6 +935,200 @@ def cs_kv_evict(score_pool, k_pool, v_pool, block_tables, dst_block_tables, seq_
                             int(max_seq_len), block_tables.shape[1], num_blocks, hkv, d, bs, budget,
                             int(min(trigger, 2 ** 31 - 1)), int(recent), kept.data_ptr(), new_lens.data_ptr(),
                             _stream_handle(stream, dev)))
+
+
+def kv_quant_tile_bytes(head_dim, bits):
+    """Bytes of a (block, KV head) tile of a quantised pool: the pool is uint8
+    ``[num_blocks, Hkv, kv_quant_tile_bytes(head_dim, bits)]`` (-1: no such format)."""
+    return int(_lib.cs_kv_quant_tile_bytes(head_dim, bits))
+
+
+_tile_bytes = functools.lru_cache(maxsize=64)(kv_quant_tile_bytes)
+_U8 = torch.uint8
+
+
+def _require_quant_pool(quant_pool, hkv, d, bits, dev, index):
+    _require_tensors(dev, index, ("quant_pool", quant_pool, _U8))
+    if bits not in (4, 8):
+        raise CacheScoutError(CS_ERR_UNSUPPORTED, f"bits {bits} (supported: 4, 8)")
+    if d not in (64, 128):
+        raise CacheScoutError(CS_ERR_UNSUPPORTED, f"head_dim {d} (supported: 64, 128)")
+    _require(quant_pool.dim() == 3 and tuple(quant_pool.shape[1:]) == (hkv, _tile_bytes(d, bits)),
+             "quant_pool must be [num_blocks, Hkv, kv_quant_tile_bytes(D, bits)]")
+
+
+def cs_kv_write_quant_raw(k_new, v_new, slot_mapping, num_tokens, quant_pool, num_blocks, num_kv_heads,
+                          head_dim, block_size, bits, stream=0):
+    """The C call with raw pointers (ints or None); returns the status code."""
+    return _lib.cs_kv_write_quant(k_new, v_new, slot_mapping, num_tokens, quant_pool, num_blocks,
+                                  num_kv_heads, head_dim, block_size, bits, stream)
+
+
+def cs_kv_write_quant(k_new, v_new, slot_mapping, quant_pool, *, bits, stream=None):
+    """Enqueue the write of new tokens' K/V into slots of a quantised pool: arguments as for
+    :func:`cs_kv_write`, ``quant_pool`` uint8 ``[num_blocks, Hkv, kv_quant_tile_bytes(D, bits)]``,
+    ``bits`` 4 or 8."""
+    dev, index = quant_pool.device, quant_pool.get_device()
+    _require_tensors(dev, index, ("k_new", k_new, _BF16), ("v_new", v_new, _BF16),
+                     ("slot_mapping", slot_mapping, _I32))
+    _require(k_new.shape == v_new.shape and k_new.dim() == 3, "k_new/v_new must be [T, Hkv, D]")
+    n, hkv, d = k_new.shape
+    _require(slot_mapping.numel() == n, "slot_mapping must have one entry per token")
+    _require_quant_pool(quant_pool, hkv, d, bits, dev, index)
+    if _current_device() != dev.index:
+        with torch.cuda.device(dev):
+            return cs_kv_write_quant(k_new, v_new, slot_mapping, quant_pool, bits=bits, stream=stream)
+    _check(_lib.cs_kv_write_quant(k_new.data_ptr(), v_new.data_ptr(), slot_mapping.data_ptr(), n,
+                                  quant_pool.data_ptr(), quant_pool.shape[0], hkv, d, BLOCK_SIZE, bits,
+                                  _stream_handle(stream, dev)))
+
+
+def cs_kv_quantize_raw(k_pool, v_pool, src_block_ids, dst_block_ids, n, quant_pool, num_blocks,
+                       num_quant_blocks, num_kv_heads, head_dim, block_size, bits, stream=0):
+    """The C call with raw pointers (ints or None); returns the status code."""
+    return _lib.cs_kv_quantize(k_pool, v_pool, src_block_ids, dst_block_ids, n, quant_pool, num_blocks,
+                               num_quant_blocks, num_kv_heads, head_dim, block_size, bits, stream)
+
+
+def cs_kv_dequantize_raw(quant_pool, src_block_ids, dst_block_ids, n, k_pool, v_pool, num_blocks,
+                         num_quant_blocks, num_kv_heads, head_dim, block_size, bits, stream=0):
+    """The C call with raw pointers (ints or None); returns the status code."""
+    return _lib.cs_kv_dequantize(quant_pool, src_block_ids, dst_block_ids, n, k_pool, v_pool, num_blocks,
+                                 num_quant_blocks, num_kv_heads, head_dim, block_size, bits, stream)
+
+
+def _quant_block_args(k_pool, v_pool, src_block_ids, dst_block_ids, quant_pool, bits):
+    """Validate a call that moves whole blocks; n, the sizes after it and the device."""
+    dev, index = quant_pool.device, quant_pool.get_device()
+    _require_tensors(dev, index, ("k_pool", k_pool, _BF16), ("v_pool", v_pool, _BF16),
+                     ("src_block_ids", src_block_ids, _I32), ("dst_block_ids", dst_block_ids, _I32))
+    _require(k_pool.shape == v_pool.shape and k_pool.dim() == 4, "pools must match")
+    num_blocks, hkv, bs, d = k_pool.shape
+    _require_quant_pool(quant_pool, hkv, d, bits, dev, index)
+    n = src_block_ids.numel()
+    _require(dst_block_ids.numel() == n, "src_block_ids and dst_block_ids must have as many entries")
+    return n, (num_blocks, quant_pool.shape[0], hkv, d, bs, bits), dev
+
+
+def cs_kv_quantize(k_pool, v_pool, src_block_ids, dst_block_ids, quant_pool, *, bits, stream=None):
+    """Enqueue the move of blocks ``src_block_ids`` of a bf16 pool to the (distinct) blocks
+    ``dst_block_ids`` of a quantised pool; both int32 ``[n]`` on the GPU."""
+    n, sizes, dev = _quant_block_args(k_pool, v_pool, src_block_ids, dst_block_ids, quant_pool, bits)
+    if _current_device() != dev.index:
+        with torch.cuda.device(dev):
+            return cs_kv_quantize(k_pool, v_pool, src_block_ids, dst_block_ids, quant_pool, bits=bits,
+                                  stream=stream)
+    _check(_lib.cs_kv_quantize(k_pool.data_ptr(), v_pool.data_ptr(), src_block_ids.data_ptr(),
+                               dst_block_ids.data_ptr(), n, quant_pool.data_ptr(), *sizes,
+                               _stream_handle(stream, dev)))
+
+
+def cs_kv_dequantize(quant_pool, src_block_ids, dst_block_ids, k_pool, v_pool, *, bits, stream=None):
+    """Enqueue the way back: blocks ``src_block_ids`` of a quantised pool into the (distinct)
+    blocks ``dst_block_ids`` of the bf16 pools, exactly the values they hold."""
+    n, sizes, dev = _quant_block_args(k_pool, v_pool, src_block_ids, dst_block_ids, quant_pool, bits)
+    if _current_device() != dev.index:
+        with torch.cuda.device(dev):
+            return cs_kv_dequantize(quant_pool, src_block_ids, dst_block_ids, k_pool, v_pool, bits=bits,
+                                    stream=stream)
+    _check(_lib.cs_kv_dequantize(quant_pool.data_ptr(), src_block_ids.data_ptr(), dst_block_ids.data_ptr(), n,
+                                 k_pool.data_ptr(), v_pool.data_ptr(), *sizes, _stream_handle(stream, dev)))
+
+
+def cs_decode_quant_attn_raw(q, quant_pool, block_tables, seq_lens, batch, max_seq_len, max_blocks_per_seq,
+                             num_blocks, num_q_heads, num_kv_heads, head_dim, block_size, bits, scale,
+                             workspace, workspace_bytes, out, stream=0):
+    """The C call with raw pointers (ints or None); returns the status code."""
+    return _lib.cs_decode_quant_attn(q, quant_pool, block_tables, seq_lens, batch, max_seq_len,
+                                     max_blocks_per_seq, num_blocks, num_q_heads, num_kv_heads, head_dim,
+                                     block_size, bits, ctypes.c_float(scale), workspace, workspace_bytes,
+                                     out, stream)
+
+
+def decode_quant_workspace_bytes(batch, max_seq_len, num_q_heads, num_kv_heads, head_dim, num_cus=0):
+    """Bytes of workspace ``cs_decode_quant_attn`` takes (negative: bad arguments, or no GPU to
+    size for)."""
+    return int(_lib.cs_decode_quant_workspace_bytes(batch, max_seq_len, num_q_heads, num_kv_heads, head_dim,
+                                                    num_cus))
+
+
+def cs_decode_quant_attn(q, quant_pool, block_tables, seq_lens, out, *, bits, max_seq_len, scale,
+                         workspace="auto", stream=None):
+    """Enqueue decode attention over a quantised pool (uint8 ``[num_blocks, Hkv,
+    kv_quant_tile_bytes(D, bits)]``).  Other tensors as for :func:`cs_paged_decode_attn`; a length
+    of 0 gives a row of zeros.  ``workspace``: "auto" (allocated here) or a uint8 GPU tensor of
+    :func:`decode_quant_workspace_bytes`."""
+    dev, index = q.device, q.get_device()
+    _require_tensors(dev, index, ("q", q, _BF16), ("out", out, _BF16), ("block_tables", block_tables, _I32),
+                     ("seq_lens", seq_lens, _I32))
+    _require(q.dim() == 3 and out.shape == q.shape, "q and out must be [B, Hq, D]")
+    _require(quant_pool.dim() == 3, "quant_pool must be [num_blocks, Hkv, kv_quant_tile_bytes(D, bits)]")
+    batch, hq, d = q.shape
+    num_blocks, hkv, _ = quant_pool.shape
+    _require_quant_pool(quant_pool, hkv, d, bits, dev, index)
+    _require(block_tables.dim() == 2 and block_tables.shape[0] == batch, "block_tables must be [B, max_blocks]")
+    _require(seq_lens.numel() == batch, "seq_lens must have B entries")
+    max_seq_len = int(max_seq_len)
+    if _current_device() != dev.index:
+        with torch.cuda.device(dev):
+            return cs_decode_quant_attn(q, quant_pool, block_tables, seq_lens, out, bits=bits,
+                                        max_seq_len=max_seq_len, scale=scale, workspace=workspace, stream=stream)
+    need = _bytes_on(dev.index, decode_quant_workspace_bytes, batch, max_seq_len, hq, hkv, d)
+    ws = _workspace(workspace, need, stream, dev)
+    _check(_lib.cs_decode_quant_attn(q.data_ptr(), quant_pool.data_ptr(), block_tables.data_ptr(),
+                                     seq_lens.data_ptr(), batch, max_seq_len, block_tables.shape[1], num_blocks,
+                                     hq, hkv, d, BLOCK_SIZE, bits, scale, _ptr(ws), _nbytes(ws), out.data_ptr(),
+                                     _stream_handle(stream, dev)))
+
+
+def cs_prefill_quant_attn_raw(q, quant_pool, block_tables, prefix_lens, cu_q_lens, batch, total_q, max_q_len,
+                              max_kv_len, max_blocks_per_seq, num_blocks, num_q_heads, num_kv_heads, head_dim,
+                              block_size, bits, scale, workspace, workspace_bytes, out, stream=0):
+    """The C call with raw pointers (ints or None); returns the status code."""
+    return _lib.cs_prefill_quant_attn(q, quant_pool, block_tables, prefix_lens, cu_q_lens, batch, total_q,
+                                      max_q_len, max_kv_len, max_blocks_per_seq, num_blocks, num_q_heads,
+                                      num_kv_heads, head_dim, block_size, bits, ctypes.c_float(scale),
+                                      workspace, workspace_bytes, out, stream)
+
+
+def prefill_quant_workspace_bytes(batch, total_q, max_q_len, max_kv_len, num_q_heads, num_kv_heads, head_dim,
+                                  num_cus=0):
+    """Bytes of workspace ``cs_prefill_quant_attn`` takes (0: none; negative: bad arguments, or no
+    GPU to size for)."""
+    return int(_lib.cs_prefill_quant_workspace_bytes(batch, total_q, max_q_len, max_kv_len, num_q_heads,
+                                                     num_kv_heads, head_dim, num_cus))
+
+
+def cs_prefill_quant_attn(q, quant_pool, block_tables, prefix_lens, cu_q_lens, out, *, bits, max_q_len,
+                          max_kv_len, scale, workspace="auto", stream=None):
+    """Enqueue prefill attention over a quantised pool (uint8 ``[num_blocks, Hkv,
+    kv_quant_tile_bytes(D, bits)]``), which holds the prefix and the suffix's own K/V.  Other tensors
+    and bounds as for :func:`cs_prefill_paged_attn`; ``workspace``: "auto" (allocated here if the
+    launch needs one) or a uint8 GPU tensor of :func:`prefill_quant_workspace_bytes`."""
+    dev, index = q.device, q.get_device()
+    _require_tensors(dev, index, ("q", q, _BF16), ("out", out, _BF16), ("block_tables", block_tables, _I32),
+                     ("prefix_lens", prefix_lens, _I32), ("cu_q_lens", cu_q_lens, _I32))
+    _require(q.dim() == 3 and out.shape == q.shape, "q and out must be [total_q, Hq, D]")
+    _require(quant_pool.dim() == 3, "quant_pool must be [num_blocks, Hkv, kv_quant_tile_bytes(D, bits)]")
+    total_q, hq, d = q.shape
+    num_blocks, hkv, _ = quant_pool.shape
+    _require_quant_pool(quant_pool, hkv, d, bits, dev, index)
+    _require(block_tables.dim() == 2, "block_tables must be [B, max_blocks]")
+    batch = block_tables.shape[0]
+    _require(prefix_lens.numel() == batch and cu_q_lens.numel() == batch + 1,
+             "prefix_lens must have B entries and cu_q_lens B + 1")
+    max_q_len, max_kv_len = int(max_q_len), int(max_kv_len)
+    if _current_device() != dev.index:
+        with torch.cuda.device(dev):
+            return cs_prefill_quant_attn(q, quant_pool, block_tables, prefix_lens, cu_q_lens, out, bits=bits,
+                                         max_q_len=max_q_len, max_kv_len=max_kv_len, scale=scale,
+                                         workspace=workspace, stream=stream)
+    need = _bytes_on(dev.index, prefill_quant_workspace_bytes, batch, total_q, max_q_len, max_kv_len, hq, hkv, d)
+    ws = _workspace(workspace, need, stream, dev)
+    _check(_lib.cs_prefill_quant_attn(q.data_ptr(), quant_pool.data_ptr(), block_tables.data_ptr(),
+                                      prefix_lens.data_ptr(), cu_q_lens.data_ptr(), batch, total_q, max_q_len,
+                                      max_kv_len, block_tables.shape[1], num_blocks, hq, hkv, d, BLOCK_SIZE, bits,
+                                      scale, _ptr(ws), _nbytes(ws), out.data_ptr(), _stream_handle(stream, dev)))
 
 
 def scout_default_params():
