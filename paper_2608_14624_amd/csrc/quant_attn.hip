@@ -18,9 +18,9 @@
 //     the largest, where 4-bit times 8-bit ones are exact to fp32's 5e-8.)
 //   * V is converted to bf16, two features of a key at a time, which two byte permutes then
 //     pair up by keys.
-// The running maximum that the exponentials are relative to follows the logits only when one is
-// above it by 2^8: P is then up to 256, which bf16 holds as well as 1, and most steps rescale
-// nothing and exchange nothing between lanes.
+// The running maximum that the exponentials are relative to follows the logits only when the
+// weights of a lane's keys add up to more than 256: bf16 holds 256 as well as 1, and most steps
+// rescale nothing, look for no maximum and exchange nothing between lanes.
 #include "decode_common.h"
 #include "internal.h"
 #include "quant_tile.h"
@@ -36,7 +36,7 @@ typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kWaves = 4;             // of a work-group, both kernels
 constexpr int kThreads = 64 * kWaves;
-constexpr float kLazy = 8.f;          // log2 of what a logit's weight may exceed 1 by
+constexpr float kLargeSum = 256.f;    // of a lane's weights of a step
 
 struct QuantParams {
   const uint16_t* q;
@@ -173,16 +173,16 @@ struct Rows16<D, 4> {
 // ---------------------------------------------------------------------------
 // Keys
 
-// The codes and scales of 32 keys (two blocks) as a lane needs them.
+// The codes and scales of a block's 16 keys as a lane needs them.
 template <int D, int kBits>
-struct Unit {
+struct Block {
   using T = QuantTile<D, kBits>;
-  static constexpr int kKWords = kBits == 4 ? 4 : D / 16;      // a lane's codes of a block, in words
-  static constexpr int kVWords = T::kPartBytes;                // 4 keys of kPartBytes
-  uint32_t k[2][kKWords];
-  uint32_t v[2][kVWords];
-  int ks[2];
-  uint32_t vs[2];
+  static constexpr int kKWords = kBits == 4 ? 4 : D / 16;      // a lane's codes of K, in words
+  static constexpr int kVWords = T::kPartBytes;                // of V: 4 keys of kPartBytes
+  uint32_t k[kKWords];
+  uint32_t v[kVWords];
+  int ks;
+  uint32_t vs;
 
   template <int kWords>
   __device__ __forceinline__ static void load_words(uint32_t (&to)[kWords], __amdgpu_buffer_rsrc_t rs, int off) {
@@ -200,9 +200,9 @@ struct Unit {
     }
   }
 
-  // Blocks id0 and id1 of the KV head whose tiles `base` starts at, `stride` bytes apart.  The
+  // Block `id` of the KV head whose tiles `base` starts at, `stride` bytes apart.  The
   // descriptor of a negative id is empty: zeros, and nothing outside the pool is read.
-  __device__ __forceinline__ void load(const uint8_t* base, size_t stride, int id0, int id1, int lane) {
+  __device__ __forceinline__ void load(const uint8_t* base, size_t stride, int id, int lane) {
     const int key = lane & 15, qd = lane >> 4;
     int k_off, ks_off;
     if constexpr (kBits == 4) {
@@ -215,100 +215,98 @@ struct Unit {
     }
     const int v_off = T::kV + (key * 16 + 4 * qd) * T::kPartBytes;
     const int vs_off = T::kVScales + key * T::kPart / kScaleGroup * 16 + 4 * qd;
-#pragma unroll
-    for (int b = 0; b < 2; ++b) {
-      const int id = b ? id1 : id0;
-      const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(
-          (void*)(base + (size_t)id * stride), (short)0, id < 0 ? 0 : T::kBytes, kRawBufferWord3);
-      load_words(k[b], rs, k_off);
-      load_words(v[b], rs, v_off);
-      ks[b] = __builtin_amdgcn_raw_buffer_load_b8(rs, ks_off, 0, 0);
-      vs[b] = __builtin_amdgcn_raw_buffer_load_b32(rs, vs_off, 0, 0);
-    }
+    const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(
+        (void*)(base + (size_t)id * stride), (short)0, id < 0 ? 0 : T::kBytes, kRawBufferWord3);
+    load_words(k, rs, k_off);
+    load_words(v, rs, v_off);
+    ks = __builtin_amdgcn_raw_buffer_load_b8(rs, ks_off, 0, 0);
+    vs = __builtin_amdgcn_raw_buffer_load_b32(rs, vs_off, 0, 0);
   }
 
-  // What stands behind `n` keys of the unit is not the sequence's: V there becomes zero (its weights
-  // are 0, but 0 times a NaN is NaN).
+  // What stands behind `n` keys of the block is not the sequence's: V there becomes zero (its
+  // weights are 0, but 0 times a NaN is NaN).
   __device__ __forceinline__ void cut_values(int n, int lane) {
 #pragma unroll
-    for (int b = 0; b < 2; ++b)
+    for (int i = 0; i < 4; ++i)
+      if (4 * (lane >> 4) + i >= n) {
+        vs = (vs & ~(0xffu << (8 * i))) | (0x7fu << (8 * i));
+        // (key i's codes: kPartBytes of them)
+        if constexpr (T::kPartBytes == 2) {
+          v[i / 2] &= i % 2 ? 0x0000ffffu : 0xffff0000u;
+        } else {
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (16 * b + 4 * (lane >> 4) + i >= n) {
-          vs[b] = (vs[b] & ~(0xffu << (8 * i))) | (0x7fu << (8 * i));
-          // (key i's codes: kPartBytes of them)
-          if constexpr (T::kPartBytes == 2) {
-            v[b][i / 2] &= i % 2 ? 0x0000ffffu : 0xffff0000u;
-          } else {
-#pragma unroll
-            for (int w = 0; w < T::kPartBytes / 4; ++w) v[b][i * (T::kPartBytes / 4) + w] = 0;
-          }
+          for (int w = 0; w < T::kPartBytes / 4; ++w) v[i * (T::kPartBytes / 4) + w] = 0;
         }
+      }
   }
 
-  // S^T of the 16 keys of block b and 16 rows: lane l has row l & 15 and keys 4 (l >> 4) .. + 3
-  __device__ __forceinline__ f32x4 logits(int b, const Rows16<D, kBits>& rows) const {
+  // S^T of the block's keys and 16 rows: lane l has row l & 15 and keys 4 (l >> 4) .. + 3
+  __device__ __forceinline__ f32x4 logits(const Rows16<D, kBits>& rows) const {
     f32x4 s = f32x4{};
     if constexpr (kBits == 4) {
-      const i32x8 a = {(int)k[b][0], (int)k[b][1], (int)k[b][2], (int)k[b][3], 0, 0, 0, 0};
+      const i32x8 a = {(int)k[0], (int)k[1], (int)k[2], (int)k[3], 0, 0, 0, 0};
 #pragma unroll
       for (int i = 0; i < D / 64; ++i)
-        s = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, rows.q[i], s, 4, 0, 0, ks[b], 0, rows.scale[i]);
+        s = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, rows.q[i], s, 4, 0, 0, ks, 0, rows.scale[i]);
     } else {
-      const float scale = scale_of(ks[b]);
+      const float scale = scale_of(ks);
 #pragma unroll
       for (int i = 0; i < D / 32; ++i) {
-        const u32x4 a = {read_pair<8>(k[b][2 * i], scale, 0), read_pair<8>(k[b][2 * i], scale, 1),
-                         read_pair<8>(k[b][2 * i + 1], scale, 0), read_pair<8>(k[b][2 * i + 1], scale, 1)};
+        const u32x4 a = {read_pair<8>(k[2 * i], scale, 0), read_pair<8>(k[2 * i], scale, 1),
+                         read_pair<8>(k[2 * i + 1], scale, 0), read_pair<8>(k[2 * i + 1], scale, 1)};
         s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), rows.q[i], s, 0, 0, 0);
       }
     }
     return s;
   }
 
-  // V^T fragments of features kPart c + t, t = 2 pair and 2 pair + 1 (c = l & 15): the lane's
-  // keys 4 qd .. + 3 of both blocks
-  __device__ __forceinline__ void values(int pair, const float (&scale)[2][4], bf16x8 (&f)[2]) const {
-    uint32_t x[2][4];
+  // The lane's four keys' features kPart c + t (c = l & 15), t = 2 pair in f[0] and 2 pair + 1 in
+  // f[1]: half of a V^T fragment
+  __device__ __forceinline__ void values(int pair, const float (&scale)[4], u32x2 (&f)[2]) const {
+    uint32_t x[4];
 #pragma unroll
-    for (int b = 0; b < 2; ++b)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        if constexpr (kBits == 4) {
-          const int byte = i * T::kPartBytes + pair;       // of the lane's codes
-          x[b][i] = read_pair<4>(v[b][byte / 4], scale[b][i], byte % 4);
-        } else {
-          const int half = i * T::kPartBytes / 2 + pair;
-          x[b][i] = read_pair<8>(v[b][half / 2], scale[b][i], half % 2);
-        }
+    for (int i = 0; i < 4; ++i) {
+      if constexpr (kBits == 4) {
+        const int byte = i * T::kPartBytes + pair;       // of the lane's codes
+        x[i] = read_pair<4>(v[byte / 4], scale[i], byte % 4);
+      } else {
+        const int half = i * T::kPartBytes / 2 + pair;
+        x[i] = read_pair<8>(v[half / 2], scale[i], half % 2);
       }
-    u32x4 lo, hi;
+    }
 #pragma unroll
-    for (int b = 0; b < 2; ++b)
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        lo[2 * b + i] = __builtin_amdgcn_perm(x[b][2 * i + 1], x[b][2 * i], 0x05040100u);
-        hi[2 * b + i] = __builtin_amdgcn_perm(x[b][2 * i + 1], x[b][2 * i], 0x07060302u);
-      }
-    f[0] = __builtin_bit_cast(bf16x8, lo);
-    f[1] = __builtin_bit_cast(bf16x8, hi);
+    for (int i = 0; i < 2; ++i) {
+      f[0][i] = __builtin_amdgcn_perm(x[2 * i + 1], x[2 * i], 0x05040100u);
+      f[1][i] = __builtin_amdgcn_perm(x[2 * i + 1], x[2 * i], 0x07060302u);
+    }
   }
 
-  __device__ __forceinline__ void value_scales(float (&scale)[2][4]) const {
-#pragma unroll
-    for (int b = 0; b < 2; ++b) {
-      scale[b][0] = __builtin_bit_cast(float, (vs[b] & 0xffu) << 23);
-      scale[b][1] = __builtin_bit_cast(float, (vs[b] & 0xff00u) << 15);
-      scale[b][2] = __builtin_bit_cast(float, (vs[b] & 0xff0000u) << 7);
-      scale[b][3] = __builtin_bit_cast(float, (vs[b] & 0xff000000u) >> 1);
-    }
+  __device__ __forceinline__ void value_scales(float (&scale)[4]) const {
+    scale[0] = __builtin_bit_cast(float, (vs & 0xffu) << 23);
+    scale[1] = __builtin_bit_cast(float, (vs & 0xff00u) << 15);
+    scale[2] = __builtin_bit_cast(float, (vs & 0xff0000u) << 7);
+    scale[3] = __builtin_bit_cast(float, (vs & 0xff000000u) >> 1);
+  }
+};
+
+// 32 keys: two blocks, whose halves of a V^T fragment make one
+template <int D, int kBits>
+struct Unit {
+  Block<D, kBits> b[2];
+  __device__ __forceinline__ void load(const uint8_t* base, size_t stride, int id0, int id1, int lane) {
+    b[0].load(base, stride, id0, lane);
+    b[1].load(base, stride, id1, lane);
+  }
+  __device__ __forceinline__ void cut_values(int n, int lane) {
+    b[0].cut_values(n, lane);
+    b[1].cut_values(n - 16, lane);
   }
 };
 
 // ---------------------------------------------------------------------------
 // The softmax of kTiles x 16 rows over the keys seen so far: lane l holds, of row l & 15 of every
 // tile, O's features D / 4 qd + D / 16 r + t in o[t][r], and its own keys' share of l.
-template <int D, int kBits, int kTiles>
+template <int D, int kTiles>
 struct Softmax {
   f32x4 o[kTiles][D / 16];
   float m[kTiles], l[kTiles];
@@ -323,65 +321,94 @@ struct Softmax {
     }
   }
 
-  // The unit's 32 keys; of them a row of tile x sees the first seen[x] (masked: some row may not
-  // see all).
-  __device__ __forceinline__ void add(const Unit<D, kBits>& u, const Rows16<D, kBits> (&rows)[kTiles], float c,
-                                      bool masked, const int (&seen)[kTiles], int lane) {
-    const int qd = lane >> 4;
-    bf16x8 p[kTiles];
+  // Weights p of tile x's logits s, of kBlocks blocks (two to a fragment); rescales what is there if
+  // a logit is too far above m for them
+  template <int kBlocks>
+  __device__ __forceinline__ void weigh(int x, const f32x4 (&s)[kBlocks], float c, bf16x8 (&p)[kBlocks / 2]) {
+    float mc = m[x] * c, sum = 0.f;
+    float e[kBlocks][4];
 #pragma unroll
-    for (int x = 0; x < kTiles; ++x) {
-      f32x4 s[2];
+    for (int b = 0; b < kBlocks; ++b)
 #pragma unroll
-      for (int b = 0; b < 2; ++b) s[b] = u.logits(b, rows[x]);
-      if (masked) {
-#pragma unroll
-        for (int b = 0; b < 2; ++b)
-#pragma unroll
-          for (int r = 0; r < 4; ++r) s[b][r] = 16 * b + 4 * qd + r < seen[x] ? s[b][r] : -INFINITY;
+      for (int r = 0; r < 4; ++r) {
+        e[b][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][r], c, -mc));
+        sum += e[b][r];
       }
-      float top = fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3]));
-      top = fmaxf(top, fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3])));
-      if (__builtin_amdgcn_ballot_w64(__builtin_fmaf(top, c, -m[x] * c) > kLazy)) {
-        const float m_new = fmaxf(m[x], quad_max(top));
-        const float alpha = __builtin_amdgcn_exp2f((m[x] - m_new) * c);
-        m[x] = m_new;
-        l[x] *= alpha;
+    // (their sum finds a weight that is too large as well as their maximum does, and is needed)
+    if (__builtin_amdgcn_ballot_w64(sum > kLargeSum)) {
+      float top = s[0][0];
 #pragma unroll
-        for (int t = 0; t < D / 16; ++t) o[x][t] *= alpha;
-      }
-      const float mc = m[x] * c;
+      for (int b = 0; b < kBlocks; ++b)
 #pragma unroll
-      for (int b = 0; b < 2; ++b)
+        for (int r = 0; r < 4; ++r) top = fmaxf(top, s[b][r]);
+      const float m_new = fmaxf(m[x], quad_max(top));
+      const float alpha = __builtin_amdgcn_exp2f((m[x] - m_new) * c);
+      m[x] = m_new;
+      mc = m_new * c;
+      l[x] *= alpha;
+#pragma unroll
+      for (int t = 0; t < D / 16; ++t) o[x][t] *= alpha;
+      sum = 0.f;
+#pragma unroll
+      for (int b = 0; b < kBlocks; ++b)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][r], c, -mc));
-          // (rounded to bf16 for the product with V; the sum takes it unrounded)
-          p[x][4 * b + r] = (__bf16)e;
-          l[x] += e;
+          e[b][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][r], c, -mc));
+          sum += e[b][r];
         }
     }
-    float scale[2][4];
-    u.value_scales(scale);
+    l[x] += sum;
+    // (rounded to bf16 for the product with V; the sum takes them unrounded)
 #pragma unroll
-    for (int t = 0; t < D / 16; t += 2) {
-      bf16x8 f[2];
-      u.values(t / 2, scale, f);
+    for (int b = 0; b < kBlocks; ++b)
 #pragma unroll
-      for (int x = 0; x < kTiles; ++x) {
-        o[x][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f[0], p[x], o[x][t], 0, 0, 0);
-        o[x][t + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f[1], p[x], o[x][t + 1], 0, 0, 0);
-      }
-    }
+      for (int r = 0; r < 4; ++r) p[b / 2][4 * (b % 2) + r] = (__bf16)e[b][r];
   }
 };
 
+// Logits of keys that a row does not see: of a block's keys it sees the first `seen`
+__device__ __forceinline__ void mask(f32x4& s, int seen, int lane) {
+#pragma unroll
+  for (int r = 0; r < 4; ++r) s[r] = 4 * (lane >> 4) + r < seen ? s[r] : -INFINITY;
+}
+
+// A unit's keys added to one tile of rows, V converted as it is needed (decode); of the keys the
+// rows see the first `seen`.
+template <int D, int kBits>
+__device__ __forceinline__ void add_unit(Softmax<D, 1>& soft, const Unit<D, kBits>& u, const Rows16<D, kBits>& rows,
+                                         float c, int seen, int lane) {
+  f32x4 s[2];
+#pragma unroll
+  for (int b = 0; b < 2; ++b) s[b] = u.b[b].logits(rows);
+  if (seen < kUnitKeys) {
+#pragma unroll
+    for (int b = 0; b < 2; ++b) mask(s[b], seen - 16 * b, lane);
+  }
+  bf16x8 p[1];
+  soft.template weigh<2>(0, s, c, p);
+  float scale[2][4];
+#pragma unroll
+  for (int b = 0; b < 2; ++b) u.b[b].value_scales(scale[b]);
+#pragma unroll
+  for (int t = 0; t < D / 16; t += 2) {
+    u32x2 f[2][2];
+#pragma unroll
+    for (int b = 0; b < 2; ++b) u.b[b].values(t / 2, scale[b], f[b]);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const u32x4 a = {f[0][i][0], f[0][i][1], f[1][i][0], f[1][i][1]};
+      soft.o[0][t + i] =
+          __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), p[0], soft.o[0][t + i], 0, 0, 0);
+    }
+  }
+}
+
 // 8 features of a lane's O (its r-th run of D / 16, at D = 64 two of them) as bf16
 template <int D>
-__device__ __forceinline__ bf16x8 rounded8(const f32x4 (&o)[D / 16], int i, float l) {
+__device__ __forceinline__ bf16x8 rounded8(const f32x4 (&o)[D / 16], int i, float inv_l) {
   bf16x8 x;
 #pragma unroll
-  for (int e = 0; e < 8; ++e) x[e] = (__bf16)(o[e % (D / 16)][8 * i / (D / 16) + e / (D / 16)] / l);
+  for (int e = 0; e < 8; ++e) x[e] = (__bf16)(o[e % (D / 16)][8 * i / (D / 16) + e / (D / 16)] * inv_l);
   return x;
 }
 
@@ -451,9 +478,9 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 4 : 3) void quant_decode_kernel
     left -= xe - x;
     const ScalarInts table = (ScalarInts)(p.block_tables + (size_t)r * p.max_blocks_per_seq);
     const int last = (len - 1) / kBlock;
-    Rows16<D, kBits> rows[1];
-    rows[0].load(j < p.group ? p.q + ((size_t)r * p.num_q_heads + g * p.group + j) * D : nullptr, lane);
-    Softmax<D, kBits, 1> soft;
+    Rows16<D, kBits> rows;
+    rows.load(j < p.group ? p.q + ((size_t)r * p.num_q_heads + g * p.group + j) * D : nullptr, lane);
+    Softmax<D, 1> soft;
     soft.reset(lowest);
     Unit<D, kBits> cur, nxt;
     int y = x + wave;
@@ -473,10 +500,9 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 4 : 3) void quant_decode_kernel
         nxt.load(base, stride, id0, id1, lane);
         if (y + 2 * kWaves < xe) ids_of(y + 2 * kWaves);
       }
-      const int seen[1] = {len - y * kUnitKeys};
-      const bool masked = seen[0] < kUnitKeys;
-      if (masked) cur.cut_values(seen[0], lane);
-      soft.add(cur, rows, c, masked, seen, lane);
+      const int seen = len - y * kUnitKeys;
+      if (seen < kUnitKeys) cur.cut_values(seen, lane);
+      add_unit(soft, cur, rows, c, seen, lane);
     }
     const float l = quad_sum(soft.l[0]);
     if (j < p.group) {
@@ -553,16 +579,30 @@ __global__ __launch_bounds__(kMergeThreads) void quant_decode_merge_kernel(Quant
 
 // ---------------------------------------------------------------------------
 // Prefill.  Rows of a KV head are (token, query head of it), heads fastest; a wave takes 32 of
-// them, a work-group 128, which its waves' loads of the same keys share in the L1 cache.  Part
-// `part` of the keys that a tile's rows see is one work-group's; several leave partial results.
+// them, a work-group 128.  Its steps are 64 keys: each wave reads one of the four blocks ahead into
+// registers, and a step later leaves it in LDS as all waves then take it, K's codes as
+// they are, V as bf16 fragments, so that each conversion is done once for 128 rows.  A step's
+// buffer is written while the other one is read: one barrier a step.  Several parts of a tile's
+// keys on as many work-groups leave partial results.
 
 constexpr int kRowTiles = 2;
 constexpr int kWaveRows = 16 * kRowTiles;
 constexpr int kTileRows = kWaves * kWaveRows;
+constexpr int kStepBlocks = kWaves;
+constexpr int kStepKeys = 16 * kStepBlocks;
+
+template <int D, int kBits>
+struct PrefillLds {
+  // lane by lane what Block holds of K, and V^T fragments
+  u32x4 k[2][kStepBlocks][Block<D, kBits>::kKWords / 4][64];
+  int ks[2][kStepBlocks][64];
+  u32x4 v[2][kStepBlocks / 2][D / 16][64];
+};
 
 template <int D, int kBits>
 __global__ __launch_bounds__(kThreads, 2) void quant_prefill_kernel(QuantParams p) {
   using T = QuantTile<D, kBits>;
+  __shared__ PrefillLds<D, kBits> sm;
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const ScalarInts prefix = (ScalarInts)p.lens;
@@ -572,26 +612,58 @@ __global__ __launch_bounds__(kThreads, 2) void quant_prefill_kernel(QuantParams 
   at /= p.num_kv_heads;
   const int part = at % p.parts;
   at /= p.parts;
-  const int r = at % p.batch;
-  const int tile = p.tiles - 1 - at / p.batch;      // those with the most keys first
+  // an invocation's tiles one after another, those with the most keys first: the work-groups that
+  // run at one time read few sequences' keys, which their L2 holds
+  const int tile = p.tiles - 1 - at % p.tiles;
+  const int r = at / p.tiles;
   const int q0 = cu[r];
   const int tokens = cu[r + 1] - q0;
   const long long n_rows = (long long)tokens * p.group;
-  const long long row0 = (long long)tile * kTileRows + wave * kWaveRows;
-  if (row0 >= n_rows) return;
+  const long long tile0 = (long long)tile * kTileRows;
+  if (tile0 >= n_rows) return;
   const int before = prefix[r];
   const int len = before + tokens;
   // tokens of the wave's first and last row
-  const int t0 = (int)(row0 / p.group);
-  const int t1 = (int)(min(row0 + kWaveRows, n_rows) - 1) / p.group;
-  const int units = units_of(before + t1 + 1);
-  const int x0 = (int)((long long)units * part / p.parts);
-  const int xe = (int)((long long)units * (part + 1) / p.parts);
+  const long long row0 = tile0 + wave * kWaveRows;
+  const bool idle = row0 >= n_rows;
+  const int t0 = (int)(min(row0, n_rows - 1) / p.group);
+  const int t1 = (int)((min(row0 + kWaveRows, n_rows) - 1) / p.group);
+  // steps of the keys that the tile's rows see, this part's
+  const int tile_t1 = (int)((min(tile0 + kTileRows, n_rows) - 1) / p.group);
+  const int steps = (before + tile_t1 + kStepKeys) / kStepKeys;
+  const int x0 = (int)((long long)steps * part / p.parts);
+  const int xe = (int)((long long)steps * (part + 1) / p.parts);
 
   const size_t stride = (size_t)p.num_kv_heads * T::kBytes;
   const uint8_t* base = p.pool + (size_t)g * T::kBytes;
   const float c = p.scale_log2;
   const int j = lane & 15;
+  const ScalarInts table = (ScalarInts)(p.block_tables + (size_t)r * p.max_blocks_per_seq);
+  const int last = (len - 1) / kBlock;
+  auto id_of = [&](int step) { return table[min(kStepBlocks * step + wave, last)]; };
+  // the wave's block of a step from registers into the step's buffer
+  Block<D, kBits> block;
+  auto store = [&](int step) __attribute__((always_inline)) {
+    const int buf = step & 1;
+    const int key0 = step * kStepKeys + 16 * wave;
+    if (key0 + 16 > len) block.cut_values(len - key0, lane);
+#pragma unroll
+    for (int i = 0; i < Block<D, kBits>::kKWords / 4; ++i)
+      sm.k[buf][wave][i][lane] = u32x4{block.k[4 * i], block.k[4 * i + 1], block.k[4 * i + 2], block.k[4 * i + 3]};
+    sm.ks[buf][wave][lane] = block.ks;
+    float scale[4];
+    block.value_scales(scale);
+#pragma unroll
+    for (int t = 0; t < D / 16; t += 2) {
+      u32x2 f[2];
+      block.values(t / 2, scale, f);
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+        *(reinterpret_cast<u32x2*>(&sm.v[buf][wave / 2][t + i][lane]) + wave % 2) = f[i];
+    }
+  };
+
+  if (x0 < xe) block.load(base, stride, id_of(x0), lane);
   Rows16<D, kBits> rows[kRowTiles];
   long long q_row[kRowTiles];      // of q and out; negative: none
   int end[kRowTiles];              // keys that the row sees
@@ -603,34 +675,54 @@ __global__ __launch_bounds__(kThreads, 2) void quant_prefill_kernel(QuantParams 
     end[i] = before + min(t, t1) + 1;
     rows[i].load(row < n_rows ? p.q + q_row[i] * D : nullptr, lane);
   }
-  Softmax<D, kBits, kRowTiles> soft;
+  Softmax<D, kRowTiles> soft;
   soft.reset(lowest_reference(c));
-  const ScalarInts table = (ScalarInts)(p.block_tables + (size_t)r * p.max_blocks_per_seq);
-  const int last = (len - 1) / kBlock;
-  int id0 = 0, id1 = 0;
-  auto ids_of = [&](int unit) {
-    id0 = table[kUnitBlocks * unit];
-    id1 = table[min(kUnitBlocks * unit + 1, last)];
-  };
-  Unit<D, kBits> cur, nxt;
   if (x0 < xe) {
-    ids_of(x0);
-    nxt.load(base, stride, id0, id1, lane);
-    if (x0 + 1 < xe) ids_of(x0 + 1);
+    store(x0);
+    if (x0 + 1 < xe) block.load(base, stride, id_of(x0 + 1), lane);
   }
   for (int x = x0; x < xe; ++x) {
-    cur = nxt;
+    const int buf = x & 1;
+    const int key0 = x * kStepKeys;
+    // step x is in LDS, and no wave reads the other buffer any more
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
     if (x + 1 < xe) {
-      nxt.load(base, stride, id0, id1, lane);
-      if (x + 2 < xe) ids_of(x + 2);
+      store(x + 1);
+      if (x + 2 < xe) block.load(base, stride, id_of(x + 2), lane);
     }
-    const int key0 = x * kUnitKeys;
-    const bool masked = key0 + kUnitKeys > before + t0 + 1;
-    int seen[kRowTiles];
+    if (idle || key0 > before + t1) continue;
+    f32x4 s[kRowTiles][kStepBlocks];
 #pragma unroll
-    for (int i = 0; i < kRowTiles; ++i) seen[i] = end[i] - key0;
-    if (key0 + kUnitKeys > len) cur.cut_values(len - key0, lane);
-    soft.add(cur, rows, c, masked, seen, lane);
+    for (int b = 0; b < kStepBlocks; ++b) {
+      Block<D, kBits> k;
+#pragma unroll
+      for (int i = 0; i < Block<D, kBits>::kKWords / 4; ++i) {
+        const u32x4 w = sm.k[buf][b][i][lane];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) k.k[4 * i + e] = w[e];
+      }
+      k.ks = sm.ks[buf][b][lane];
+#pragma unroll
+      for (int i = 0; i < kRowTiles; ++i) s[i][b] = k.logits(rows[i]);
+    }
+    if (key0 + kStepKeys > before + t0 + 1) {
+#pragma unroll
+      for (int i = 0; i < kRowTiles; ++i)
+#pragma unroll
+        for (int b = 0; b < kStepBlocks; ++b) mask(s[i][b], end[i] - key0 - 16 * b, lane);
+    }
+    bf16x8 w[kRowTiles][kStepBlocks / 2];
+#pragma unroll
+    for (int i = 0; i < kRowTiles; ++i) soft.template weigh<kStepBlocks>(i, s[i], c, w[i]);
+#pragma unroll
+    for (int u = 0; u < kStepBlocks / 2; ++u)
+#pragma unroll
+      for (int t = 0; t < D / 16; ++t) {
+        const bf16x8 f = __builtin_bit_cast(bf16x8, sm.v[buf][u][t][lane]);
+#pragma unroll
+        for (int i = 0; i < kRowTiles; ++i)
+          soft.o[i][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f, w[i][u], soft.o[i][t], 0, 0, 0);
+      }
   }
 #pragma unroll
   for (int i = 0; i < kRowTiles; ++i) {
@@ -640,7 +732,7 @@ __global__ __launch_bounds__(kThreads, 2) void quant_prefill_kernel(QuantParams 
     if (p.parts == 1) {
 #pragma unroll
       for (int k = 0; k < D / 32; ++k)
-        *reinterpret_cast<bf16x8*>(p.out + q_row[i] * D + d0 + 8 * k) = rounded8<D>(soft.o[i], k, l);
+        *reinterpret_cast<bf16x8*>(p.out + q_row[i] * D + d0 + 8 * k) = rounded8<D>(soft.o[i], k, 1.f / l);
     } else {
       const size_t to = (size_t)part * p.total_q * p.num_q_heads + q_row[i];
 #pragma unroll
@@ -752,8 +844,8 @@ hipError_t launch_quant_decode(const QuantAttnLaunch& a, const QuantDecodeGeomet
 }
 
 constexpr int kPrefillMaxParts = 16;
-// fewest units of a part
-constexpr int kPrefillPartUnits = 4;
+// fewest steps of a part of the longest sequence
+constexpr int kPrefillPartSteps = 2;
 
 QuantPrefillGeometry quant_prefill_geometry(int batch, int total_q, int max_q_len, int max_kv_len,
                                             int num_q_heads, int num_kv_heads, int head_dim, int cus) {
@@ -765,8 +857,8 @@ QuantPrefillGeometry quant_prefill_geometry(int batch, int total_q, int max_q_le
   double tiles = (double)geo.tiles * batch * num_kv_heads;
   if (bound < tiles) tiles = bound;
   long long parts = tiles > 0 ? (long long)(2 * cus / tiles) : 1;
-  const long long units = (max_kv_len + 31LL) / 32;
-  if (parts > units / kPrefillPartUnits) parts = units / kPrefillPartUnits;
+  const long long steps = (max_kv_len + kStepKeys - 1LL) / kStepKeys;
+  if (parts > steps / kPrefillPartSteps) parts = steps / kPrefillPartSteps;
   if (parts > kPrefillMaxParts) parts = kPrefillMaxParts;
   geo.parts = parts < 1 ? 1 : (int)parts;
   const double grid = (double)geo.tiles * batch * num_kv_heads * geo.parts;
