@@ -18,9 +18,9 @@
 //     the largest, where 4-bit times 8-bit ones are exact to fp32's 5e-8.)
 //   * V is converted to bf16, two features of a key at a time, which two byte permutes then
 //     pair up by keys.
-// The running maximum that the exponentials are relative to follows the logits only when the
-// weights of a lane's keys add up to more than 256: bf16 holds 256 as well as 1, and most steps
-// rescale nothing, look for no maximum and exchange nothing between lanes.
+// The running maximum that the exponentials are relative to follows the logits only when a weight
+// would be above 2^8: bf16 holds 256 as well as 1, and most steps rescale nothing and exchange
+// nothing between lanes.
 #include "decode_common.h"
 #include "internal.h"
 #include "quant_tile.h"
@@ -36,7 +36,10 @@ typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kWaves = 4;             // of a work-group, both kernels
 constexpr int kThreads = 64 * kWaves;
-constexpr float kLargeSum = 256.f;    // of a lane's weights of a step
+constexpr float kLazy = 8.f;          // log2 of what a weight may exceed 1 by
+// The reference of rows that have seen no key: about the lowest number, so that masked logits
+// (-inf) weigh 0 and not NaN, and every other one is above it
+constexpr float kLowest = -0x1.fffffp127f;
 
 struct QuantParams {
   const uint16_t* q;
@@ -202,7 +205,11 @@ struct Block {
 
   // Block `id` of the KV head whose tiles `base` starts at, `stride` bytes apart.  The
   // descriptor of a negative id is empty: zeros, and nothing outside the pool is read.
-  __device__ __forceinline__ void load(const uint8_t* base, size_t stride, int id, int lane) {
+  __device__ __forceinline__ static __amdgpu_buffer_rsrc_t tile(const uint8_t* base, size_t stride, int id) {
+    return __builtin_amdgcn_make_buffer_rsrc((void*)(base + (size_t)id * stride), (short)0, id < 0 ? 0 : T::kBytes,
+                                             kRawBufferWord3);
+  }
+  __device__ __forceinline__ void load_keys(__amdgpu_buffer_rsrc_t rs, int lane) {
     const int key = lane & 15, qd = lane >> 4;
     int k_off, ks_off;
     if constexpr (kBits == 4) {
@@ -213,14 +220,13 @@ struct Block {
       k_off = key * T::kRowBytes + D / 4 * qd;
       ks_off = T::kKScales + key * T::kGroups + qd * T::kGroups / 4;
     }
-    const int v_off = T::kV + (key * 16 + 4 * qd) * T::kPartBytes;
-    const int vs_off = T::kVScales + key * T::kPart / kScaleGroup * 16 + 4 * qd;
-    const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(
-        (void*)(base + (size_t)id * stride), (short)0, id < 0 ? 0 : T::kBytes, kRawBufferWord3);
     load_words(k, rs, k_off);
-    load_words(v, rs, v_off);
     ks = __builtin_amdgcn_raw_buffer_load_b8(rs, ks_off, 0, 0);
-    vs = __builtin_amdgcn_raw_buffer_load_b32(rs, vs_off, 0, 0);
+  }
+  __device__ __forceinline__ void load_values(__amdgpu_buffer_rsrc_t rs, int lane) {
+    const int c = lane & 15, qd = lane >> 4;
+    load_words(v, rs, T::kV + (c * 16 + 4 * qd) * T::kPartBytes);
+    vs = __builtin_amdgcn_raw_buffer_load_b32(rs, T::kVScales + c * T::kPart / kScaleGroup * 16 + 4 * qd, 0, 0);
   }
 
   // What stands behind `n` keys of the block is not the sequence's: V there becomes zero (its
@@ -294,8 +300,12 @@ template <int D, int kBits>
 struct Unit {
   Block<D, kBits> b[2];
   __device__ __forceinline__ void load(const uint8_t* base, size_t stride, int id0, int id1, int lane) {
-    b[0].load(base, stride, id0, lane);
-    b[1].load(base, stride, id1, lane);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const __amdgpu_buffer_rsrc_t rs = Block<D, kBits>::tile(base, stride, i ? id1 : id0);
+      b[i].load_keys(rs, lane);
+      b[i].load_values(rs, lane);
+    }
   }
   __device__ __forceinline__ void cut_values(int n, int lane) {
     b[0].cut_values(n, lane);
@@ -305,64 +315,62 @@ struct Unit {
 
 // ---------------------------------------------------------------------------
 // The softmax of kTiles x 16 rows over the keys seen so far: lane l holds, of row l & 15 of every
-// tile, O's features D / 4 qd + D / 16 r + t in o[t][r], and its own keys' share of l.
+// tile, O's features D / 4 qd + D / 16 r + t in o[t][r], and its own keys' share of l.  Weights are
+// 2^(s c - m) with m a whole number, so that moving m is exact.
 template <int D, int kTiles>
 struct Softmax {
   f32x4 o[kTiles][D / 16];
   float m[kTiles], l[kTiles];
 
-  __device__ __forceinline__ void reset(float lowest) {
+  __device__ __forceinline__ void reset() {
 #pragma unroll
     for (int x = 0; x < kTiles; ++x) {
 #pragma unroll
       for (int t = 0; t < D / 16; ++t) o[x][t] = f32x4{};
-      m[x] = lowest;
+      m[x] = kLowest;
       l[x] = 0.f;
     }
   }
 
-  // Weights p of tile x's logits s, of kBlocks blocks (two to a fragment); rescales what is there if
-  // a logit is too far above m for them
-  template <int kBlocks>
-  __device__ __forceinline__ void weigh(int x, const f32x4 (&s)[kBlocks], float c, bf16x8 (&p)[kBlocks / 2]) {
-    float mc = m[x] * c, sum = 0.f;
-    float e[kBlocks][4];
+  // Where a logit of the two blocks' s is too far above m for its weight: m up to the largest, and
+  // what there is so far, with the weights p that are not in O yet, relative to that
+  __device__ __forceinline__ void follow(const f32x4 (&s)[kTiles][2], float c, bf16x8 (&p)[kTiles]) {
+    float top[kTiles];
+    bool far = false;
 #pragma unroll
-    for (int b = 0; b < kBlocks; ++b)
+    for (int x = 0; x < kTiles; ++x) {
+      top[x] = fmaxf(fmaxf(s[x][0][0], s[x][0][1]), s[x][0][2]);
+      top[x] = fmaxf(fmaxf(top[x], s[x][0][3]), s[x][1][0]);
+      top[x] = fmaxf(fmaxf(top[x], s[x][1][1]), s[x][1][2]);
+      top[x] = fmaxf(top[x], s[x][1][3]);
+      far |= __builtin_fmaf(top[x], c, -m[x]) > kLazy;
+    }
+    if (__builtin_amdgcn_ballot_w64(far) == 0) return;
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        e[b][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][r], c, -mc));
-        sum += e[b][r];
-      }
-    // (their sum finds a weight that is too large as well as their maximum does, and is needed)
-    if (__builtin_amdgcn_ballot_w64(sum > kLargeSum)) {
-      float top = s[0][0];
-#pragma unroll
-      for (int b = 0; b < kBlocks; ++b)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) top = fmaxf(top, s[b][r]);
-      const float m_new = fmaxf(m[x], quad_max(top));
-      const float alpha = __builtin_amdgcn_exp2f((m[x] - m_new) * c);
+    for (int x = 0; x < kTiles; ++x) {
+      const float m_new = fmaxf(m[x], ceilf(quad_max(top[x]) * c));
+      const float alpha = __builtin_amdgcn_exp2f(m[x] - m_new);
       m[x] = m_new;
-      mc = m_new * c;
       l[x] *= alpha;
 #pragma unroll
       for (int t = 0; t < D / 16; ++t) o[x][t] *= alpha;
-      sum = 0.f;
 #pragma unroll
-      for (int b = 0; b < kBlocks; ++b)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          e[b][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][r], c, -mc));
-          sum += e[b][r];
-        }
+      for (int i = 0; i < 8; ++i) p[x][i] = (__bf16)((float)p[x][i] * alpha);
     }
-    l[x] += sum;
-    // (rounded to bf16 for the product with V; the sum takes them unrounded)
+  }
+
+  // Tile x's logits as weights, rounded to bf16 for the product with V; l takes them unrounded
+  __device__ __forceinline__ bf16x8 weigh(int x, const f32x4 (&s)[2], float c) {
+    bf16x8 p;
 #pragma unroll
-    for (int b = 0; b < kBlocks; ++b)
+    for (int b = 0; b < 2; ++b)
 #pragma unroll
-      for (int r = 0; r < 4; ++r) p[b / 2][4 * (b % 2) + r] = (__bf16)e[b][r];
+      for (int r = 0; r < 4; ++r) {
+        const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][r], c, -m[x]));
+        l[x] += e;
+        p[4 * b + r] = (__bf16)e;
+      }
+    return p;
   }
 };
 
@@ -377,15 +385,16 @@ __device__ __forceinline__ void mask(f32x4& s, int seen, int lane) {
 template <int D, int kBits>
 __device__ __forceinline__ void add_unit(Softmax<D, 1>& soft, const Unit<D, kBits>& u, const Rows16<D, kBits>& rows,
                                          float c, int seen, int lane) {
-  f32x4 s[2];
+  f32x4 s[1][2];
 #pragma unroll
-  for (int b = 0; b < 2; ++b) s[b] = u.b[b].logits(rows);
+  for (int b = 0; b < 2; ++b) s[0][b] = u.b[b].logits(rows);
   if (seen < kUnitKeys) {
 #pragma unroll
-    for (int b = 0; b < 2; ++b) mask(s[b], seen - 16 * b, lane);
+    for (int b = 0; b < 2; ++b) mask(s[0][b], seen - 16 * b, lane);
   }
-  bf16x8 p[1];
-  soft.template weigh<2>(0, s, c, p);
+  bf16x8 p[1] = {};
+  soft.follow(s, c, p);
+  p[0] = soft.weigh(0, s[0], c);
   float scale[2][4];
 #pragma unroll
   for (int b = 0; b < 2; ++b) u.b[b].value_scales(scale[b]);
@@ -469,7 +478,6 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 4 : 3) void quant_decode_kernel
   const uint8_t* base = p.pool + (size_t)g * T::kBytes;
   const int j = lane & 15;
   const float c = p.scale_log2;
-  const float lowest = lowest_reference(c);
   for (;;) {
     const int len = lens[r];
     const int n = units_of(len);
@@ -481,7 +489,7 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 4 : 3) void quant_decode_kernel
     Rows16<D, kBits> rows;
     rows.load(j < p.group ? p.q + ((size_t)r * p.num_q_heads + g * p.group + j) * D : nullptr, lane);
     Softmax<D, 1> soft;
-    soft.reset(lowest);
+    soft.reset();
     Unit<D, kBits> cur, nxt;
     int y = x + wave;
     int id0 = 0, id1 = 0;
@@ -524,7 +532,7 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 4 : 3) void quant_decode_kernel
       f32x4 acc = f32x4{};
 #pragma unroll
       for (int k = 0; k < kWaves; ++k) {
-        const float wt = __builtin_amdgcn_exp2f((sm.ml[k][hj].x - m) * c);
+        const float wt = __builtin_amdgcn_exp2f(sm.ml[k][hj].x - m);
         den = __builtin_fmaf(wt, sm.ml[k][hj].y, den);
         const f32x4 o = *reinterpret_cast<const f32x4*>(&sm.o[k][hj][d]);
 #pragma unroll
@@ -569,7 +577,7 @@ __global__ __launch_bounds__(kMergeThreads) void quant_decode_merge_kernel(Quant
   if (pieces == 1) return;
   const size_t first = ((size_t)g * p.rows + r + w0) * p.group;
   merge_pieces<D>(
-      p.ws_o, p.ws_ml, p.group, p.scale_log2, [&](int) { return pieces; },
+      p.ws_o, p.ws_ml, p.group, 1.f, [&](int) { return pieces; },
       [&](int hj, int k) { return first + (size_t)k * p.group + hj; },
       [&](int hj, int d, bf16x4 o) {
         *reinterpret_cast<uint2*>(p.out + ((size_t)r * p.num_q_heads + g * p.group + hj) * D + d) =
@@ -591,6 +599,8 @@ constexpr int kTileRows = kWaves * kWaveRows;
 constexpr int kStepBlocks = kWaves;
 constexpr int kStepKeys = 16 * kStepBlocks;
 
+// What a step's buffer holds: step x computes the logits of blocks 4 x + 2 .. 4 x + 5 and adds the
+// values of blocks 4 x - 2 .. 4 x + 1.
 template <int D, int kBits>
 struct PrefillLds {
   // lane by lane what Block holds of K, and V^T fragments
@@ -625,7 +635,6 @@ __global__ __launch_bounds__(kThreads, 2) void quant_prefill_kernel(QuantParams 
   const int len = before + tokens;
   // tokens of the wave's first and last row
   const long long row0 = tile0 + wave * kWaveRows;
-  const bool idle = row0 >= n_rows;
   const int t0 = (int)(min(row0, n_rows - 1) / p.group);
   const int t1 = (int)((min(row0 + kWaveRows, n_rows) - 1) / p.group);
   // steps of the keys that the tile's rows see, this part's
@@ -640,17 +649,24 @@ __global__ __launch_bounds__(kThreads, 2) void quant_prefill_kernel(QuantParams 
   const int j = lane & 15;
   const ScalarInts table = (ScalarInts)(p.block_tables + (size_t)r * p.max_blocks_per_seq);
   const int last = (len - 1) / kBlock;
-  auto id_of = [&](int step) { return table[min(kStepBlocks * step + wave, last)]; };
-  // the wave's block of a step from registers into the step's buffer
+  // The wave's blocks of a step: in registers, and a step later in the step's buffer.  Blocks outside
+  // the part are read but not used; before its beginning (where weights are 0) V is zeros.
   Block<D, kBits> block;
-  auto store = [&](int step) __attribute__((always_inline)) {
-    const int buf = step & 1;
-    const int key0 = step * kStepKeys + 16 * wave;
-    if (key0 + 16 > len) block.cut_values(len - key0, lane);
+  auto key_tile = [&](int step) {
+    return Block<D, kBits>::tile(base, stride, table[max(0, min(kStepBlocks * step + 2 + wave, last))]);
+  };
+  auto value_tile = [&](int step) {
+    const int b = kStepBlocks * step - 2 + wave;
+    return Block<D, kBits>::tile(base, stride, b < kStepBlocks * x0 ? -1 : table[min(b, last)]);
+  };
+  auto store_keys = [&](int step) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < Block<D, kBits>::kKWords / 4; ++i)
-      sm.k[buf][wave][i][lane] = u32x4{block.k[4 * i], block.k[4 * i + 1], block.k[4 * i + 2], block.k[4 * i + 3]};
-    sm.ks[buf][wave][lane] = block.ks;
+      sm.k[step & 1][wave][i][lane] =
+          u32x4{block.k[4 * i], block.k[4 * i + 1], block.k[4 * i + 2], block.k[4 * i + 3]};
+    sm.ks[step & 1][wave][lane] = block.ks;
+  };
+  auto store_values = [&](int step) __attribute__((always_inline)) {
     float scale[4];
     block.value_scales(scale);
 #pragma unroll
@@ -659,11 +675,15 @@ __global__ __launch_bounds__(kThreads, 2) void quant_prefill_kernel(QuantParams 
       block.values(t / 2, scale, f);
 #pragma unroll
       for (int i = 0; i < 2; ++i)
-        *(reinterpret_cast<u32x2*>(&sm.v[buf][wave / 2][t + i][lane]) + wave % 2) = f[i];
+        *(reinterpret_cast<u32x2*>(&sm.v[step & 1][wave / 2][t + i][lane]) + wave % 2) = f[i];
     }
   };
+  auto cut_values = [&](int step) __attribute__((always_inline)) {
+    const int n = len - step * kStepKeys + 16 * (2 - wave);
+    if (n < 16) block.cut_values(n, lane);
+  };
 
-  if (x0 < xe) block.load(base, stride, id_of(x0), lane);
+  if (x0 < xe) block.load_keys(key_tile(x0 - 1), lane);
   Rows16<D, kBits> rows[kRowTiles];
   long long q_row[kRowTiles];      // of q and out; negative: none
   int end[kRowTiles];              // keys that the row sees
@@ -676,53 +696,76 @@ __global__ __launch_bounds__(kThreads, 2) void quant_prefill_kernel(QuantParams 
     rows[i].load(row < n_rows ? p.q + q_row[i] * D : nullptr, lane);
   }
   Softmax<D, kRowTiles> soft;
-  soft.reset(lowest_reference(c));
-  if (x0 < xe) {
-    store(x0);
-    if (x0 + 1 < xe) block.load(base, stride, id_of(x0 + 1), lane);
-  }
-  for (int x = x0; x < xe; ++x) {
-    const int buf = x & 1;
-    const int key0 = x * kStepKeys;
-    // step x is in LDS, and no wave reads the other buffer any more
-    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-    if (x + 1 < xe) {
-      store(x + 1);
-      if (x + 2 < xe) block.load(base, stride, id_of(x + 2), lane);
-    }
-    if (idle || key0 > before + t1) continue;
-    f32x4 s[kRowTiles][kStepBlocks];
+  soft.reset();
+  auto barrier = [&]() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); };
+  // of the buffer's blocks 2 half and 2 half + 1
+  auto logits = [&](int step, int half, f32x4 (&s)[kRowTiles][2]) __attribute__((always_inline)) {
 #pragma unroll
-    for (int b = 0; b < kStepBlocks; ++b) {
+    for (int b = 0; b < 2; ++b) {
       Block<D, kBits> k;
 #pragma unroll
       for (int i = 0; i < Block<D, kBits>::kKWords / 4; ++i) {
-        const u32x4 w = sm.k[buf][b][i][lane];
+        const u32x4 w = sm.k[step & 1][2 * half + b][i][lane];
 #pragma unroll
         for (int e = 0; e < 4; ++e) k.k[4 * i + e] = w[e];
       }
-      k.ks = sm.ks[buf][b][lane];
+      k.ks = sm.ks[step & 1][2 * half + b][lane];
 #pragma unroll
       for (int i = 0; i < kRowTiles; ++i) s[i][b] = k.logits(rows[i]);
     }
-    if (key0 + kStepKeys > before + t0 + 1) {
+  };
+  auto add_values = [&](int step, int half, const bf16x8 (&w)[kRowTiles]) __attribute__((always_inline)) {
+#pragma unroll
+    for (int t = 0; t < D / 16; ++t) {
+      const bf16x8 f = __builtin_bit_cast(bf16x8, sm.v[step & 1][half][t][lane]);
+#pragma unroll
+      for (int i = 0; i < kRowTiles; ++i)
+        soft.o[i][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f, w[i], soft.o[i][t], 0, 0, 0);
+    }
+  };
+  // Half a step: from the logits s of 32 keys their weights w; beside that the logits of the next
+  // 32 and the values of the last 32
+  auto half_step = [&](int x, int half, f32x4 (&s)[kRowTiles][2], f32x4 (&next)[kRowTiles][2],
+                       bf16x8 (&before_w)[kRowTiles], bf16x8 (&w)[kRowTiles]) __attribute__((always_inline)) {
+    const int key0 = x * kStepKeys + 32 * half;
+    if (key0 + 32 > before + t0 + 1) {
 #pragma unroll
       for (int i = 0; i < kRowTiles; ++i)
 #pragma unroll
-        for (int b = 0; b < kStepBlocks; ++b) mask(s[i][b], end[i] - key0 - 16 * b, lane);
+        for (int b = 0; b < 2; ++b) mask(s[i][b], end[i] - key0 - 16 * b, lane);
     }
-    bf16x8 w[kRowTiles][kStepBlocks / 2];
+    soft.follow(s, c, before_w);
+    logits(x, half, next);
 #pragma unroll
-    for (int i = 0; i < kRowTiles; ++i) soft.template weigh<kStepBlocks>(i, s[i], c, w[i]);
-#pragma unroll
-    for (int u = 0; u < kStepBlocks / 2; ++u)
-#pragma unroll
-      for (int t = 0; t < D / 16; ++t) {
-        const bf16x8 f = __builtin_bit_cast(bf16x8, sm.v[buf][u][t][lane]);
-#pragma unroll
-        for (int i = 0; i < kRowTiles; ++i)
-          soft.o[i][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f, w[i][u], soft.o[i][t], 0, 0, 0);
-      }
+    for (int i = 0; i < kRowTiles; ++i) w[i] = soft.weigh(i, s[i], c);
+    add_values(x, half, before_w);
+  };
+  if (x0 < xe) {
+    f32x4 s0[kRowTiles][2], s1[kRowTiles][2];
+    bf16x8 w0[kRowTiles], w1[kRowTiles] = {};
+    store_keys(x0 - 1);
+    block.load_keys(key_tile(x0), lane);
+    block.load_values(value_tile(x0), lane);
+    barrier();
+    logits(x0 - 1, 1, s0);
+    cut_values(x0);
+    store_keys(x0);
+    store_values(x0);
+    block.load_keys(key_tile(x0 + 1), lane);
+    block.load_values(value_tile(x0 + 1), lane);
+    for (int x = x0; x < xe; ++x) {
+      // step x is in LDS, and no wave reads the other buffer any more
+      barrier();
+      cut_values(x + 1);
+      half_step(x, 0, s0, s1, w1, w0);
+      store_keys(x + 1);
+      store_values(x + 1);
+      block.load_keys(key_tile(x + 2), lane);
+      block.load_values(value_tile(x + 2), lane);
+      half_step(x, 1, s1, s0, w0, w1);
+    }
+    barrier();
+    add_values(xe, 0, w1);
   }
 #pragma unroll
   for (int i = 0; i < kRowTiles; ++i) {
@@ -760,7 +803,7 @@ __global__ __launch_bounds__(kThreads) void quant_prefill_merge_kernel(QuantPara
   f32x4 acc = f32x4{};
   for (int k = 0; k < p.parts; ++k) {
     const float2 ml = *reinterpret_cast<const float2*>(p.ws_ml + 2 * (k * n + row));
-    const float wt = __builtin_amdgcn_exp2f((ml.x - m) * p.scale_log2);
+    const float wt = __builtin_amdgcn_exp2f(ml.x - m);
     const f32x4 o = *reinterpret_cast<const f32x4*>(p.ws_o + (k * n + row) * D + d);
     den = __builtin_fmaf(wt, ml.y, den);
 #pragma unroll
