@@ -280,6 +280,7 @@ hipError_t launch_quant_decode(const QuantAttnLaunch& a, const QuantDecodeGeomet
 
 // Prefill: tiles of query rows, each in `parts` parts of its keys where there are few.
 struct QuantPrefillGeometry {
+  int wave_tiles;               // tiles of 32 rows that a wave takes
   int parts;
   long long tiles;              // of the longest suffix, per (invocation, KV head)
   long long grid;

@@ -18,9 +18,9 @@
 //     the largest, where 4-bit times 8-bit ones are exact to fp32's 5e-8.)
 //   * V is converted to bf16, two features of a key at a time, which two byte permutes then
 //     pair up by keys.
-// The running maximum that the exponentials are relative to follows the logits only when a weight
-// would be above 2^8: bf16 holds 256 as well as 1, and most steps rescale nothing and exchange
-// nothing between lanes.
+// The running maximum that the exponentials are relative to follows the logits only when the
+// weights of a lane's keys add up to more than 2^16: bf16 holds large numbers as well as 1, and most
+// steps rescale nothing, look for no maximum and exchange nothing between lanes.
 #include "decode_common.h"
 #include "internal.h"
 #include "quant_tile.h"
@@ -36,7 +36,7 @@ typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kWaves = 4;             // of a work-group, both kernels
 constexpr int kThreads = 64 * kWaves;
-constexpr float kLazy = 8.f;          // log2 of what a weight may exceed 1 by
+constexpr float kLargeSum = 65536.f;  // of a lane's weights of 32 keys, where their reference moves
 // The reference of rows that have seen no key: about the lowest number, so that masked logits
 // (-inf) weigh 0 and not NaN, and every other one is above it
 constexpr float kLowest = -0x1.fffffp127f;
@@ -173,6 +173,61 @@ struct Rows16<D, 4> {
   }
 };
 
+// 32 rows as the B operand of 32 x 32 products: lane l holds row l & 31, half l >> 5.
+template <int D, int kBits>
+struct Rows32;
+
+template <int D>
+struct Rows32<D, 8> {
+  bf16x8 q[D / 16];
+  __device__ __forceinline__ void load(const uint16_t* row, int lane) {
+    // step s of the contracted index: features (D / 2) half + 8 s .. + 7, as K's lanes take them
+#pragma unroll
+    for (int s = 0; s < D / 16; ++s) {
+      q[s] = bf16x8{};
+      if (row != nullptr) q[s] = *reinterpret_cast<const bf16x8*>(row + D / 2 * (lane >> 5) + 8 * s);
+    }
+  }
+};
+
+template <int D>
+struct Rows32<D, 4> {
+  // of 64 features each the heads, [0], and the rests, [1]
+  i32x8 q[D / 64][2];
+  int scale[D / 64][2];
+  __device__ __forceinline__ void load(const uint16_t* row, int lane) {
+    const int half = lane >> 5;
+#pragma unroll
+    for (int f = 0; f < D / 64; ++f) {
+      // the 8-bit operand's lane holds indices 16 half .. + 15 of both groups of 32
+      u32x4 x[2][2];
+      int byte[2];
+#pragma unroll
+      for (int g = 0; g < 2; ++g) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          x[g][i] = u32x4{};
+          if (row != nullptr) x[g][i] = *reinterpret_cast<const u32x4*>(row + 64 * f + 32 * g + 16 * half + 8 * i);
+        }
+        unsigned top = top_of(x[g]);
+        top = max(top, (unsigned)__shfl_xor((int)top, 32));
+        byte[g] = query_scale(top);
+        int head[4], rest[4];
+        split16(x[g], byte[g] == kNanScale ? 1.f : scale_of(byte[g]), head, rest);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          q[f][0][4 * g + i] = head[i];
+          q[f][1][4 * g + i] = rest[i];
+        }
+      }
+      // and the scale of indices 32 half .. + 31
+      const int b = half ? byte[1] : byte[0];
+      scale[f][0] = b;
+      scale[f][1] = b == kNanScale ? b : b - 4;
+    }
+  }
+};
+
 // ---------------------------------------------------------------------------
 // Keys
 
@@ -287,6 +342,28 @@ struct Block {
     }
   }
 
+  // The codes of half the lane's features, kPart / 2 of each of its keys, in the low bits
+  __device__ __forceinline__ void half_values(int part, uint32_t (&codes)[4]) const {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if constexpr (T::kPartBytes == 8) codes[i] = part ? v[2 * i + 1] : v[2 * i];
+      else if constexpr (T::kPartBytes == 4) codes[i] = v[i] >> (16 * part);
+      else codes[i] = v[i / 2] >> (16 * (i % 2) + 8 * part);
+    }
+  }
+  // Of such codes feature 2 pair, in f[0], and 2 pair + 1: the lane's four keys
+  __device__ __forceinline__ static void fragments(const uint32_t (&codes)[4], int pair, const float (&scale)[4],
+                                                   u32x2 (&f)[2]) {
+    uint32_t x[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = read_pair<kBits>(codes[i], scale[i], pair);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      f[0][i] = __builtin_amdgcn_perm(x[2 * i + 1], x[2 * i], 0x05040100u);
+      f[1][i] = __builtin_amdgcn_perm(x[2 * i + 1], x[2 * i], 0x07060302u);
+    }
+  }
+
   __device__ __forceinline__ void value_scales(float (&scale)[4]) const {
     scale[0] = __builtin_bit_cast(float, (vs & 0xffu) << 23);
     scale[1] = __builtin_bit_cast(float, (vs & 0xff00u) << 15);
@@ -314,87 +391,73 @@ struct Unit {
 };
 
 // ---------------------------------------------------------------------------
-// The softmax of kTiles x 16 rows over the keys seen so far: lane l holds, of row l & 15 of every
-// tile, O's features D / 4 qd + D / 16 r + t in o[t][r], and its own keys' share of l.  Weights are
-// 2^(s c - m) with m a whole number, so that moving m is exact.
-template <int D, int kTiles>
+// The softmax of a tile's rows over the keys seen so far, the rows 16 (a lane has four keys of
+// every block) or 32 (eight).  l is of the lane's own keys.  Weights are 2^(s c - m) with m a
+// whole number, so that moving m is exact.
+template <int kRows>
 struct Softmax {
-  f32x4 o[kTiles][D / 16];
-  float m[kTiles], l[kTiles];
+  typedef float Logits __attribute__((ext_vector_type(kRows / 2)));       // of 32 keys
+  float m = kLowest, l = 0.f;
 
-  __device__ __forceinline__ void reset() {
+  // Logits from .. to - 1 as weights, rounded to bf16 as operands; sum and theirs
+  __device__ __forceinline__ float weigh(const Logits& s, float c, bf16x8 (&p)[kRows / 16], float sum = 0.f,
+                                         int from = 0, int to = kRows / 2) const {
 #pragma unroll
-    for (int x = 0; x < kTiles; ++x) {
+    for (int i = from; i < to; i += 2) {
+      bf16_pair e;
 #pragma unroll
-      for (int t = 0; t < D / 16; ++t) o[x][t] = f32x4{};
-      m[x] = kLowest;
-      l[x] = 0.f;
-    }
-  }
-
-  // Where a logit of the two blocks' s is too far above m for its weight: m up to the largest, and
-  // what there is so far, with the weights p that are not in O yet, relative to that
-  __device__ __forceinline__ void follow(const f32x4 (&s)[kTiles][2], float c, bf16x8 (&p)[kTiles]) {
-    float top[kTiles];
-    bool far = false;
-#pragma unroll
-    for (int x = 0; x < kTiles; ++x) {
-      top[x] = fmaxf(fmaxf(s[x][0][0], s[x][0][1]), s[x][0][2]);
-      top[x] = fmaxf(fmaxf(top[x], s[x][0][3]), s[x][1][0]);
-      top[x] = fmaxf(fmaxf(top[x], s[x][1][1]), s[x][1][2]);
-      top[x] = fmaxf(top[x], s[x][1][3]);
-      far |= __builtin_fmaf(top[x], c, -m[x]) > kLazy;
-    }
-    if (__builtin_amdgcn_ballot_w64(far) == 0) return;
-#pragma unroll
-    for (int x = 0; x < kTiles; ++x) {
-      const float m_new = fmaxf(m[x], ceilf(quad_max(top[x]) * c));
-      const float alpha = __builtin_amdgcn_exp2f(m[x] - m_new);
-      m[x] = m_new;
-      l[x] *= alpha;
-#pragma unroll
-      for (int t = 0; t < D / 16; ++t) o[x][t] *= alpha;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) p[x][i] = (__bf16)((float)p[x][i] * alpha);
-    }
-  }
-
-  // Tile x's logits as weights, rounded to bf16 for the product with V; l takes them unrounded
-  __device__ __forceinline__ bf16x8 weigh(int x, const f32x4 (&s)[2], float c) {
-    bf16x8 p;
-#pragma unroll
-    for (int b = 0; b < 2; ++b)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][r], c, -m[x]));
-        l[x] += e;
-        p[4 * b + r] = (__bf16)e;
+      for (int k = 0; k < 2; ++k) {
+        e[k] = (__bf16)__builtin_amdgcn_exp2f(__builtin_fmaf(s[i + k], c, -m));
+        p[i / 8][i % 8 + k] = e[k];
       }
-    return p;
+      sum = __builtin_amdgcn_fdot2_f32_bf16(e, bf16_pair{(__bf16)1.f, (__bf16)1.f}, sum, false);
+    }
+    return sum;
+  }
+
+  // Adds the weights p of logits s to l, by their sum; where one is too large (the sum finds it as
+  // well as a maximum would, and is needed) m moves up to the largest logit, what there is so far
+  // (o) with it, and the weights are made anew
+  template <int kWords, typename O>
+  __device__ __forceinline__ void add(float sum, const Logits& s, float c, O (&o)[kWords], bf16x8 (&p)[kRows / 16]) {
+    if (__builtin_amdgcn_ballot_w64(sum > kLargeSum) != 0) {
+      float top = s[0];
+#pragma unroll
+      for (int i = 1; i < kRows / 2; ++i) top = fmaxf(top, s[i]);
+      float a, b;
+      swap32(top, a, b);
+      top = kRows == 16 ? quad_max(top) : fmaxf(a, b);
+      const float m_new = fmaxf(m, ceilf(top * c));
+      const float alpha = __builtin_amdgcn_exp2f(m - m_new);
+      m = m_new;
+      l *= alpha;
+#pragma unroll
+      for (int t = 0; t < kWords; ++t) o[t] *= alpha;
+      sum = weigh(s, c, p);
+    }
+    l += sum;
   }
 };
 
-// Logits of keys that a row does not see: of a block's keys it sees the first `seen`
-__device__ __forceinline__ void mask(f32x4& s, int seen, int lane) {
-#pragma unroll
-  for (int r = 0; r < 4; ++r) s[r] = 4 * (lane >> 4) + r < seen ? s[r] : -INFINITY;
-}
-
-// A unit's keys added to one tile of rows, V converted as it is needed (decode); of the keys the
-// rows see the first `seen`.
+// A unit's keys added to 16 rows, V converted as it is needed (decode); of the keys the rows see the
+// first `seen`.  Lane l has of row l & 15 O's features D / 4 qd + D / 16 r + t in o[t][r].
 template <int D, int kBits>
-__device__ __forceinline__ void add_unit(Softmax<D, 1>& soft, const Unit<D, kBits>& u, const Rows16<D, kBits>& rows,
-                                         float c, int seen, int lane) {
-  f32x4 s[1][2];
+__device__ __forceinline__ void add_unit(Softmax<16>& soft, f32x4 (&o)[D / 16], const Unit<D, kBits>& u,
+                                         const Rows16<D, kBits>& rows, float c, int seen, int lane) {
+  Softmax<16>::Logits s;
 #pragma unroll
-  for (int b = 0; b < 2; ++b) s[0][b] = u.b[b].logits(rows);
+  for (int b = 0; b < 2; ++b) {
+    const f32x4 x = u.b[b].logits(rows);
+#pragma unroll
+    for (int r = 0; r < 4; ++r) s[4 * b + r] = x[r];
+  }
   if (seen < kUnitKeys) {
 #pragma unroll
-    for (int b = 0; b < 2; ++b) mask(s[0][b], seen - 16 * b, lane);
+    for (int i = 0; i < 8; ++i) s[i] = 16 * (i / 4) + 4 * (lane >> 4) + i % 4 < seen ? s[i] : -INFINITY;
   }
-  bf16x8 p[1] = {};
-  soft.follow(s, c, p);
-  p[0] = soft.weigh(0, s[0], c);
+  bf16x8 p[1];
+  const float sum = soft.weigh(s, c, p);
+  soft.add(sum, s, c, o, p);
   float scale[2][4];
 #pragma unroll
   for (int b = 0; b < 2; ++b) u.b[b].value_scales(scale[b]);
@@ -406,19 +469,9 @@ __device__ __forceinline__ void add_unit(Softmax<D, 1>& soft, const Unit<D, kBit
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       const u32x4 a = {f[0][i][0], f[0][i][1], f[1][i][0], f[1][i][1]};
-      soft.o[0][t + i] =
-          __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), p[0], soft.o[0][t + i], 0, 0, 0);
+      o[t + i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), p[0], o[t + i], 0, 0, 0);
     }
   }
-}
-
-// 8 features of a lane's O (its r-th run of D / 16, at D = 64 two of them) as bf16
-template <int D>
-__device__ __forceinline__ bf16x8 rounded8(const f32x4 (&o)[D / 16], int i, float inv_l) {
-  bf16x8 x;
-#pragma unroll
-  for (int e = 0; e < 8; ++e) x[e] = (__bf16)(o[e % (D / 16)][8 * i / (D / 16) + e / (D / 16)] * inv_l);
-  return x;
 }
 
 // ---------------------------------------------------------------------------
@@ -488,8 +541,10 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 4 : 3) void quant_decode_kernel
     const int last = (len - 1) / kBlock;
     Rows16<D, kBits> rows;
     rows.load(j < p.group ? p.q + ((size_t)r * p.num_q_heads + g * p.group + j) * D : nullptr, lane);
-    Softmax<D, 1> soft;
-    soft.reset();
+    Softmax<16> soft;
+    f32x4 o[D / 16];
+#pragma unroll
+    for (int t = 0; t < D / 16; ++t) o[t] = f32x4{};
     Unit<D, kBits> cur, nxt;
     int y = x + wave;
     int id0 = 0, id1 = 0;
@@ -510,17 +565,17 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 4 : 3) void quant_decode_kernel
       }
       const int seen = len - y * kUnitKeys;
       if (seen < kUnitKeys) cur.cut_values(seen, lane);
-      add_unit(soft, cur, rows, c, seen, lane);
+      add_unit<D, kBits>(soft, o, cur, rows, c, seen, lane);
     }
-    const float l = quad_sum(soft.l[0]);
+    const float l = quad_sum(soft.l);
     if (j < p.group) {
 #pragma unroll
       for (int rr = 0; rr < 4; ++rr)
 #pragma unroll
         for (int t = 0; t < D / 16; t += 4)
           *reinterpret_cast<f32x4*>(&sm.o[wave][j][D / 4 * (lane >> 4) + D / 16 * rr + t]) =
-              f32x4{soft.o[0][t][rr], soft.o[0][t + 1][rr], soft.o[0][t + 2][rr], soft.o[0][t + 3][rr]};
-      if (lane < 16) sm.ml[wave][j] = make_float2(soft.m[0], l);
+              f32x4{o[t][rr], o[t + 1][rr], o[t + 2][rr], o[t + 3][rr]};
+      if (lane < 16) sm.ml[wave][j] = make_float2(soft.m, l);
     }
     __syncthreads();
     for (int i = threadIdx.x; i < p.group * (D / 4); i += kThreads) {
@@ -586,16 +641,17 @@ __global__ __launch_bounds__(kMergeThreads) void quant_decode_merge_kernel(Quant
 }
 
 // ---------------------------------------------------------------------------
-// Prefill.  Rows of a KV head are (token, query head of it), heads fastest; a wave takes 32 of
-// them, a work-group 128.  Its steps are 64 keys: each wave reads one of the four blocks ahead into
-// registers, and a step later leaves it in LDS as all waves then take it, K's codes as
-// they are, V as bf16 fragments, so that each conversion is done once for 128 rows.  A step's
-// buffer is written while the other one is read: one barrier a step.  Several parts of a tile's
-// keys on as many work-groups leave partial results.
+// Prefill.  Rows of a KV head are (token, query head of it), heads fastest; a wave takes 32 of them,
+// or at D = 64, where the launch fills the device so, 64 (kTiles).  A work-group's steps are 64
+// keys: each wave reads one of the four blocks ahead into registers, and a step later leaves it in
+// LDS as all waves then take it, K's codes as they are, V as bf16 fragments, so that a
+// conversion is done once for the work-group's rows.  A step's buffer is written while the other one
+// is read: one barrier a step.
+//
+// Within a wave the matrix unit works on the logits of the next 32 keys and the values of the last
+// 32 while the vector unit makes the weights of the present ones.  Several parts of a tile's keys
+// on as many work-groups leave partial results.
 
-constexpr int kRowTiles = 2;
-constexpr int kWaveRows = 16 * kRowTiles;
-constexpr int kTileRows = kWaves * kWaveRows;
 constexpr int kStepBlocks = kWaves;
 constexpr int kStepKeys = 16 * kStepBlocks;
 
@@ -606,12 +662,14 @@ struct PrefillLds {
   // lane by lane what Block holds of K, and V^T fragments
   u32x4 k[2][kStepBlocks][Block<D, kBits>::kKWords / 4][64];
   int ks[2][kStepBlocks][64];
-  u32x4 v[2][kStepBlocks / 2][D / 16][64];
+  u32x4 v[2][kStepBlocks][D / 32][64];
 };
 
-template <int D, int kBits>
+template <int D, int kBits, int kTiles>
 __global__ __launch_bounds__(kThreads, 2) void quant_prefill_kernel(QuantParams p) {
   using T = QuantTile<D, kBits>;
+  constexpr int kWaveRows = 32 * kTiles;
+  constexpr int kTileRows = kWaves * kWaveRows;
   __shared__ PrefillLds<D, kBits> sm;
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -646,18 +704,15 @@ __global__ __launch_bounds__(kThreads, 2) void quant_prefill_kernel(QuantParams 
   const size_t stride = (size_t)p.num_kv_heads * T::kBytes;
   const uint8_t* base = p.pool + (size_t)g * T::kBytes;
   const float c = p.scale_log2;
-  const int j = lane & 15;
   const ScalarInts table = (ScalarInts)(p.block_tables + (size_t)r * p.max_blocks_per_seq);
   const int last = (len - 1) / kBlock;
   // The wave's blocks of a step: in registers, and a step later in the step's buffer.  Blocks outside
   // the part are read but not used; before its beginning (where weights are 0) V is zeros.
   Block<D, kBits> block;
-  auto key_tile = [&](int step) {
-    return Block<D, kBits>::tile(base, stride, table[max(0, min(kStepBlocks * step + 2 + wave, last))]);
-  };
-  auto value_tile = [&](int step) {
-    const int b = kStepBlocks * step - 2 + wave;
-    return Block<D, kBits>::tile(base, stride, b < kStepBlocks * x0 ? -1 : table[min(b, last)]);
+  auto load = [&](int key_step, int value_step) __attribute__((always_inline)) {
+    const int b = kStepBlocks * value_step - 2 + wave;
+    block.load_keys(Block<D, kBits>::tile(base, stride, table[max(0, min(kStepBlocks * key_step + 2 + wave, last))]), lane);
+    block.load_values(Block<D, kBits>::tile(base, stride, b < kStepBlocks * x0 ? -1 : table[min(b, last)]), lane);
   };
   auto store_keys = [&](int step) __attribute__((always_inline)) {
 #pragma unroll
@@ -666,125 +721,209 @@ __global__ __launch_bounds__(kThreads, 2) void quant_prefill_kernel(QuantParams 
           u32x4{block.k[4 * i], block.k[4 * i + 1], block.k[4 * i + 2], block.k[4 * i + 3]};
     sm.ks[step & 1][wave][lane] = block.ks;
   };
-  auto store_values = [&](int step) __attribute__((always_inline)) {
-    float scale[4];
-    block.value_scales(scale);
+  // Of a 32 x 16 fragment of V^T lane l holds feature group l & 31, D / 32 features each in as many
+  // fragments, and of the block's keys 4 h .. + 3 and 8 + 4 h .. + 3, h = l >> 5, as P's lanes do.
+  const int v_lane = (lane >> 4 & 1) * 32 + 2 * (lane & 15);
+  const int v_half = lane >> 5;
+  float v_scale[4];
+  // features 2 pair and 2 pair + 1 of the lane's D / 16
+  auto store_values = [&](int step, int pair) __attribute__((always_inline)) {
+    u32x2 f[2];
+    block.values(pair, v_scale, f);
 #pragma unroll
-    for (int t = 0; t < D / 16; t += 2) {
-      u32x2 f[2];
-      block.values(t / 2, scale, f);
-#pragma unroll
-      for (int i = 0; i < 2; ++i)
-        *(reinterpret_cast<u32x2*>(&sm.v[step & 1][wave / 2][t + i][lane]) + wave % 2) = f[i];
+    for (int i = 0; i < 2; ++i) {
+      const int t = 2 * pair + i;
+      *(reinterpret_cast<u32x2*>(&sm.v[step & 1][wave][t % (D / 32)][v_lane + t / (D / 32)]) + v_half) = f[i];
     }
   };
   auto cut_values = [&](int step) __attribute__((always_inline)) {
     const int n = len - step * kStepKeys + 16 * (2 - wave);
     if (n < 16) block.cut_values(n, lane);
+    block.value_scales(v_scale);
   };
 
-  if (x0 < xe) block.load_keys(key_tile(x0 - 1), lane);
-  Rows16<D, kBits> rows[kRowTiles];
-  long long q_row[kRowTiles];      // of q and out; negative: none
-  int end[kRowTiles];              // keys that the row sees
+  if (x0 < xe) load(x0 - 1, x0);
+  long long q_row[kTiles];      // of q and out; negative: none
+  int end[kTiles];              // keys that the row sees
+  Rows32<D, kBits> rows[kTiles];
 #pragma unroll
-  for (int i = 0; i < kRowTiles; ++i) {
-    const long long row = row0 + 16 * i + j;
+  for (int x = 0; x < kTiles; ++x) {
+    const long long row = row0 + 32 * x + (lane & 31);
     const int t = (int)(row / p.group);
-    q_row[i] = row < n_rows ? (long long)(q0 + t) * p.num_q_heads + g * p.group + (int)(row - (long long)t * p.group) : -1;
-    end[i] = before + min(t, t1) + 1;
-    rows[i].load(row < n_rows ? p.q + q_row[i] * D : nullptr, lane);
+    q_row[x] = row < n_rows ? (long long)(q0 + t) * p.num_q_heads + g * p.group + (int)(row - (long long)t * p.group) : -1;
+    end[x] = before + min(t, t1) + 1;
+    rows[x].load(row < n_rows ? p.q + q_row[x] * D : nullptr, lane);
   }
-  Softmax<D, kRowTiles> soft;
-  soft.reset();
+  // lane l has of row l & 31 and with h = l >> 5 the weights of keys 8 i + 4 h .. + 3 and O's
+  // features of groups 8 i + 4 h .. + 3, i < 4
+  typedef typename Softmax<32>::Logits Logits;
+  Softmax<32> soft[kTiles];
+  Logits o[kTiles][D / 32];
+#pragma unroll
+  for (int x = 0; x < kTiles; ++x)
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i) o[x][i] = Logits{};
   auto barrier = [&]() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); };
   // of the buffer's blocks 2 half and 2 half + 1
-  auto logits = [&](int step, int half, f32x4 (&s)[kRowTiles][2]) __attribute__((always_inline)) {
+  const int key = lane & 15, k_block = lane >> 4 & 1, k_half = lane >> 5;
+  // The work of half a step comes in as many chunks as its logits take products of 64 cycles.
+  constexpr int kChunks = D / 32;
+  struct Keys {
+    u32x4 w[kChunks / (kBits == 4 ? 2 : 1)];
+    int ks[kBits == 4 ? kChunks / 2 : 2];
+  };
+  auto read_keys = [&](int step, int half) __attribute__((always_inline)) {
+    const int buf = step & 1, b = 2 * half + k_block;
+    Keys k;
+    if constexpr (kBits == 4) {
 #pragma unroll
-    for (int b = 0; b < 2; ++b) {
-      Block<D, kBits> k;
-#pragma unroll
-      for (int i = 0; i < Block<D, kBits>::kKWords / 4; ++i) {
-        const u32x4 w = sm.k[step & 1][2 * half + b][i][lane];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) k.k[4 * i + e] = w[e];
+      for (int f = 0; f < D / 64; ++f) {
+        k.w[f] = sm.k[buf][b][0][(2 * f + k_half) * 16 + key];
+        k.ks[f] = sm.ks[buf][b][(2 * f + k_half) * 16 + key];
       }
-      k.ks = sm.ks[step & 1][2 * half + b][lane];
+    } else {
 #pragma unroll
-      for (int i = 0; i < kRowTiles; ++i) s[i][b] = k.logits(rows[i]);
+      for (int x = 0; x < 2; ++x) {
+#pragma unroll
+        for (int i = 0; i < D / 64; ++i) k.w[x * (D / 64) + i] = sm.k[buf][b][i][(2 * k_half + x) * 16 + key];
+        k.ks[x] = sm.ks[buf][b][(2 * k_half + x) * 16 + key];
+      }
+    }
+    return k;
+  };
+  auto add_logits = [&](int chunk, const Keys& k, Logits (&s)[kTiles]) __attribute__((always_inline)) {
+    if constexpr (kBits == 4) {
+      const u32x4 w = k.w[chunk / 2];
+      const i32x8 a = {(int)w[0], (int)w[1], (int)w[2], (int)w[3], 0, 0, 0, 0};
+#pragma unroll
+      for (int x = 0; x < kTiles; ++x)
+        s[x] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, rows[x].q[chunk / 2][chunk % 2], s[x], 4, 0, 0,
+                                                               k.ks[chunk / 2], 0, rows[x].scale[chunk / 2][chunk % 2]);
+    } else {
+      const float scale = scale_of(k.ks[chunk / (D / 64)]);
+      const u32x4 w = k.w[chunk];
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const u32x4 a = {read_pair<8>(w[2 * e], scale, 0), read_pair<8>(w[2 * e], scale, 1),
+                         read_pair<8>(w[2 * e + 1], scale, 0), read_pair<8>(w[2 * e + 1], scale, 1)};
+#pragma unroll
+        for (int x = 0; x < kTiles; ++x)
+          s[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), rows[x].q[2 * chunk + e], s[x], 0,
+                                                         0, 0);
+      }
     }
   };
-  auto add_values = [&](int step, int half, const bf16x8 (&w)[kRowTiles]) __attribute__((always_inline)) {
+  auto read_values = [&](int step, int half, int i) {
+    return __builtin_bit_cast(bf16x8, sm.v[step & 1][2 * half + i / (D / 32)][i % (D / 32)][lane]);
+  };
+  auto add_values = [&](int i, const bf16x8& f, const bf16x8 (&w)[kTiles][2]) __attribute__((always_inline)) {
 #pragma unroll
-    for (int t = 0; t < D / 16; ++t) {
-      const bf16x8 f = __builtin_bit_cast(bf16x8, sm.v[step & 1][half][t][lane]);
-#pragma unroll
-      for (int i = 0; i < kRowTiles; ++i)
-        soft.o[i][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f, w[i], soft.o[i][t], 0, 0, 0);
-    }
+    for (int x = 0; x < kTiles; ++x)
+      o[x][i % (D / 32)] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, w[x][i / (D / 32)], o[x][i % (D / 32)], 0, 0, 0);
   };
   // Half a step: from the logits s of 32 keys their weights w; beside that the logits of the next
-  // 32 and the values of the last 32
-  auto half_step = [&](int x, int half, f32x4 (&s)[kRowTiles][2], f32x4 (&next)[kRowTiles][2],
-                       bf16x8 (&before_w)[kRowTiles], bf16x8 (&w)[kRowTiles]) __attribute__((always_inline)) {
+  // 32 and the values of the last 32, and the wave's share of the next step's buffer
+  auto half_step = [&](int x, int half, Logits (&s)[kTiles], Logits (&next)[kTiles], const bf16x8 (&last_w)[kTiles][2],
+                       bf16x8 (&w)[kTiles][2]) __attribute__((always_inline)) {
     const int key0 = x * kStepKeys + 32 * half;
     if (key0 + 32 > before + t0 + 1) {
 #pragma unroll
-      for (int i = 0; i < kRowTiles; ++i)
+      for (int y = 0; y < kTiles; ++y)
 #pragma unroll
-        for (int b = 0; b < 2; ++b) mask(s[i][b], end[i] - key0 - 16 * b, lane);
+        for (int i = 0; i < 16; ++i) s[y][i] = key0 + 8 * (i / 4) + 4 * k_half + i % 4 < end[y] ? s[y][i] : -INFINITY;
     }
-    soft.follow(s, c, before_w);
-    logits(x, half, next);
+    // A wave issues in order, and a product that waits for the matrix unit, or for the one before
+    // it in its sum, holds up what stands behind it: so they are dealt out among the weights.
+    __builtin_amdgcn_sched_barrier(0);
+    const Keys keys = read_keys(x, half);
+    bf16x8 f[2][2];
 #pragma unroll
-    for (int i = 0; i < kRowTiles; ++i) w[i] = soft.weigh(i, s[i], c);
-    add_values(x, half, before_w);
+    for (int i = 0; i < 2; ++i) f[0][i] = read_values(x, half, i);
+    float sum[kTiles];
+#pragma unroll
+    for (int y = 0; y < kTiles; ++y) {
+      next[y] = Logits{};
+      sum[y] = 0.f;
+    }
+#pragma unroll
+    for (int k = 0; k < kChunks; ++k) {
+      if (k + 1 < kChunks) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) f[(k + 1) % 2][i] = read_values(x, half, 2 * (k + 1) + i);
+      }
+      if (half == 0 && k == 0) store_keys(x + 1);
+      if (k % 2 == 1) store_values(x + 1, half * (D / 64) + k / 2);
+#pragma unroll
+      for (int y = 0; y < kTiles; ++y)
+        sum[y] = soft[y].weigh(s[y], c, w[y], sum[y], 16 / kChunks * k, 16 / kChunks * (k + 1));
+      add_logits(k, keys, next);
+#pragma unroll
+      for (int i = 0; i < 2; ++i) add_values(2 * k + i, f[k % 2][i], last_w);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+#pragma unroll
+    for (int y = 0; y < kTiles; ++y) asm volatile("" : "+v"(next[y]));
+#pragma unroll
+    for (int y = 0; y < kTiles; ++y) soft[y].add(sum[y], s[y], c, o[y], w[y]);
   };
   if (x0 < xe) {
-    f32x4 s0[kRowTiles][2], s1[kRowTiles][2];
-    bf16x8 w0[kRowTiles], w1[kRowTiles] = {};
+    Logits s0[kTiles], s1[kTiles];
+    bf16x8 w0[kTiles][2], w1[kTiles][2] = {};
     store_keys(x0 - 1);
-    block.load_keys(key_tile(x0), lane);
-    block.load_values(value_tile(x0), lane);
-    barrier();
-    logits(x0 - 1, 1, s0);
     cut_values(x0);
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i) store_values(x0, i);
+    barrier();
+    block.load_keys(Block<D, kBits>::tile(base, stride, table[min(kStepBlocks * x0 + 2 + wave, last)]), lane);
+    const Keys keys = read_keys(x0 - 1, 1);
+#pragma unroll
+    for (int y = 0; y < kTiles; ++y) s0[y] = Logits{};
+#pragma unroll
+    for (int k = 0; k < kChunks; ++k) add_logits(k, keys, s0);
     store_keys(x0);
-    store_values(x0);
-    block.load_keys(key_tile(x0 + 1), lane);
-    block.load_values(value_tile(x0 + 1), lane);
+    load(x0 + 1, x0 + 1);
     for (int x = x0; x < xe; ++x) {
       // step x is in LDS, and no wave reads the other buffer any more
       barrier();
       cut_values(x + 1);
       half_step(x, 0, s0, s1, w1, w0);
-      store_keys(x + 1);
-      store_values(x + 1);
-      block.load_keys(key_tile(x + 2), lane);
-      block.load_values(value_tile(x + 2), lane);
       half_step(x, 1, s1, s0, w0, w1);
+      load(x + 2, x + 2);
     }
     barrier();
-    add_values(xe, 0, w1);
+#pragma unroll
+    for (int i = 0; i < 2 * kChunks; ++i) add_values(i, read_values(xe, 0, i), w1);
   }
 #pragma unroll
-  for (int i = 0; i < kRowTiles; ++i) {
-    const float l = quad_sum(soft.l[i]);
-    if (q_row[i] < 0) continue;
-    const int d0 = D / 4 * (lane >> 4);
+  for (int x = 0; x < kTiles; ++x) {
+    float la, lb;
+    swap32(soft[x].l, la, lb);
+    const float l = la + lb;
+    if (q_row[x] < 0) continue;
+    // D / 8 neighbouring features for each i, feature k of them in o[k % (D / 32)]
     if (p.parts == 1) {
+      const float inv_l = 1.f / l;
 #pragma unroll
-      for (int k = 0; k < D / 32; ++k)
-        *reinterpret_cast<bf16x8*>(p.out + q_row[i] * D + d0 + 8 * k) = rounded8<D>(soft.o[i], k, 1.f / l);
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int k = 0; k < D / 8; k += 8) {
+          bf16x8 y;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) y[e] = (__bf16)(o[x][(k + e) % (D / 32)][4 * i + (k + e) / (D / 32)] * inv_l);
+          *reinterpret_cast<bf16x8*>(p.out + q_row[x] * D + D / 4 * i + D / 8 * k_half + k) = y;
+        }
     } else {
-      const size_t to = (size_t)part * p.total_q * p.num_q_heads + q_row[i];
+      const size_t to = (size_t)part * p.total_q * p.num_q_heads + q_row[x];
 #pragma unroll
-      for (int rr = 0; rr < 4; ++rr)
+      for (int i = 0; i < 4; ++i)
 #pragma unroll
-        for (int t = 0; t < D / 16; t += 4)
-          *reinterpret_cast<f32x4*>(p.ws_o + to * D + d0 + D / 16 * rr + t) =
-              f32x4{soft.o[i][t][rr], soft.o[i][t + 1][rr], soft.o[i][t + 2][rr], soft.o[i][t + 3][rr]};
-      if (lane < 16) *reinterpret_cast<float2*>(p.ws_ml + 2 * to) = make_float2(soft.m[i], l);
+        for (int k = 0; k < D / 8; k += 4) {
+          f32x4 y;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) y[e] = o[x][(k + e) % (D / 32)][4 * i + (k + e) / (D / 32)];
+          *reinterpret_cast<f32x4*>(p.ws_o + to * D + D / 4 * i + D / 8 * k_half + k) = y;
+        }
+      if (lane < 32) *reinterpret_cast<float2*>(p.ws_ml + 2 * to) = make_float2(soft[x].m, l);
     }
   }
 }
@@ -845,8 +984,11 @@ hipError_t decode(const QuantParams& p, hipStream_t stream) {
 }
 
 template <int D, int kBits>
-hipError_t prefill(const QuantParams& p, long long grid, hipStream_t stream) {
-  hipLaunchKernelGGL((quant_prefill_kernel<D, kBits>), dim3((unsigned)grid), dim3(kThreads), 0, stream, p);
+hipError_t prefill(const QuantParams& p, int wave_tiles, long long grid, hipStream_t stream) {
+  if (D == 64 && wave_tiles == 2)
+    hipLaunchKernelGGL((quant_prefill_kernel<64, kBits, 2>), dim3((unsigned)grid), dim3(kThreads), 0, stream, p);
+  else
+    hipLaunchKernelGGL((quant_prefill_kernel<D, kBits, 1>), dim3((unsigned)grid), dim3(kThreads), 0, stream, p);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.parts == 1) return e;
   const long long threads = (long long)p.total_q * p.num_q_heads * (D / 4);
@@ -894,12 +1036,18 @@ QuantPrefillGeometry quant_prefill_geometry(int batch, int total_q, int max_q_le
                                             int num_q_heads, int num_kv_heads, int head_dim, int cus) {
   QuantPrefillGeometry geo = {};
   const long long group = num_q_heads / num_kv_heads;
-  geo.tiles = (max_q_len * group + kTileRows - 1) / kTileRows;
-  // tiles there are at most: of the longest suffix, or as many as the rows of all make
-  const double bound = (double)num_kv_heads * ((double)total_q * group / kTileRows + batch);
-  double tiles = (double)geo.tiles * batch * num_kv_heads;
-  if (bound < tiles) tiles = bound;
-  long long parts = tiles > 0 ? (long long)(2 * cus / tiles) : 1;
+  // work-groups there are at most: of the longest suffix, or as many as the rows of all make
+  auto tiles_of = [&](int wave_tiles) {
+    const long long rows = 32 * kWaves * wave_tiles;
+    const double longest = (double)((max_q_len * group + rows - 1) / rows) * batch;
+    const double all = (double)total_q * group / rows + batch;
+    return num_kv_heads * (longest < all ? longest : all);
+  };
+  geo.wave_tiles = head_dim == 64 && tiles_of(2) >= cus ? 2 : 1;
+  const long long rows = 32 * kWaves * geo.wave_tiles;
+  geo.tiles = (max_q_len * group + rows - 1) / rows;
+  const double tiles = tiles_of(geo.wave_tiles);
+  long long parts = tiles > 0 ? (long long)(2 / geo.wave_tiles * cus / tiles) : 1;
   const long long steps = (max_kv_len + kStepKeys - 1LL) / kStepKeys;
   if (parts > steps / kPrefillPartSteps) parts = steps / kPrefillPartSteps;
   if (parts > kPrefillMaxParts) parts = kPrefillMaxParts;
@@ -919,8 +1067,8 @@ hipError_t launch_quant_prefill(const QuantAttnLaunch& a, const QuantPrefillGeom
   p.tiles = (int)geo.tiles;
   p.ws_o = a.workspace;
   p.ws_ml = a.workspace + (long long)geo.parts * a.total_q * a.num_q_heads * a.head_dim;
-  if (a.head_dim == 64) return a.bits == 4 ? prefill<64, 4>(p, geo.grid, stream) : prefill<64, 8>(p, geo.grid, stream);
-  return a.bits == 4 ? prefill<128, 4>(p, geo.grid, stream) : prefill<128, 8>(p, geo.grid, stream);
+  if (a.head_dim == 64) return a.bits == 4 ? prefill<64, 4>(p, geo.wave_tiles, geo.grid, stream) : prefill<64, 8>(p, geo.wave_tiles, geo.grid, stream);
+  return a.bits == 4 ? prefill<128, 4>(p, geo.wave_tiles, geo.grid, stream) : prefill<128, 8>(p, geo.wave_tiles, geo.grid, stream);
 }
 
 }  // namespace cs
