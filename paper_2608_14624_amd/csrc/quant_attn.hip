@@ -480,14 +480,14 @@ __device__ __forceinline__ void add_unit(Softmax<16>& soft, f32x4 (&o)[D / 16], 
 // part of the range) in turn and merge in LDS; a sequence cut over several ranges leaves partial
 // results (O relative to m, m, and l) that a second kernel merges.
 
-__device__ __forceinline__ long long total_units(const QuantParams& p, int lane) {
-  long long total = 0;
+__device__ __forceinline__ int total_units(const QuantParams& p, int lane) {
+  int total = 0;
   for (int s = 0; s < p.batch; s += 64) total += wave_total(s + lane < p.batch ? units_of(p.lens[s + lane]) : 0);
   return total;
 }
 
-__device__ __forceinline__ int units_per_range(const QuantParams& p, long long total) {
-  return max((int)((total + p.ranges - 1) / p.ranges), kWaves);
+__device__ __forceinline__ int units_per_range(const QuantParams& p, int total) {
+  return max((int)(((unsigned)total + p.ranges - 1) / (unsigned)p.ranges), kWaves);
 }
 
 template <int D>
@@ -496,8 +496,14 @@ struct DecodeLds {
   float2 ml[kWaves][kMaxGroup];
 };
 
+// Units that a wave's registers hold, one of them being attended while the others are on their way
+constexpr int decode_depth(int head_dim, int bits) { return head_dim == 128 && bits == 8 ? 2 : 3; }
+// Work-groups per compute unit that a decode's keys are dealt to: as many as its registers allow
+constexpr int decode_groups_per_cu(int head_dim) { return head_dim == 64 ? 4 : 3; }
+
 template <int D, int kBits>
-__global__ __launch_bounds__(kThreads, D == 64 ? 4 : 3) void quant_decode_kernel(QuantParams p) {
+__global__ __launch_bounds__(kThreads, decode_groups_per_cu(D)) void quant_decode_kernel(QuantParams p) {
+  constexpr int kDepth = decode_depth(D, kBits);
   using T = QuantTile<D, kBits>;
   __shared__ DecodeLds<D> sm;
   const int lane = threadIdx.x & 63;
@@ -505,15 +511,15 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 4 : 3) void quant_decode_kernel
   const int g = blockIdx.x % p.num_kv_heads;
   const int w = blockIdx.x / p.num_kv_heads;
   const ScalarInts lens = (ScalarInts)p.lens;
-  const long long total = total_units(p, lane);
+  const int total = total_units(p, lane);
   const int per = units_per_range(p, total);
-  const long long u0 = (long long)w * per;
-  if (u0 >= total) return;
-  int left = (int)min((long long)per, total - u0);
+  if ((long long)w * per >= total) return;
+  const int u0 = w * per;
+  int left = min(per, total - u0);
   // the sequence that holds unit u0
   int r = 0, x = 0;
   {
-    long long first = 0;
+    int first = 0;
     for (int s = 0;; s += 64) {
       const int n = s + lane < p.batch ? units_of(p.lens[s + lane]) : 0;
       const int incl = wave_scan(n);
@@ -521,7 +527,7 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 4 : 3) void quant_decode_kernel
       if (past != 0) {
         const int at = __builtin_ctzll(past);
         r = s + at;
-        x = (int)(u0 - first - __builtin_amdgcn_readlane(incl - n, at));
+        x = u0 - first - __builtin_amdgcn_readlane(incl - n, at);
         break;
       }
       first += __builtin_amdgcn_readlane(incl, 63);
@@ -545,27 +551,32 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 4 : 3) void quant_decode_kernel
     f32x4 o[D / 16];
 #pragma unroll
     for (int t = 0; t < D / 16; ++t) o[t] = f32x4{};
-    Unit<D, kBits> cur, nxt;
-    int y = x + wave;
+    Unit<D, kBits> ring[kDepth];
     int id0 = 0, id1 = 0;
     auto ids_of = [&](int unit) {
       id0 = table[kUnitBlocks * unit];
       id1 = table[min(kUnitBlocks * unit + 1, last)];
     };
-    if (y < xe) {
-      ids_of(y);
-      nxt.load(base, stride, id0, id1, lane);
-      if (y + kWaves < xe) ids_of(y + kWaves);
+    int y = x + wave;
+    if (y < xe) ids_of(y);
+#pragma unroll
+    for (int d = 0; d < kDepth; ++d) {
+      if (y + d * kWaves >= xe) break;
+      ring[d].load(base, stride, id0, id1, lane);
+      if (y + (d + 1) * kWaves < xe) ids_of(y + (d + 1) * kWaves);
     }
-    for (; y < xe; y += kWaves) {
-      cur = nxt;
-      if (y + kWaves < xe) {
-        nxt.load(base, stride, id0, id1, lane);
-        if (y + 2 * kWaves < xe) ids_of(y + 2 * kWaves);
+    while (y < xe) {
+#pragma unroll
+      for (int d = 0; d < kDepth; ++d, y += kWaves) {
+        if (y >= xe) break;
+        const int seen = len - y * kUnitKeys;
+        if (seen < kUnitKeys) ring[d].cut_values(seen, lane);
+        add_unit<D, kBits>(soft, o, ring[d], rows, c, seen, lane);
+        if (y + kDepth * kWaves < xe) {
+          ring[d].load(base, stride, id0, id1, lane);
+          if (y + (kDepth + 1) * kWaves < xe) ids_of(y + (kDepth + 1) * kWaves);
+        }
       }
-      const int seen = len - y * kUnitKeys;
-      if (seen < kUnitKeys) cur.cut_values(seen, lane);
-      add_unit<D, kBits>(soft, o, cur, rows, c, seen, lane);
     }
     const float l = quad_sum(soft.l);
     if (j < p.group) {
@@ -619,7 +630,7 @@ __global__ __launch_bounds__(kMergeThreads) void quant_decode_merge_kernel(Quant
   const int g = blockIdx.x % p.num_kv_heads;
   const int r = blockIdx.x / p.num_kv_heads;
   const int lane = threadIdx.x & 63;
-  long long total = 0, before = 0;
+  int total = 0, before = 0;
   for (int s = 0; s < p.batch; s += 64) {
     const int n = s + lane < p.batch ? units_of(p.lens[s + lane]) : 0;
     total += wave_total(n);
@@ -627,8 +638,8 @@ __global__ __launch_bounds__(kMergeThreads) void quant_decode_merge_kernel(Quant
   }
   const int per = units_per_range(p, total);
   const int n = units_of(p.lens[r]);
-  const int w0 = (int)(before / per);
-  const int pieces = n == 0 ? 0 : (int)((before + n - 1) / per) - w0 + 1;
+  const int w0 = (unsigned)before / (unsigned)per;
+  const int pieces = n == 0 ? 0 : (int)((unsigned)(before + n - 1) / (unsigned)per) - w0 + 1;
   if (pieces == 1) return;
   const size_t first = ((size_t)g * p.rows + r + w0) * p.group;
   merge_pieces<D>(
@@ -666,7 +677,7 @@ struct PrefillLds {
 };
 
 template <int D, int kBits, int kTiles>
-__global__ __launch_bounds__(kThreads, 2) void quant_prefill_kernel(QuantParams p) {
+__global__ __launch_bounds__(kThreads, kTiles == 1 ? 2 : 1) void quant_prefill_kernel(QuantParams p) {
   using T = QuantTile<D, kBits>;
   constexpr int kWaveRows = 32 * kTiles;
   constexpr int kTileRows = kWaves * kWaveRows;
@@ -686,20 +697,21 @@ __global__ __launch_bounds__(kThreads, 2) void quant_prefill_kernel(QuantParams 
   const int r = at / p.tiles;
   const int q0 = cu[r];
   const int tokens = cu[r + 1] - q0;
-  const long long n_rows = (long long)tokens * p.group;
-  const long long tile0 = (long long)tile * kTileRows;
+  const unsigned group = p.group;
+  const int n_rows = tokens * p.group;
+  const int tile0 = tile * kTileRows;
   if (tile0 >= n_rows) return;
   const int before = prefix[r];
   const int len = before + tokens;
   // tokens of the wave's first and last row
-  const long long row0 = tile0 + wave * kWaveRows;
-  const int t0 = (int)(min(row0, n_rows - 1) / p.group);
-  const int t1 = (int)((min(row0 + kWaveRows, n_rows) - 1) / p.group);
+  const int row0 = tile0 + wave * kWaveRows;
+  const int t0 = (unsigned)min(row0, n_rows - 1) / group;
+  const int t1 = (unsigned)(min(row0 + kWaveRows, n_rows) - 1) / group;
   // steps of the keys that the tile's rows see, this part's
-  const int tile_t1 = (int)((min(tile0 + kTileRows, n_rows) - 1) / p.group);
-  const int steps = (before + tile_t1 + kStepKeys) / kStepKeys;
-  const int x0 = (int)((long long)steps * part / p.parts);
-  const int xe = (int)((long long)steps * (part + 1) / p.parts);
+  const int tile_t1 = (unsigned)(min(tile0 + kTileRows, n_rows) - 1) / group;
+  const unsigned steps = (unsigned)(before + tile_t1) / kStepKeys + 1;
+  const int x0 = steps * part / (unsigned)p.parts;
+  const int xe = steps * (part + 1) / (unsigned)p.parts;
 
   const size_t stride = (size_t)p.num_kv_heads * T::kBytes;
   const uint8_t* base = p.pool + (size_t)g * T::kBytes;
@@ -748,9 +760,9 @@ __global__ __launch_bounds__(kThreads, 2) void quant_prefill_kernel(QuantParams 
   Rows32<D, kBits> rows[kTiles];
 #pragma unroll
   for (int x = 0; x < kTiles; ++x) {
-    const long long row = row0 + 32 * x + (lane & 31);
-    const int t = (int)(row / p.group);
-    q_row[x] = row < n_rows ? (long long)(q0 + t) * p.num_q_heads + g * p.group + (int)(row - (long long)t * p.group) : -1;
+    const int row = row0 + 32 * x + (lane & 31);
+    const int t = (unsigned)row / group;
+    q_row[x] = row < n_rows ? (long long)(q0 + t) * p.num_q_heads + g * p.group + (row - t * p.group) : -1;
     end[x] = before + min(t, t1) + 1;
     rows[x].load(row < n_rows ? p.q + q_row[x] * D : nullptr, lane);
   }
@@ -936,22 +948,39 @@ __global__ __launch_bounds__(kThreads) void quant_prefill_merge_kernel(QuantPara
   const long long row = i / (D / 4);
   const int d = (int)(i % (D / 4)) * 4;
   if (row >= (long long)p.cu_q_lens[p.batch] * p.num_q_heads) return;
-  float m = -INFINITY;
-  for (int k = 0; k < p.parts; ++k) m = fmaxf(m, p.ws_ml[2 * (k * n + row)]);
-  float den = 0.f;
+  float m = -INFINITY, den = 0.f;
   f32x4 acc = f32x4{};
-  for (int k = 0; k < p.parts; ++k) {
-    const float2 ml = *reinterpret_cast<const float2*>(p.ws_ml + 2 * (k * n + row));
-    const float wt = __builtin_amdgcn_exp2f(ml.x - m);
-    const f32x4 o = *reinterpret_cast<const f32x4*>(p.ws_o + (k * n + row) * D + d);
-    den = __builtin_fmaf(wt, ml.y, den);
+  for (int k0 = 0; k0 < p.parts; k0 += kMergeStep) {
+    float2 ml[kMergeStep];
+    f32x4 o[kMergeStep];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) acc[e] = __builtin_fmaf(wt, o[e], acc[e]);
+    for (int k = 0; k < kMergeStep; ++k) {
+      ml[k] = make_float2(-INFINITY, 0.f);
+      o[k] = f32x4{};
+      if (k0 + k >= p.parts) continue;
+      const size_t at = (size_t)((k0 + k) * n + row);
+      ml[k] = *reinterpret_cast<const float2*>(p.ws_ml + 2 * at);
+      o[k] = *reinterpret_cast<const f32x4*>(p.ws_o + at * D + d);
+    }
+    float m_new = m;
+#pragma unroll
+    for (int k = 0; k < kMergeStep; ++k) m_new = fmaxf(m_new, ml[k].x);
+    const float alpha = __builtin_amdgcn_exp2f(m - m_new);
+    m = m_new;
+    den *= alpha;
+    acc *= alpha;
+#pragma unroll
+    for (int k = 0; k < kMergeStep; ++k) {
+      const float wt = __builtin_amdgcn_exp2f(ml[k].x - m);
+      den = __builtin_fmaf(wt, ml[k].y, den);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc[e] = __builtin_fmaf(wt, o[k][e], acc[e]);
+    }
   }
-  bf16x4 o;
+  bf16x4 y;
 #pragma unroll
-  for (int e = 0; e < 4; ++e) o[e] = (__bf16)(acc[e] / den);
-  *reinterpret_cast<uint2*>(p.out + row * D + d) = __builtin_bit_cast(uint2, o);
+  for (int e = 0; e < 4; ++e) y[e] = (__bf16)(acc[e] / den);
+  *reinterpret_cast<uint2*>(p.out + row * D + d) = __builtin_bit_cast(uint2, y);
 }
 
 QuantParams params_of(const QuantAttnLaunch& a) {
@@ -999,22 +1028,18 @@ hipError_t prefill(const QuantParams& p, int wave_tiles, long long grid, hipStre
 
 }  // namespace
 
-// Work-groups per compute unit that a decode's keys are dealt to
-constexpr int kDecodeGroupsPerCu = 4;
-
 QuantDecodeGeometry quant_decode_geometry(int batch, int max_seq_len, int num_q_heads, int num_kv_heads,
                                           int head_dim, int cus) {
   QuantDecodeGeometry geo = {};
   const double units = (double)((max_seq_len + 31LL) / 32);
   const double most = batch * units;
-  geo.ranges = (kDecodeGroupsPerCu * cus + num_kv_heads - 1) / num_kv_heads;
+  geo.ranges = (decode_groups_per_cu(head_dim) * cus + num_kv_heads - 1) / num_kv_heads;
   if (most < geo.ranges) geo.ranges = most < 1 ? 1 : (int)most;
   geo.rows = (long long)geo.ranges + batch;
   geo.bytes = geo.rows * num_q_heads * (head_dim + 2) * (long long)sizeof(float);
-  // (the units of 64 sequences, and those of a range, are counted in 32 bits)
+  // (units are counted in 32 bits, 64 sequences' at a time)
   geo.fits = launch_fits((double)geo.ranges * num_kv_heads, kThreads) &&
-             launch_fits((double)batch * num_kv_heads, kMergeThreads) && 64 * units < 0x1p31 &&
-             most / geo.ranges < 0x1p31;
+             launch_fits((double)batch * num_kv_heads, kMergeThreads) && (batch + 63.0) * units < 0x1p31;
   return geo;
 }
 
@@ -1029,8 +1054,8 @@ hipError_t launch_quant_decode(const QuantAttnLaunch& a, const QuantDecodeGeomet
 }
 
 constexpr int kPrefillMaxParts = 16;
-// fewest steps of a part of the longest sequence
-constexpr int kPrefillPartSteps = 2;
+// fewest steps of a part of the longest sequence: work-groups start and merge for about the time of 30
+constexpr int kPrefillPartSteps = 6;
 
 QuantPrefillGeometry quant_prefill_geometry(int batch, int total_q, int max_q_len, int max_kv_len,
                                             int num_q_heads, int num_kv_heads, int head_dim, int cus) {
@@ -1053,7 +1078,8 @@ QuantPrefillGeometry quant_prefill_geometry(int batch, int total_q, int max_q_le
   if (parts > kPrefillMaxParts) parts = kPrefillMaxParts;
   geo.parts = parts < 1 ? 1 : (int)parts;
   const double grid = (double)geo.tiles * batch * num_kv_heads * geo.parts;
-  geo.fits = launch_fits(grid, kThreads) &&
+  // (an invocation's rows of a KV head are counted in 32 bits)
+  geo.fits = launch_fits(grid, kThreads) && max_q_len * group < 0x7fffff00LL &&
              (geo.parts == 1 || launch_fits((double)total_q * num_q_heads * (head_dim / 4) / kThreads + 1, kThreads));
   if (!geo.fits) return geo;
   geo.grid = (long long)grid;
