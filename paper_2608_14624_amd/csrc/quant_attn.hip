@@ -27,6 +27,8 @@
 
 #include <math.h>
 
+#include <type_traits>
+
 namespace cs {
 namespace {
 
@@ -242,16 +244,16 @@ struct Block {
   int ks;
   uint32_t vs;
 
-  template <int kWords>
+  template <int kPolicy, int kWords>
   __device__ __forceinline__ static void load_words(uint32_t (&to)[kWords], __amdgpu_buffer_rsrc_t rs, int off) {
     if constexpr (kWords == 2) {
-      const u32x2 x = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(rs, off, 0, 0));
+      const u32x2 x = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(rs, off, 0, kPolicy));
       to[0] = x[0];
       to[1] = x[1];
     } else {
 #pragma unroll
       for (int w = 0; w < kWords; w += 4) {
-        const u32x4 x = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rs, off + 4 * w, 0, 0));
+        const u32x4 x = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rs, off + 4 * w, 0, kPolicy));
 #pragma unroll
         for (int i = 0; i < 4; ++i) to[w + i] = x[i];
       }
@@ -264,6 +266,7 @@ struct Block {
     return __builtin_amdgcn_make_buffer_rsrc((void*)(base + (size_t)id * stride), (short)0, id < 0 ? 0 : T::kBytes,
                                              kRawBufferWord3);
   }
+  template <int kPolicy = 0>
   __device__ __forceinline__ void load_keys(__amdgpu_buffer_rsrc_t rs, int lane) {
     const int key = lane & 15, qd = lane >> 4;
     int k_off, ks_off;
@@ -275,12 +278,13 @@ struct Block {
       k_off = key * T::kRowBytes + D / 4 * qd;
       ks_off = T::kKScales + key * T::kGroups + qd * T::kGroups / 4;
     }
-    load_words(k, rs, k_off);
+    load_words<kPolicy>(k, rs, k_off);
     ks = __builtin_amdgcn_raw_buffer_load_b8(rs, ks_off, 0, 0);
   }
+  template <int kPolicy = 0>
   __device__ __forceinline__ void load_values(__amdgpu_buffer_rsrc_t rs, int lane) {
     const int c = lane & 15, qd = lane >> 4;
-    load_words(v, rs, T::kV + (c * 16 + 4 * qd) * T::kPartBytes);
+    load_words<kPolicy>(v, rs, T::kV + (c * 16 + 4 * qd) * T::kPartBytes);
     vs = __builtin_amdgcn_raw_buffer_load_b32(rs, T::kVScales + c * T::kPart / kScaleGroup * 16 + 4 * qd, 0, 0);
   }
 
@@ -376,12 +380,15 @@ struct Block {
 template <int D, int kBits>
 struct Unit {
   Block<D, kBits> b[2];
+  // kOnce: no other sequence is known to read the blocks, so they need not stay in the caches.  (At 8
+  // bits a lane's codes of K are 32 bytes, two loads that take half of every line each.)
+  template <bool kOnce>
   __device__ __forceinline__ void load(const uint8_t* base, size_t stride, int id0, int id1, int lane) {
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       const __amdgpu_buffer_rsrc_t rs = Block<D, kBits>::tile(base, stride, i ? id1 : id0);
-      b[i].load_keys(rs, lane);
-      b[i].load_values(rs, lane);
+      b[i].template load_keys<kOnce && kBits == 4 ? kNonTemporal : 0>(rs, lane);
+      b[i].template load_values<kOnce ? kNonTemporal : 0>(rs, lane);
     }
   }
   __device__ __forceinline__ void cut_values(int n, int lane) {
@@ -496,13 +503,39 @@ struct DecodeLds {
   float2 ml[kWaves][kMaxGroup];
 };
 
-// Units that a wave's registers hold, one of them being attended while the others are on their way
-constexpr int decode_depth(int head_dim, int bits) { return head_dim == 128 && bits == 8 ? 2 : 3; }
-// Work-groups per compute unit that a decode's keys are dealt to: as many as its registers allow
-constexpr int decode_groups_per_cu(int head_dim) { return head_dim == 64 ? 4 : 3; }
+// How many sequences hold the block at index 31 that the one before them holds: a batch's agents'
+// sequences usually stand together, and a prefix that short is not worth asking for.
+constexpr int kProbeBlock = 31;
+__device__ __forceinline__ int count_sharing(const QuantParams& p, int lane) {
+  int count = 0;
+  for (int s = 0; s < p.batch; s += 63) {      // (lane 0: the sequence before the 63)
+    const int i = s + lane - 1;
+    int id = -1 - lane;
+    if (i >= 0 && i < p.batch && p.lens[i] > kProbeBlock * kBlock)
+      id = p.block_tables[(size_t)i * p.max_blocks_per_seq + kProbeBlock];
+    const int last = __shfl_up(id, 1);
+    count += __builtin_popcountll(__builtin_amdgcn_ballot_w64(lane > 0 && id == last));
+  }
+  return count;
+}
+
+// Units that a wave's registers hold, one of them being attended while the others are on their way,
+// and work-groups per compute unit, to which a decode's keys are dealt: all run at once.  us a call
+// of 128 sequences of 4.2k-10.8k keys, 32 / 8 heads of 128, at 4 bits: 4 units and 2 work-groups 175, 3 and 2
+// 177, 6 and 2 178, 2 and 3 179, 3 and 3 183; at 8 bits 3 and 2 363, 2 and 3 379.
+constexpr int decode_depth(int head_dim, int bits) { return head_dim == 128 && bits == 8 ? 3 : 4; }
+constexpr int kDecodeGroupsPerCu = 2;
+// Blocks are loaded as read once (non-temporal) unless at least one sequence in kSharingPart shares
+// them, in launches of at least kSharedUnits units a work-group; in smaller ones the answer is not worth
+// waiting for.  us a call so and with ordinary loads: those 128 sequences at 4 bits 175 and 205, at 8 bits 348 and
+// 363; 61 sequences of 4 agents with 4096 shared keys and 100-3000 of their own, 64 / 8 heads, 55 and 49 at 4
+// bits, 102 and 94 at 8.  (Pieces cut at the same positions of all sequences, dealt so that the
+// work-groups that run at one time share them, raise the L2's hits from 49% to 68% there and take 108.)
+constexpr int kSharingPart = 4;
+constexpr int kSharedUnits = 16;
 
 template <int D, int kBits>
-__global__ __launch_bounds__(kThreads, decode_groups_per_cu(D)) void quant_decode_kernel(QuantParams p) {
+__global__ __launch_bounds__(kThreads, kDecodeGroupsPerCu) void quant_decode_kernel(QuantParams p) {
   constexpr int kDepth = decode_depth(D, kBits);
   using T = QuantTile<D, kBits>;
   __shared__ DecodeLds<D> sm;
@@ -537,91 +570,98 @@ __global__ __launch_bounds__(kThreads, decode_groups_per_cu(D)) void quant_decod
   const uint8_t* base = p.pool + (size_t)g * T::kBytes;
   const int j = lane & 15;
   const float c = p.scale_log2;
-  for (;;) {
-    const int len = lens[r];
-    const int n = units_of(len);
-    const int xe = min(n, x + left);
-    const bool whole = x == 0 && xe == n;
-    left -= xe - x;
-    const ScalarInts table = (ScalarInts)(p.block_tables + (size_t)r * p.max_blocks_per_seq);
-    const int last = (len - 1) / kBlock;
-    Rows16<D, kBits> rows;
-    rows.load(j < p.group ? p.q + ((size_t)r * p.num_q_heads + g * p.group + j) * D : nullptr, lane);
-    Softmax<16> soft;
-    f32x4 o[D / 16];
+  const bool shared = total >= kSharedUnits * p.ranges && p.batch > 1 && p.max_blocks_per_seq > kProbeBlock &&
+                      kSharingPart * count_sharing(p, lane) >= p.batch;
+  auto run = [&](auto once) __attribute__((always_inline)) {
+    constexpr bool kOnce = decltype(once)::value;
+    for (;;) {
+      const int len = lens[r];
+      const int n = units_of(len);
+      const int xe = min(n, x + left);
+      const bool whole = x == 0 && xe == n;
+      left -= xe - x;
+      const ScalarInts table = (ScalarInts)(p.block_tables + (size_t)r * p.max_blocks_per_seq);
+      const int last = (len - 1) / kBlock;
+      Rows16<D, kBits> rows;
+      rows.load(j < p.group ? p.q + ((size_t)r * p.num_q_heads + g * p.group + j) * D : nullptr, lane);
+      Softmax<16> soft;
+      f32x4 o[D / 16];
 #pragma unroll
-    for (int t = 0; t < D / 16; ++t) o[t] = f32x4{};
-    Unit<D, kBits> ring[kDepth];
-    int id0 = 0, id1 = 0;
-    auto ids_of = [&](int unit) {
-      id0 = table[kUnitBlocks * unit];
-      id1 = table[min(kUnitBlocks * unit + 1, last)];
-    };
-    int y = x + wave;
-    if (y < xe) ids_of(y);
+      for (int t = 0; t < D / 16; ++t) o[t] = f32x4{};
+      Unit<D, kBits> ring[kDepth];
+      int id0 = 0, id1 = 0;
+      auto ids_of = [&](int unit) {
+        id0 = table[kUnitBlocks * unit];
+        id1 = table[min(kUnitBlocks * unit + 1, last)];
+      };
+      int y = x + wave;
+      if (y < xe) ids_of(y);
 #pragma unroll
-    for (int d = 0; d < kDepth; ++d) {
-      if (y + d * kWaves >= xe) break;
-      ring[d].load(base, stride, id0, id1, lane);
-      if (y + (d + 1) * kWaves < xe) ids_of(y + (d + 1) * kWaves);
-    }
-    while (y < xe) {
+      for (int d = 0; d < kDepth; ++d) {
+        if (y + d * kWaves >= xe) break;
+        ring[d].template load<kOnce>(base, stride, id0, id1, lane);
+        if (y + (d + 1) * kWaves < xe) ids_of(y + (d + 1) * kWaves);
+      }
+      while (y < xe) {
 #pragma unroll
-      for (int d = 0; d < kDepth; ++d, y += kWaves) {
-        if (y >= xe) break;
-        const int seen = len - y * kUnitKeys;
-        if (seen < kUnitKeys) ring[d].cut_values(seen, lane);
-        add_unit<D, kBits>(soft, o, ring[d], rows, c, seen, lane);
-        if (y + kDepth * kWaves < xe) {
-          ring[d].load(base, stride, id0, id1, lane);
-          if (y + (kDepth + 1) * kWaves < xe) ids_of(y + (kDepth + 1) * kWaves);
+        for (int d = 0; d < kDepth; ++d, y += kWaves) {
+          if (y >= xe) break;
+          const int seen = len - y * kUnitKeys;
+          if (seen < kUnitKeys) ring[d].cut_values(seen, lane);
+          add_unit<D, kBits>(soft, o, ring[d], rows, c, seen, lane);
+          if (y + kDepth * kWaves < xe) {
+            ring[d].template load<kOnce>(base, stride, id0, id1, lane);
+            if (y + (kDepth + 1) * kWaves < xe) ids_of(y + (kDepth + 1) * kWaves);
+          }
         }
       }
-    }
-    const float l = quad_sum(soft.l);
-    if (j < p.group) {
+      const float l = quad_sum(soft.l);
+      if (j < p.group) {
 #pragma unroll
-      for (int rr = 0; rr < 4; ++rr)
+        for (int rr = 0; rr < 4; ++rr)
 #pragma unroll
-        for (int t = 0; t < D / 16; t += 4)
-          *reinterpret_cast<f32x4*>(&sm.o[wave][j][D / 4 * (lane >> 4) + D / 16 * rr + t]) =
-              f32x4{o[t][rr], o[t + 1][rr], o[t + 2][rr], o[t + 3][rr]};
-      if (lane < 16) sm.ml[wave][j] = make_float2(soft.m, l);
-    }
-    __syncthreads();
-    for (int i = threadIdx.x; i < p.group * (D / 4); i += kThreads) {
-      const int hj = i / (D / 4), d = i % (D / 4) * 4;
-      float m = sm.ml[0][hj].x;
-#pragma unroll
-      for (int k = 1; k < kWaves; ++k) m = fmaxf(m, sm.ml[k][hj].x);
-      float den = 0.f;
-      f32x4 acc = f32x4{};
-#pragma unroll
-      for (int k = 0; k < kWaves; ++k) {
-        const float wt = __builtin_amdgcn_exp2f(sm.ml[k][hj].x - m);
-        den = __builtin_fmaf(wt, sm.ml[k][hj].y, den);
-        const f32x4 o = *reinterpret_cast<const f32x4*>(&sm.o[k][hj][d]);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) acc[e] = __builtin_fmaf(wt, o[e], acc[e]);
+          for (int t = 0; t < D / 16; t += 4)
+            *reinterpret_cast<f32x4*>(&sm.o[wave][j][D / 4 * (lane >> 4) + D / 16 * rr + t]) =
+                f32x4{o[t][rr], o[t + 1][rr], o[t + 2][rr], o[t + 3][rr]};
+        if (lane < 16) sm.ml[wave][j] = make_float2(soft.m, l);
       }
-      if (whole) {
-        bf16x4 o;
+      __syncthreads();
+      for (int i = threadIdx.x; i < p.group * (D / 4); i += kThreads) {
+        const int hj = i / (D / 4), d = i % (D / 4) * 4;
+        float m = sm.ml[0][hj].x;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) o[e] = (__bf16)(acc[e] / den);
-        *reinterpret_cast<uint2*>(p.out + ((size_t)r * p.num_q_heads + g * p.group + hj) * D + d) =
-            __builtin_bit_cast(uint2, o);
-      } else {
-        const size_t at = ((size_t)g * p.rows + r + w) * p.group + hj;
-        *reinterpret_cast<f32x4*>(p.ws_o + at * D + d) = acc;
-        if (d == 0) *reinterpret_cast<float2*>(p.ws_ml + 2 * at) = make_float2(m, den);
+        for (int k = 1; k < kWaves; ++k) m = fmaxf(m, sm.ml[k][hj].x);
+        float den = 0.f;
+        f32x4 acc = f32x4{};
+#pragma unroll
+        for (int k = 0; k < kWaves; ++k) {
+          const float wt = __builtin_amdgcn_exp2f(sm.ml[k][hj].x - m);
+          den = __builtin_fmaf(wt, sm.ml[k][hj].y, den);
+          const f32x4 o = *reinterpret_cast<const f32x4*>(&sm.o[k][hj][d]);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) acc[e] = __builtin_fmaf(wt, o[e], acc[e]);
+        }
+        if (whole) {
+          bf16x4 o;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) o[e] = (__bf16)(acc[e] / den);
+          *reinterpret_cast<uint2*>(p.out + ((size_t)r * p.num_q_heads + g * p.group + hj) * D + d) =
+              __builtin_bit_cast(uint2, o);
+        } else {
+          const size_t at = ((size_t)g * p.rows + r + w) * p.group + hj;
+          *reinterpret_cast<f32x4*>(p.ws_o + at * D + d) = acc;
+          if (d == 0) *reinterpret_cast<float2*>(p.ws_ml + 2 * at) = make_float2(m, den);
+        }
       }
+      if (left <= 0) return;
+      do ++r;
+      while (lens[r] <= 0);
+      x = 0;
+      __syncthreads();
     }
-    if (left <= 0) return;
-    do ++r;
-    while (lens[r] <= 0);
-    x = 0;
-    __syncthreads();
-  }
+  };
+  if (shared) run(std::false_type{});
+  else run(std::true_type{});
 }
 
 // One work-group per (sequence, KV head) merges what the ranges left of it.
@@ -1033,7 +1073,7 @@ QuantDecodeGeometry quant_decode_geometry(int batch, int max_seq_len, int num_q_
   QuantDecodeGeometry geo = {};
   const double units = (double)((max_seq_len + 31LL) / 32);
   const double most = batch * units;
-  geo.ranges = (decode_groups_per_cu(head_dim) * cus + num_kv_heads - 1) / num_kv_heads;
+  geo.ranges = (kDecodeGroupsPerCu * cus + num_kv_heads - 1) / num_kv_heads;
   if (most < geo.ranges) geo.ranges = most < 1 ? 1 : (int)most;
   geo.rows = (long long)geo.ranges + batch;
   geo.bytes = geo.rows * num_q_heads * (head_dim + 2) * (long long)sizeof(float);
