@@ -76,6 +76,25 @@ def test_decode_many(d, bits):
 
 
 @pytest.mark.parametrize("bits", [4, 8])
+@pytest.mark.parametrize("hq,hkv,d,seqs", [(16, 8, 128, 70), (8, 4, 64, 130)])
+def test_decode_on_a_shared_anchor(hq, hkv, d, seqs, bits):
+    """Enough sequences on one anchor of 40 blocks that its blocks are asked for and loaded to stay in
+    the caches; some end inside it or before its 32nd block, some are empty."""
+    rng = np.random.default_rng(7)
+    lens = list(rng.integers(640, 1100, seqs - 6)) + [0, 5, 496, 497, 640, 0]
+    scale = float(np.float32(d ** -0.5))
+    print(f"[case] decode of {seqs} sequences on an anchor, {hq}/{hkv} heads of {d}, {bits} bits", flush=True)
+    pg = QuantPaged(7, lens, hkv, d, bits, shared=40)
+    q = bf16_bits(pg.rng, len(lens), hq, d)
+    got = run_decode(pg, q, bits, scale)
+    for r, n in enumerate(lens):
+        if n == 0:
+            assert (got[r] == 0).all()
+        elif r % 7 == 0 or r > seqs - 7:
+            check_rows(got[r:r + 1], q[r:r + 1], pg, r, n - 1, hq, hkv, scale)
+
+
+@pytest.mark.parametrize("bits", [4, 8])
 def test_decode_loose_bound_and_workspace(bits):
     """A bound far above the lengths, and a workspace tensor larger than needed."""
     ws = torch.full((1 << 26,), 0xFF, dtype=torch.uint8, device="cuda")      # NaN, were it read
