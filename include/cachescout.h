@@ -787,8 +787,9 @@ int cs_kv_dequantize(const void *quant_pool, const int32_t *src_block_ids,
  *
  * Arithmetic: fp32 logits, of bf16 products, or at 4 bits of the query's products with the codes:
  * a query feature is there held as two 8-bit numbers, exact unless it is more than 2^14 times
- * smaller than the largest of its group of 32, and then off by at most 2^-22 of that one.  (Query
- * features from 1.8125 * 2^127 on count as infinite.)  Probabilities are rounded to bf16 for the
+ * smaller than the largest of its group of 32, and then off by at most 2^-22 of that one, or below
+ * 2^-117, and then off by at most 2^-127.  (Query features from 1.8125 * 2^127 on count as
+ * infinite.)  Probabilities are rounded to bf16 for the
  * product with V, the output to nearest-even bf16.  A row's low bits may change with the rest of
  * the batch, as there; the result is the same from run to run.
  *
@@ -817,6 +818,9 @@ int64_t cs_decode_quant_workspace_bytes(int32_t batch, int32_t max_seq_len, int3
 /*
  * Prefill attention over a quantised pool: cs_prefill_paged_attn with K and V, of the prefix and
  * of the suffix itself, the values that quant_pool holds; arithmetic as in cs_decode_quant_attn.
+ * A suffix token's V that is NaN may also reach rows of the invocation before it (its probability
+ * there is 0, but 0 times NaN is NaN); NaN keys, and what lies behind an invocation's last token,
+ * reach only the rows that see them.
  *
  * Arguments as in cs_prefill_paged_attn, except
  *   quant_pool     device, as above, of num_blocks blocks of `bits` (4 or 8) bits.

@@ -3,17 +3,17 @@
 //
 //   out = sum_j softmax_j(scale * q . K_j) V_j,   K, V the values of the pool's codes
 //
-// Both kernels are made of waves that need nothing of each other in the loop: a wave takes 16
-// or 32 query rows (token, query head of the KV head) and a run of keys, 32 at a time, and no
-// LDS.  With S^T = K Q^T and O^T = V^T P^T on 16 x 16 tiles, S^T leaves the matrix unit in the very
-// registers that P^T enters it from (a lane's keys 4q .. 4q + 3 of the two blocks), and the
-// tile's layout (quant_tile.h) gives K and V to the lanes that need them.
-//   * 4 bits: K goes into the matrix unit as it is (v_mfma_scale_f32_16x16x128_f8f6f4, codes and
-//     scales from the pool).  Its partner then has to be of 8 bits or fewer: Q is the sum of two
-//     E4M3 numbers with scales of their own, which holds bf16's 8 bits (a 4-bit head and what
-//     is left, of 4 bits again); features more than 2^14 below the largest of their group of
-//     32 are off by 2^-22 of that largest at most.  At D = 64 the two halves of the contracted
-//     index hold the head and the rest, so it is one product.
+// With S^T = K Q^T and O^T = V^T P^T, S^T leaves the matrix unit in the very registers that P^T
+// enters it from: a lane's keys of S^T are the ones it is to supply of P^T, in the order that the
+// V^T operand takes them in too, and the tile's layout (quant_tile.h) gives K and V to the lanes
+// that need them.  Decode works on 16 rows (the heads of a KV head) and keeps what it reads in
+// registers; prefill works on 32 rows a wave and shares conversions through LDS.
+//   * 4 bits: K goes into the matrix unit as it is (v_mfma_scale_f32_*_f8f6f4, codes and scales
+//     from the pool).  Its partner then has to be of 8 bits or fewer: Q is the sum of two E4M3
+//     numbers with scales of their own, which holds bf16's 8 bits (a 4-bit head and what is left,
+//     of 4 bits again); features more than 2^14 below the largest of their group of 32 are off by
+//     2^-22 of that largest at most.  In 16 x 16 products at D = 64 the two halves of the
+//     contracted index hold the head and the rest, so it is one product.
 //   * 8 bits: K is converted to bf16.  (8-bit times 8-bit products sum up with errors of 3e-5 of
 //     the largest, where 4-bit times 8-bit ones are exact to fp32's 5e-8.)
 //   * V is converted to bf16, two features of a key at a time, which two byte permutes then
@@ -1118,8 +1118,9 @@ QuantPrefillGeometry quant_prefill_geometry(int batch, int total_q, int max_q_le
   if (parts > kPrefillMaxParts) parts = kPrefillMaxParts;
   geo.parts = parts < 1 ? 1 : (int)parts;
   const double grid = (double)geo.tiles * batch * num_kv_heads * geo.parts;
-  // (an invocation's rows of a KV head are counted in 32 bits)
-  geo.fits = launch_fits(grid, kThreads) && max_q_len * group < 0x7fffff00LL &&
+  // (an invocation's rows of a KV head, and its keys up to the end of the step after next, are counted
+  // in 32 bits)
+  geo.fits = launch_fits(grid, kThreads) && max_q_len * group < 0x7fffff00LL && max_kv_len < 0x7fffff00LL &&
              (geo.parts == 1 || launch_fits((double)total_q * num_q_heads * (head_dim / 4) / kThreads + 1, kThreads));
   if (!geo.fits) return geo;
   geo.grid = (long long)grid;
