@@ -695,9 +695,9 @@ __global__ __launch_bounds__(kMergeThreads) void quant_decode_merge_kernel(Quant
 // Prefill.  Rows of a KV head are (token, query head of it), heads fastest; a wave takes 32 of them,
 // or at D = 64, where the launch fills the device so, 64 (kTiles).  A work-group's steps are 64
 // keys: each wave reads one of the four blocks ahead into registers, and a step later leaves it in
-// LDS as all waves then take it, K's codes as they are, V as bf16 fragments, so that a
-// conversion is done once for the work-group's rows.  A step's buffer is written while the other one
-// is read: one barrier a step.
+// LDS as all waves then take it, K's 4-bit codes as they are, 8-bit K and V as bf16 fragments, so that
+// a conversion is done once for the work-group's rows.  A step's buffer is written while the other
+// one is read: one barrier a step.
 //
 // Within a wave the matrix unit works on the logits of the next 32 keys and the values of the last
 // 32 while the vector unit makes the weights of the present ones.  Several parts of a tile's keys
@@ -710,9 +710,9 @@ constexpr int kStepKeys = 16 * kStepBlocks;
 // values of blocks 4 x - 2 .. 4 x + 1.
 template <int D, int kBits>
 struct PrefillLds {
-  // lane by lane what Block holds of K, and V^T fragments
-  u32x4 k[2][kStepBlocks][Block<D, kBits>::kKWords / 4][64];
-  int ks[2][kStepBlocks][64];
+  // of K at 4 bits lane by lane what Block holds, at 8 bits fragments of 16 keys; V^T fragments
+  u32x4 k[2][kStepBlocks][kBits == 4 ? 1 : D / 32][64];
+  int ks[2][kBits == 4 ? kStepBlocks : 1][64];
   u32x4 v[2][kStepBlocks][D / 32][64];
 };
 
@@ -767,11 +767,21 @@ __global__ __launch_bounds__(kThreads, kTiles == 1 ? 2 : 1) void quant_prefill_k
     block.load_values(Block<D, kBits>::tile(base, stride, b < kStepBlocks * x0 ? -1 : table[min(b, last)]), lane);
   };
   auto store_keys = [&](int step) __attribute__((always_inline)) {
+    if constexpr (kBits == 4) {
+      sm.k[step & 1][wave][0][lane] = u32x4{block.k[0], block.k[1], block.k[2], block.k[3]};
+      sm.ks[step & 1][wave][lane] = block.ks;
+    } else {
+      // lane (key, qd)'s features D / 4 qd + 8 i .. + 7: step s of the products, half h of the wave
+      const float scale = scale_of(block.ks);
+      const int qd = lane >> 4;
 #pragma unroll
-    for (int i = 0; i < Block<D, kBits>::kKWords / 4; ++i)
-      sm.k[step & 1][wave][i][lane] =
-          u32x4{block.k[4 * i], block.k[4 * i + 1], block.k[4 * i + 2], block.k[4 * i + 3]};
-    sm.ks[step & 1][wave][lane] = block.ks;
+      for (int i = 0; i < D / 32; ++i) {
+        const int step8 = qd % 2 * (D / 32) + i;
+        (&sm.k[step & 1][wave][0][0])[(step8 * 2 + qd / 2) * 16 + (lane & 15)] =
+            u32x4{read_pair<8>(block.k[2 * i], scale, 0), read_pair<8>(block.k[2 * i], scale, 1),
+                  read_pair<8>(block.k[2 * i + 1], scale, 0), read_pair<8>(block.k[2 * i + 1], scale, 1)};
+      }
+    }
   };
   // Of a 32 x 16 fragment of V^T lane l holds feature group l & 31, D / 32 features each in as many
   // fragments, and of the block's keys 4 h .. + 3 and 8 + 4 h .. + 3, h = l >> 5, as P's lanes do.
@@ -821,8 +831,8 @@ __global__ __launch_bounds__(kThreads, kTiles == 1 ? 2 : 1) void quant_prefill_k
   // The work of half a step comes in as many chunks as its logits take products of 64 cycles.
   constexpr int kChunks = D / 32;
   struct Keys {
-    u32x4 w[kChunks / (kBits == 4 ? 2 : 1)];
-    int ks[kBits == 4 ? kChunks / 2 : 2];
+    u32x4 w[kBits == 4 ? kChunks / 2 : 2 * kChunks];
+    int ks[kBits == 4 ? kChunks / 2 : 1];
   };
   auto read_keys = [&](int step, int half) __attribute__((always_inline)) {
     const int buf = step & 1, b = 2 * half + k_block;
@@ -835,11 +845,7 @@ __global__ __launch_bounds__(kThreads, kTiles == 1 ? 2 : 1) void quant_prefill_k
       }
     } else {
 #pragma unroll
-      for (int x = 0; x < 2; ++x) {
-#pragma unroll
-        for (int i = 0; i < D / 64; ++i) k.w[x * (D / 64) + i] = sm.k[buf][b][i][(2 * k_half + x) * 16 + key];
-        k.ks[x] = sm.ks[buf][b][(2 * k_half + x) * 16 + key];
-      }
+      for (int i = 0; i < D / 16; ++i) k.w[i] = (&sm.k[buf][b][0][0])[(2 * i + k_half) * 16 + key];
     }
     return k;
   };
@@ -852,16 +858,12 @@ __global__ __launch_bounds__(kThreads, kTiles == 1 ? 2 : 1) void quant_prefill_k
         s[x] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, rows[x].q[chunk / 2][chunk % 2], s[x], 4, 0, 0,
                                                                k.ks[chunk / 2], 0, rows[x].scale[chunk / 2][chunk % 2]);
     } else {
-      const float scale = scale_of(k.ks[chunk / (D / 64)]);
-      const u32x4 w = k.w[chunk];
 #pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const u32x4 a = {read_pair<8>(w[2 * e], scale, 0), read_pair<8>(w[2 * e], scale, 1),
-                         read_pair<8>(w[2 * e + 1], scale, 0), read_pair<8>(w[2 * e + 1], scale, 1)};
+      for (int e = 2 * chunk; e < 2 * chunk + 2; ++e) {
+        const u32x4 a = k.w[e];
 #pragma unroll
         for (int x = 0; x < kTiles; ++x)
-          s[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), rows[x].q[2 * chunk + e], s[x], 0,
-                                                         0, 0);
+          s[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), rows[x].q[e], s[x], 0, 0, 0);
       }
     }
   };
