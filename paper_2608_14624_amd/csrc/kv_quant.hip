@@ -131,7 +131,8 @@ __global__ __launch_bounds__(kThreads) void kv_write_quant_kernel(QuantCopyLaunc
     x[i] = u32x4{};
     if (t >= a.n) continue;
     slot[i] = a.ids[t];
-    x[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(src + ((size_t)t * a.num_kv_heads + h) * D + 8 * part));
+    const uint16_t* row = src + ((size_t)t * a.num_kv_heads + h) * D;
+    x[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(row + 8 * part));
   }
 #pragma unroll
   for (int i = 0; i < R::kRows; ++i) {
@@ -158,7 +159,8 @@ __global__ __launch_bounds__(kThreads) void kv_quantize_kernel(QuantCopyLaunch a
   const int part = R::part(lane);
   u32x4 x[R::kRows];
 #pragma unroll
-  for (int k = 0; k < R::kRows; ++k) x[k] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(src + (R::first(lane) + k) * D + 8 * part));
+  for (int k = 0; k < R::kRows; ++k)
+    x[k] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(src + (R::first(lane) + k) * D + 8 * part));
 #pragma unroll
   for (int k = 0; k < R::kRows; ++k) {
     int byte;
@@ -203,7 +205,8 @@ __global__ __launch_bounds__(kThreads) void kv_dequantize_kernel(QuantCopyLaunch
           c[k][0] = *reinterpret_cast<const uint16_t*>(at) |
                     (uint32_t)*reinterpret_cast<const uint16_t*>(at + 16 * T::kPartBytes) << 16;
         else
-          c[k] = u32x2{*reinterpret_cast<const uint32_t*>(at), *reinterpret_cast<const uint32_t*>(at + 16 * T::kPartBytes)};
+          c[k] = u32x2{*reinterpret_cast<const uint32_t*>(at),
+                       *reinterpret_cast<const uint32_t*>(at + 16 * T::kPartBytes)};
       }
       byte[k] = tile[T::kVScales + part / 4 * 16 + key];
     }

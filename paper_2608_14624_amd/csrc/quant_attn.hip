@@ -346,28 +346,6 @@ struct Block {
     }
   }
 
-  // The codes of half the lane's features, kPart / 2 of each of its keys, in the low bits
-  __device__ __forceinline__ void half_values(int part, uint32_t (&codes)[4]) const {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      if constexpr (T::kPartBytes == 8) codes[i] = part ? v[2 * i + 1] : v[2 * i];
-      else if constexpr (T::kPartBytes == 4) codes[i] = v[i] >> (16 * part);
-      else codes[i] = v[i / 2] >> (16 * (i % 2) + 8 * part);
-    }
-  }
-  // Of such codes feature 2 pair, in f[0], and 2 pair + 1: the lane's four keys
-  __device__ __forceinline__ static void fragments(const uint32_t (&codes)[4], int pair, const float (&scale)[4],
-                                                   u32x2 (&f)[2]) {
-    uint32_t x[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) x[i] = read_pair<kBits>(codes[i], scale[i], pair);
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      f[0][i] = __builtin_amdgcn_perm(x[2 * i + 1], x[2 * i], 0x05040100u);
-      f[1][i] = __builtin_amdgcn_perm(x[2 * i + 1], x[2 * i], 0x07060302u);
-    }
-  }
-
   __device__ __forceinline__ void value_scales(float (&scale)[4]) const {
     scale[0] = __builtin_bit_cast(float, (vs & 0xffu) << 23);
     scale[1] = __builtin_bit_cast(float, (vs & 0xff00u) << 15);
@@ -485,7 +463,9 @@ __device__ __forceinline__ void add_unit(Softmax<16>& soft, f32x4 (&o)[D / 16], 
 // Decode.  The batch's keys are counted in units of 32 and dealt to `ranges` work-groups per KV
 // head in equal contiguous ranges.  A work-group's waves take the units of a piece (a sequence's
 // part of the range) in turn and merge in LDS; a sequence cut over several ranges leaves partial
-// results (O relative to m, m, and l) that a second kernel merges.
+// results (O relative to m, m, and l) that a second kernel merges.  Bound by HBM: 128 sequences of 4.2k-10.8k
+// keys, 32 / 8 heads of 128, take 172 us at 4 bits (1.08 GB, 6.2 TB/s).  Where sequences share anchors, by the
+// loads through L1 and L2 instead: 61 of them at 8 bits take 93 us, the loads alone 88, all else 52.
 
 __device__ __forceinline__ int total_units(const QuantParams& p, int lane) {
   int total = 0;
@@ -699,9 +679,19 @@ __global__ __launch_bounds__(kMergeThreads) void quant_decode_merge_kernel(Quant
 // a conversion is done once for the work-group's rows.  A step's buffer is written while the other
 // one is read: one barrier a step.
 //
-// Within a wave the matrix unit works on the logits of the next 32 keys and the values of the last
-// 32 while the vector unit makes the weights of the present ones.  Several parts of a tile's keys
-// on as many work-groups leave partial results.
+// Within a wave the logits of the next 32 keys, the weights of the present ones and the values of the
+// last 32 stand side by side, so that the matrix unit's work does not depend on the vector unit's.
+// Several parts of a tile's keys on as many work-groups leave partial results.
+//
+// us a call: 64 / 8 heads of 128, 4 x (4096 + 512), 4 bits 252 (1.16 PFLOP/s; a large bf16 product of
+// the library reaches 1.24); 32 / 8 heads, 16 ragged invocations, 8 bits 1003 (0.93).  Bound by the step's
+// own work: of 305 us in short runs of the first the products alone take 135, and all but the
+// products 177 (LDS reads and barriers 95, weights 47, conversions and their loads and stores 34),
+// which overlap little.  Each wave converting all for itself took 317 and 2850; 16 x 16 products,
+// three waves a SIMD and, at D = 128, 64 rows a wave (O in accumulation registers) were as fast or
+// slower; loads one more step ahead, the rows' all at once, are within 1% both ways.  Of a small launch
+// (83 rows x 32 / 8 heads on 3094 keys, 21 us in this kernel) a wave alone on its SIMD takes 1.3 us a
+// step, 6 to get to the second step, and 4 to store its partial results.
 
 constexpr int kStepBlocks = kWaves;
 constexpr int kStepKeys = 16 * kStepBlocks;
@@ -763,8 +753,10 @@ __global__ __launch_bounds__(kThreads, kTiles == 1 ? 2 : 1) void quant_prefill_k
   Block<D, kBits> block;
   auto load = [&](int key_step, int value_step) __attribute__((always_inline)) {
     const int b = kStepBlocks * value_step - 2 + wave;
-    block.load_keys(Block<D, kBits>::tile(base, stride, table[max(0, min(kStepBlocks * key_step + 2 + wave, last))]), lane);
-    block.load_values(Block<D, kBits>::tile(base, stride, b < kStepBlocks * x0 ? -1 : table[min(b, last)]), lane);
+    const int k_id = table[max(0, min(kStepBlocks * key_step + 2 + wave, last))];
+    const int v_id = b < kStepBlocks * x0 ? -1 : table[min(b, last)];
+    block.load_keys(Block<D, kBits>::tile(base, stride, k_id), lane);
+    block.load_values(Block<D, kBits>::tile(base, stride, v_id), lane);
   };
   auto store_keys = [&](int step) __attribute__((always_inline)) {
     if constexpr (kBits == 4) {
@@ -886,8 +878,8 @@ __global__ __launch_bounds__(kThreads, kTiles == 1 ? 2 : 1) void quant_prefill_k
 #pragma unroll
         for (int i = 0; i < 16; ++i) s[y][i] = key0 + 8 * (i / 4) + 4 * k_half + i % 4 < end[y] ? s[y][i] : -INFINITY;
     }
-    // A wave issues in order, and a product that waits for the matrix unit, or for the one before
-    // it in its sum, holds up what stands behind it: so they are dealt out among the weights.
+    // Chunk by chunk, so that a fragment is read one chunk before its products and few are held at a
+    // time (the order within a chunk makes no difference that was measured)
     __builtin_amdgcn_sched_barrier(0);
     const Keys keys = read_keys(x, half);
     bf16x8 f[2][2];
@@ -1126,7 +1118,8 @@ QuantPrefillGeometry quant_prefill_geometry(int batch, int total_q, int max_q_le
              (geo.parts == 1 || launch_fits((double)total_q * num_q_heads * (head_dim / 4) / kThreads + 1, kThreads));
   if (!geo.fits) return geo;
   geo.grid = (long long)grid;
-  geo.bytes = geo.parts == 1 ? 0 : (long long)geo.parts * total_q * num_q_heads * (head_dim + 2) * (long long)sizeof(float);
+  if (geo.parts > 1)
+    geo.bytes = (long long)geo.parts * total_q * num_q_heads * (head_dim + 2) * (long long)sizeof(float);
   return geo;
 }
 
@@ -1136,8 +1129,9 @@ hipError_t launch_quant_prefill(const QuantAttnLaunch& a, const QuantPrefillGeom
   p.tiles = (int)geo.tiles;
   p.ws_o = a.workspace;
   p.ws_ml = a.workspace + (long long)geo.parts * a.total_q * a.num_q_heads * a.head_dim;
-  if (a.head_dim == 64) return a.bits == 4 ? prefill<64, 4>(p, geo.wave_tiles, geo.grid, stream) : prefill<64, 8>(p, geo.wave_tiles, geo.grid, stream);
-  return a.bits == 4 ? prefill<128, 4>(p, geo.wave_tiles, geo.grid, stream) : prefill<128, 8>(p, geo.wave_tiles, geo.grid, stream);
+  auto* run = a.head_dim == 64 ? (a.bits == 4 ? prefill<64, 4> : prefill<64, 8>)
+                               : (a.bits == 4 ? prefill<128, 4> : prefill<128, 8>);
+  return run(p, geo.wave_tiles, geo.grid, stream);
 }
 
 }  // namespace cs
