@@ -288,6 +288,51 @@ struct Block {
     vs = __builtin_amdgcn_raw_buffer_load_b32(rs, T::kVScales + c * T::kPart / kScaleGroup * 16 + 4 * qd, 0, 0);
   }
 
+  // The same by whole lines, where a key's codes, and those of a group of V, are lines of 128 bytes: lane
+  // l holds bytes 16 (l % 8) .. + 15 of lines l / 8 and 8 + l / 8 of K and of V, until `arrange`.  (The
+  // loads above have 16 neighbouring lanes take 16 bytes of as many lines, and a compute unit then
+  // reads 16 bytes a clock.  us a call: the 61 sequences of the decode's comment 96 so and 65 by lines, the
+  // 128 at 8 bits 350 and 320.  With rows of 64 bytes there was nothing to gain.)
+  static constexpr bool kLines = T::kRowBytes == 128;
+  template <int kPolicy = 0>
+  __device__ __forceinline__ void load_lines(__amdgpu_buffer_rsrc_t rs, int lane) {
+    const int key = lane & 15, qd = lane >> 4;
+#pragma unroll
+    for (int w = 0; w < 2; ++w) {
+      const u32x4 a = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rs, 1024 * w + 16 * lane, 0, kPolicy));
+      const u32x4 b = __builtin_bit_cast(
+          u32x4, __builtin_amdgcn_raw_buffer_load_b128(rs, T::kV + 1024 * w + 16 * lane, 0, kPolicy));
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        k[4 * w + i] = a[i];
+        v[4 * w + i] = b[i];
+      }
+    }
+    ks = __builtin_amdgcn_raw_buffer_load_b8(rs, T::kKScales + key * T::kGroups + qd, 0, 0);
+    vs = __builtin_amdgcn_raw_buffer_load_b32(rs, T::kVScales + key / 4 * 16 + 4 * qd, 0, 0);
+  }
+  // ... through 4096 bytes of LDS that only this wave uses (its accesses are in order).  Chunk c of line
+  // r stands at c ^ (r & 7), so that eight lanes' chunks are in different banks both ways.
+  __device__ __forceinline__ void arrange(uint8_t* lds, int lane) {
+    uint8_t* to = lds + lane / 8 * 128 + (lane % 8 ^ lane / 8) * 16;
+    const int from = (lane & 15) * 128 + (2 * (lane >> 4) ^ (lane & 7)) * 16;
+#pragma unroll
+    for (int w = 0; w < 2; ++w) {
+      *reinterpret_cast<u32x4*>(to + 1024 * w) = u32x4{k[4 * w], k[4 * w + 1], k[4 * w + 2], k[4 * w + 3]};
+      *reinterpret_cast<u32x4*>(to + 2048 + 1024 * w) = u32x4{v[4 * w], v[4 * w + 1], v[4 * w + 2], v[4 * w + 3]};
+    }
+#pragma unroll
+    for (int w = 0; w < 2; ++w) {
+      const u32x4 a = *reinterpret_cast<const u32x4*>(lds + (from ^ 16 * w));
+      const u32x4 b = *reinterpret_cast<const u32x4*>(lds + 2048 + (from ^ 16 * w));
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        k[4 * w + i] = a[i];
+        v[4 * w + i] = b[i];
+      }
+    }
+  }
+
   // What stands behind `n` keys of the block is not the sequence's: V there becomes zero (its
   // weights are 0, but 0 times a NaN is NaN).
   __device__ __forceinline__ void cut_values(int n, int lane) {
@@ -358,15 +403,26 @@ struct Block {
 template <int D, int kBits>
 struct Unit {
   Block<D, kBits> b[2];
-  // kOnce: no other sequence is known to read the blocks, so they need not stay in the caches.  (At 8
-  // bits a lane's codes of K are 32 bytes, two loads that take half of every line each.)
+  // kOnce: no other sequence is known to read the blocks, so they need not stay in the caches
   template <bool kOnce>
   __device__ __forceinline__ void load(const uint8_t* base, size_t stride, int id0, int id1, int lane) {
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       const __amdgpu_buffer_rsrc_t rs = Block<D, kBits>::tile(base, stride, i ? id1 : id0);
-      b[i].template load_keys<kOnce && kBits == 4 ? kNonTemporal : 0>(rs, lane);
-      b[i].template load_values<kOnce ? kNonTemporal : 0>(rs, lane);
+      if constexpr (Block<D, kBits>::kLines) {
+        b[i].template load_lines<kOnce ? kNonTemporal : 0>(rs, lane);
+      } else {
+        b[i].template load_keys<kOnce && kBits == 4 ? kNonTemporal : 0>(rs, lane);
+        b[i].template load_values<kOnce ? kNonTemporal : 0>(rs, lane);
+      }
+    }
+  }
+  // `lds`: kArea bytes that only this wave uses
+  static constexpr int kArea = Block<D, kBits>::kLines ? 2 * 4096 : 0;
+  __device__ __forceinline__ void arrange(uint8_t* lds, int lane) {
+    if constexpr (Block<D, kBits>::kLines) {
+      b[0].arrange(lds, lane);
+      b[1].arrange(lds + 4096, lane);
     }
   }
   __device__ __forceinline__ void cut_values(int n, int lane) {
@@ -464,8 +520,9 @@ __device__ __forceinline__ void add_unit(Softmax<16>& soft, f32x4 (&o)[D / 16], 
 // head in equal contiguous ranges.  A work-group's waves take the units of a piece (a sequence's
 // part of the range) in turn and merge in LDS; a sequence cut over several ranges leaves partial
 // results (O relative to m, m, and l) that a second kernel merges.  Bound by HBM: 128 sequences of 4.2k-10.8k
-// keys, 32 / 8 heads of 128, take 172 us at 4 bits (1.08 GB, 6.2 TB/s).  Where sequences share anchors, by the
-// loads through L1 and L2 instead: 61 of them at 8 bits take 93 us, the loads alone 88, all else 52.
+// keys, 32 / 8 heads of 128, take 172 us at 4 bits (1.08 GB, 6.2 TB/s), 320 at 8 (6.5).  Where sequences
+// share anchors, by conversions and products instead: 64 / 8 heads, 61 sequences, 8 bits, 65 us, of
+// which all but the loads 52; with every anchor in L2 61.
 
 __device__ __forceinline__ int total_units(const QuantParams& p, int lane) {
   int total = 0;
@@ -502,15 +559,16 @@ __device__ __forceinline__ int count_sharing(const QuantParams& p, int lane) {
 // Units that a wave's registers hold, one of them being attended while the others are on their way,
 // and work-groups per compute unit, to which a decode's keys are dealt: all run at once.  us a call
 // of 128 sequences of 4.2k-10.8k keys, 32 / 8 heads of 128, at 4 bits: 4 units and 2 work-groups 175, 3 and 2
-// 177, 6 and 2 178, 2 and 3 179, 3 and 3 183; at 8 bits 3 and 2 363, 2 and 3 379.
+// 177, 6 and 2 178, 2 and 3 179, 3 and 3 183; at 8 bits 3 and 2 320, 2 and 2 320, 2 and 3 336.
 constexpr int decode_depth(int head_dim, int bits) { return head_dim == 128 && bits == 8 ? 3 : 4; }
 constexpr int kDecodeGroupsPerCu = 2;
 // Blocks are loaded as read once (non-temporal) unless at least one sequence in kSharingPart shares
 // them, in launches of at least kSharedUnits units a work-group; in smaller ones the answer is not worth
-// waiting for.  us a call so and with ordinary loads: those 128 sequences at 4 bits 175 and 205, at 8 bits 348 and
-// 363; 61 sequences of 4 agents with 4096 shared keys and 100-3000 of their own, 64 / 8 heads, 55 and 49 at 4
-// bits, 102 and 94 at 8.  (Pieces cut at the same positions of all sequences, dealt so that the
-// work-groups that run at one time share them, raise the L2's hits from 49% to 68% there and take 108.)
+// waiting for.  us a call so and with ordinary loads: those 128 sequences at 4 bits 173 and 200, at 8 bits 320 and
+// 363; 61 sequences of 4 agents with 4096 shared keys and 100-3000 of their own, 64 / 8 heads, 52 and 49 at 4
+// bits, 84 and 65 at 8.  (Pieces cut at the same positions of all sequences, dealt so that the
+// work-groups that run at one time share them, raised the L2's hits from 49% to 68% there, but took 108 us
+// where 96 had been.)
 constexpr int kSharingPart = 4;
 constexpr int kSharedUnits = 16;
 
@@ -521,6 +579,9 @@ __global__ __launch_bounds__(kThreads, kDecodeGroupsPerCu) void quant_decode_ker
   __shared__ DecodeLds<D> sm;
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  // a wave's part of `o`, which it writes after its last unit, and others read between two barriers
+  static_assert(sizeof(sm.o[0]) >= Unit<D, kBits>::kArea, "a unit is arranged there");
+  uint8_t* area = reinterpret_cast<uint8_t*>(sm.o[wave]);
   const int g = blockIdx.x % p.num_kv_heads;
   const int w = blockIdx.x / p.num_kv_heads;
   const ScalarInts lens = (ScalarInts)p.lens;
@@ -587,6 +648,7 @@ __global__ __launch_bounds__(kThreads, kDecodeGroupsPerCu) void quant_decode_ker
         for (int d = 0; d < kDepth; ++d, y += kWaves) {
           if (y >= xe) break;
           const int seen = len - y * kUnitKeys;
+          ring[d].arrange(area, lane);
           if (seen < kUnitKeys) ring[d].cut_values(seen, lane);
           add_unit<D, kBits>(soft, o, ring[d], rows, c, seen, lane);
           if (y + kDepth * kWaves < xe) {
