@@ -299,7 +299,8 @@ struct Block {
     const int key = lane & 15, qd = lane >> 4;
 #pragma unroll
     for (int w = 0; w < 2; ++w) {
-      const u32x4 a = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rs, 1024 * w + 16 * lane, 0, kPolicy));
+      const u32x4 a = __builtin_bit_cast(
+          u32x4, __builtin_amdgcn_raw_buffer_load_b128(rs, 1024 * w + 16 * lane, 0, kPolicy));
       const u32x4 b = __builtin_bit_cast(
           u32x4, __builtin_amdgcn_raw_buffer_load_b128(rs, T::kV + 1024 * w + 16 * lane, 0, kPolicy));
 #pragma unroll
@@ -521,8 +522,8 @@ __device__ __forceinline__ void add_unit(Softmax<16>& soft, f32x4 (&o)[D / 16], 
 // part of the range) in turn and merge in LDS; a sequence cut over several ranges leaves partial
 // results (O relative to m, m, and l) that a second kernel merges.  Bound by HBM: 128 sequences of 4.2k-10.8k
 // keys, 32 / 8 heads of 128, take 172 us at 4 bits (1.08 GB, 6.2 TB/s), 320 at 8 (6.5).  Where sequences
-// share anchors, by conversions and products instead: 64 / 8 heads, 61 sequences, 8 bits, 65 us, of
-// which all but the loads 52; with every anchor in L2 61.
+// share anchors, by conversions and products: 64 / 8 heads, 61 sequences, 8 bits, 65 us (73 where the caches
+// are cold), of which all but the loads 52; with every anchor in L2 61.
 
 __device__ __forceinline__ int total_units(const QuantParams& p, int lane) {
   int total = 0;
@@ -745,7 +746,7 @@ __global__ __launch_bounds__(kMergeThreads) void quant_decode_merge_kernel(Quant
 // last 32 stand side by side, so that the matrix unit's work does not depend on the vector unit's.
 // Several parts of a tile's keys on as many work-groups leave partial results.
 //
-// us a call: 64 / 8 heads of 128, 4 x (4096 + 512), 4 bits 252 (1.16 PFLOP/s; a large bf16 product of
+// us a call: 64 / 8 heads of 128, 4 x (4096 + 512), 4 bits 247 (1.18 PFLOP/s; a large bf16 product of
 // the library reaches 1.24); 32 / 8 heads, 16 ragged invocations, 8 bits 1003 (0.93).  Bound by the step's
 // own work: of 305 us in short runs of the first the products alone take 135, and all but the
 // products 177 (LDS reads and barriers 95, weights 47, conversions and their loads and stores 34),

@@ -102,3 +102,5 @@ def test_workspace_sizes():
     assert ops.decode_quant_workspace_bytes(1, 2 ** 30, 32, 8, 128, 256) == -1
     assert ops.decode_quant_workspace_bytes(2 ** 24, 100, 32, 8, 128, 256) == -1
     assert ops.prefill_quant_workspace_bytes(2 ** 16, 2 ** 30, 2 ** 14, 2 ** 14, 32, 8, 128, 256) == -1
+    assert ops.prefill_quant_workspace_bytes(1, 8, 8, 0x7fffff00, 32, 8, 128, 256) == -1
+    assert ops.prefill_quant_workspace_bytes(1, 8, 8, 0x7ffffeff, 32, 8, 128, 256) > 0
