@@ -6,8 +6,8 @@
 // With S^T = K Q^T and O^T = V^T P^T, S^T leaves the matrix unit in the very registers that P^T
 // enters it from: a lane's keys of S^T are the ones it is to supply of P^T, in the order that the
 // V^T operand takes them in too, and the tile's layout (quant_tile.h) gives K and V to the lanes
-// that need them.  Decode works on 16 rows (the heads of a KV head) and keeps what it reads in
-// registers; prefill works on 32 rows a wave and shares conversions through LDS.
+// that need them.  Decode works on 16 rows (the heads of a KV head), each wave on
+// keys of its own; prefill works on 32 rows a wave and shares conversions through LDS.
 //   * 4 bits: K goes into the matrix unit as it is (v_mfma_scale_f32_*_f8f6f4, codes and scales
 //     from the pool).  Its partner then has to be of 8 bits or fewer: Q is the sum of two E4M3
 //     numbers with scales of their own, which holds bf16's 8 bits (a 4-bit head and what is left,
