@@ -790,7 +790,8 @@ int cs_kv_dequantize(const void *quant_pool, const int32_t *src_block_ids,
  * smaller than the largest of its group of 32, and then off by at most 2^-22 of that one, or below
  * 2^-117, and then off by at most 2^-127.  (Query features from 1.8125 * 2^127 on count as
  * infinite.)  Probabilities are rounded to bf16 for the
- * product with V, the output to nearest-even bf16.  A row's low bits may change with the rest of
+ * product with V, the output to nearest-even bf16.  V of every size is added up without overflow; an
+ * output of n keys is besides off by up to n * 2^-81.  A row's low bits may change with the rest of
  * the batch, as there; the result is the same from run to run.
  *
  * Arguments as in cs_paged_decode_attn_ws, except

@@ -18,8 +18,8 @@
 //     the largest, where 4-bit times 8-bit ones are exact to fp32's 5e-8.)
 //   * V is converted to bf16, two features of a key at a time, which two byte permutes then
 //     pair up by keys.
-// The running maximum that the exponentials are relative to follows the logits only when the
-// weights of a lane's keys add up to more than 2^16: bf16 holds large numbers as well as 1, and most
+// The reference that the exponentials are relative to follows the logits only when the weights of a
+// lane's keys have become 2^16 times as large as it left them: bf16 holds numbers of any size, and most
 // steps rescale nothing, look for no maximum and exchange nothing between lanes.
 #include "decode_common.h"
 #include "internal.h"
@@ -38,7 +38,13 @@ typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kWaves = 4;             // of a work-group, both kernels
 constexpr int kThreads = 64 * kWaves;
-constexpr float kLargeSum = 65536.f;  // of a lane's weights of 32 keys, where their reference moves
+// The sum of a lane's weights of 32 keys at which their reference moves, and how far above the largest
+// logit it goes then.  A row's weights of n keys add up to n / 8 * kLargeSum at most, below 1 for every
+// length, so that O, which is relative to the same reference, holds what V holds, up to 448 * 2^119.  (Weights
+// up to 2^16 took sums past float32 from V's of 2^112 on.)  The price is at the other end: weights of
+// 2^-45 on leave 2^-126 for V's below 2^-64 to lose bits in.
+constexpr float kLargeSum = 0x1p-28f;
+constexpr float kReferenceAbove = 44.f;
 // The reference of rows that have seen no key: about the lowest number, so that masked logits
 // (-inf) weigh 0 and not NaN, and every other one is above it
 constexpr float kLowest = -0x1.fffffp127f;
@@ -458,8 +464,8 @@ struct Softmax {
   }
 
   // Adds the weights p of logits s to l, by their sum; where one is too large (the sum finds it as
-  // well as a maximum would, and is needed) m moves up to the largest logit, what there is so far
-  // (o) with it, and the weights are made anew
+  // well as a maximum would, and is needed) m moves to its place above the largest logit, what there is
+  // so far (o) with it, and the weights are made anew
   template <int kWords, typename O>
   __device__ __forceinline__ void add(float sum, const Logits& s, float c, O (&o)[kWords], bf16x8 (&p)[kRows / 16]) {
     if (__builtin_amdgcn_ballot_w64(sum > kLargeSum) != 0) {
@@ -469,7 +475,7 @@ struct Softmax {
       float a, b;
       swap32(top, a, b);
       top = kRows == 16 ? quad_max(top) : fmaxf(a, b);
-      const float m_new = fmaxf(m, ceilf(top * c));
+      const float m_new = fmaxf(m, ceilf(top * c) + kReferenceAbove);
       const float alpha = __builtin_amdgcn_exp2f(m - m_new);
       m = m_new;
       l *= alpha;
