@@ -791,7 +791,9 @@ int cs_kv_dequantize(const void *quant_pool, const int32_t *src_block_ids,
  * 2^-117, and then off by at most 2^-127.  (Query features from 1.8125 * 2^127 on count as
  * infinite.)  Probabilities are rounded to bf16 for the
  * product with V, the output to nearest-even bf16.  V of every size is added up without overflow; an
- * output of n keys is besides off by up to n * 2^-81.  A row's low bits may change with the rest of
+ * output of n keys is besides off by up to n * 2^-81.  Both hold for scaled logits up to 2^23; larger ones
+ * weigh as fp32 rounds them, and sums over V may overflow there from 2^127 / n on.  q . K and scale q . K
+ * log2(e) have to be fp32 numbers, or the row may be NaN.  A row's low bits may change with the rest of
  * the batch, as there; the result is the same from run to run.
  *
  * Arguments as in cs_paged_decode_attn_ws, except

@@ -45,6 +45,10 @@ constexpr int kThreads = 64 * kWaves;
 // 2^-45 on leave 2^-126 for V's below 2^-64 to lose bits in.
 constexpr float kLargeSum = 0x1p-28f;
 constexpr float kReferenceAbove = 44.f;
+// Past this a reference is no longer a whole number of any size, and a logit's product with the scale,
+// which the weights take unrounded, may be off the rounded one that the reference was found from by more
+// than float32's exponents: from 2^31 on the largest logit would weigh 2^128 or 2^-128
+constexpr float kFarReference = 0x1p24f;
 // The reference of rows that have seen no key: about the lowest number, so that masked logits
 // (-inf) weigh 0 and not NaN, and every other one is above it
 constexpr float kLowest = -0x1.fffffp127f;
@@ -446,6 +450,7 @@ template <int kRows>
 struct Softmax {
   typedef float Logits __attribute__((ext_vector_type(kRows / 2)));       // of 32 keys
   float m = kLowest, l = 0.f;
+  float limit = -1.f;       // kLargeSum, or below every sum while a row's m is past kFarReference; the wave's
 
   // Logits from .. to - 1 as weights, rounded to bf16 as operands; sum and theirs
   __device__ __forceinline__ float weigh(const Logits& s, float c, bf16x8 (&p)[kRows / 16], float sum = 0.f,
@@ -465,10 +470,11 @@ struct Softmax {
 
   // Adds the weights p of logits s to l, by their sum; where one is too large (the sum finds it as
   // well as a maximum would, and is needed) m moves to its place above the largest logit, what there is
-  // so far (o) with it, and the weights are made anew
+  // so far (o) with it, and the weights are made anew.  Rows with a reference that is far from 0 always
+  // come here: their weights are of the rounded products.
   template <int kWords, typename O>
   __device__ __forceinline__ void add(float sum, const Logits& s, float c, O (&o)[kWords], bf16x8 (&p)[kRows / 16]) {
-    if (__builtin_amdgcn_ballot_w64(sum > kLargeSum) != 0) {
+    if (__builtin_amdgcn_ballot_w64(sum > limit) != 0) {
       float top = s[0];
 #pragma unroll
       for (int i = 1; i < kRows / 2; ++i) top = fmaxf(top, s[i]);
@@ -482,6 +488,21 @@ struct Softmax {
 #pragma unroll
       for (int t = 0; t < kWords; ++t) o[t] *= alpha;
       sum = weigh(s, c, p);
+      const bool is_far = fabsf(m) > kFarReference;
+      limit = kLargeSum;
+      if (__builtin_amdgcn_ballot_w64(is_far) != 0) {
+#pragma clang fp contract(off)
+        limit = -1.f;
+        float far_sum = 0.f;
+#pragma unroll
+        for (int i = 0; i < kRows / 2; ++i) {
+          const float x = s[i] * c;
+          const __bf16 e = (__bf16)__builtin_amdgcn_exp2f(x - m);
+          if (is_far) p[i / 8][i % 8] = e;
+          far_sum += (float)e;
+        }
+        if (is_far) sum = far_sum;
+      }
     }
     l += sum;
   }

@@ -1,5 +1,5 @@
 """Attention over a pool held in 4 or 8 bits at the ends of the numbers' range: values near the
-format's largest and far below 1."""
+format's largest and far below 1, and logits past 2^31, where float32 holds no fractions."""
 
 import numpy as np
 import pytest
@@ -85,3 +85,49 @@ def test_small_values(d, bits, power):
     rng = pg.rng
     q, qp = bf16_bits(rng, len(invs), HQ, d), bf16_bits(rng, sum(s for _, s in invs), HQ, d)
     both(pg, q, qp, invs, bits, d, unit=2.0 ** power)
+
+
+def huge_logits(pg, d, rows, exponents, sign):
+    """Queries of one feature, so that a key's logit is that feature's product: K of +-2^e with e from
+    `exponents` by position.  Logits are then equal or at least twice as large, in any arithmetic."""
+    q = np.zeros((rows, HQ, d), dtype=np.uint16)
+    q[:, :, 0] = 0x3FB0 + (10 << 7)                      # 1.375 * 2^10
+    q[:, 1::2, 0] |= 0x8000
+    for r, n in enumerate(pg.lens):
+        for j in range(n):
+            e = exponents(j, n)
+            x = np.uint16((127 + e) << 7) | (0x8000 if sign(j) else 0)
+            pg.k[pg.tables[r, j // 16], :, j % 16, 0] = x
+    return q
+
+
+HUGE = {
+    "equal": (lambda j, n: 24, lambda j: False),
+    "equal, 2^31": (lambda j, n: 21, lambda j: False),
+    "equal and far": (lambda j, n: 100, lambda j: False),
+    "both signs": (lambda j, n: 30, lambda j: j % 5 == 2),
+    "rising": (lambda j, n: -20 + 80 * j // n, lambda j: False),
+    "falling": (lambda j, n: 60 - 80 * j // n, lambda j: False),
+    "mixed": (lambda j, n: 20 + j * 37 % 23, lambda j: j % 3 == 0),
+}
+
+
+@pytest.mark.parametrize("bits", [4, 8])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("name", list(HUGE))
+def test_logits_past_float32s_whole_numbers(name, d, bits):
+    """The result is the mean of V over the largest logit's keys (a single key's V where there is one)."""
+    exponents, sign = HUGE[name]
+    invs = [(0, 1), (0, 5), (300, 2), (900, 70)]
+    print(f"[case] huge logits, {name}, head_dim {d}, {bits} bits", flush=True)
+    pg = QuantPaged(53, [p + s for p, s in invs], HKV, d, bits)
+    q = huge_logits(pg, d, len(invs), exponents, sign)
+    qp = huge_logits(pg, d, sum(s for _, s in invs), exponents, sign)
+    pg.requantise(bits)
+    scale = float(np.float32(d ** -0.5))
+    got = run_decode(pg, q, bits, scale)
+    for r, n in enumerate(pg.lens):
+        compare(got[r:r + 1], q[r:r + 1], pg, r, int(n) - 1, d)
+    got, cu = run_prefill(pg, qp, invs, bits, scale)
+    for r, (p, s) in enumerate(invs):
+        compare(got[cu[r]:cu[r + 1]], qp[cu[r]:cu[r + 1]], pg, r, p, d)
