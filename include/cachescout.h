@@ -785,16 +785,12 @@ int cs_kv_dequantize(const void *quant_pool, const int32_t *src_block_ids,
  * Decode attention over a quantised pool: cs_paged_decode_attn_ws with K and V the values that
  * quant_pool holds.  The token's own K/V must already be there (cs_kv_write_quant).
  *
- * Arithmetic: fp32 logits, of bf16 products, or at 4 bits of the query's products with the codes:
- * a query feature is there held as two 8-bit numbers, exact unless it is more than 2^14 times
- * smaller than the largest of its group of 32, and then off by at most 2^-22 of that one, or below
- * 2^-117, and then off by at most 2^-127.  (Query features from 1.8125 * 2^127 on count as
- * infinite.)  Probabilities are rounded to bf16 for the
- * product with V, the output to nearest-even bf16.  V of every size is added up without overflow; an
- * output of n keys is besides off by up to n * 2^-81.  Both hold for scaled logits up to 2^23; larger ones
- * weigh as fp32 rounds them, and sums over V may overflow there from 2^127 / n on.  q . K and scale q . K
- * log2(e) have to be fp32 numbers, or the row may be NaN.  A row's low bits may change with the rest of
- * the batch, as there; the result is the same from run to run.
+ * Arithmetic: K and V as bf16, which holds their values exactly, fp32 logits; probabilities are rounded
+ * to bf16 for the product with V, the output to nearest-even bf16.  V of every size is added up without
+ * overflow, and an output of n keys is besides off by up to n * 2^-81, while scaled logits are at most
+ * 2^23; larger ones weigh as fp32 rounds them, and sums over V may overflow there from 2^127 / n on.
+ * q . K and scale q . K log2(e) have to be fp32 numbers, or the row may be NaN.  A row's low bits may
+ * change with the rest of the batch, as there; the result is the same from run to run.
  *
  * Arguments as in cs_paged_decode_attn_ws, except
  *   quant_pool     device, as above, of num_blocks blocks of `bits` (4 or 8) bits.
@@ -804,6 +800,7 @@ int cs_kv_dequantize(const void *quant_pool, const int32_t *src_block_ids,
  *   workspace,
  *   workspace_bytes  sized by cs_decode_quant_workspace_bytes.
  * Batches of any size share the device; what a pool holds behind a sequence's end is not used.
+ * Sequences that share blocks may stand in any order, but are faster next to each other.
  */
 int cs_decode_quant_attn(const void *q, const void *quant_pool, const int32_t *block_tables,
                          const int32_t *seq_lens, int32_t batch, int32_t max_seq_len,

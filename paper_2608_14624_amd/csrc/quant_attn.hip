@@ -8,16 +8,13 @@
 // V^T operand takes them in too, and the tile's layout (quant_tile.h) gives K and V to the lanes
 // that need them.  Decode works on 16 rows (the heads of a KV head), each wave on
 // keys of its own; prefill works on 32 rows a wave and shares conversions through LDS.
-//   * 4 bits: K goes into the matrix unit as it is (v_mfma_scale_f32_*_f8f6f4, codes and scales
-//     from the pool).  Its partner then has to be of 8 bits or fewer: Q is the sum of two E4M3
-//     numbers with scales of their own, which holds bf16's 8 bits (a 4-bit head and what is left,
-//     of 4 bits again); features more than 2^14 below the largest of their group of 32 are off by
-//     2^-22 of that largest at most.  In 16 x 16 products at D = 64 the two halves of the
-//     contracted index hold the head and the rest, so it is one product.
-//   * 8 bits: K is converted to bf16.  (8-bit times 8-bit products sum up with errors of 3e-5 of
-//     the largest, where 4-bit times 8-bit ones are exact to fp32's 5e-8.)
-//   * V is converted to bf16, two features of a key at a time, which two byte permutes then
-//     pair up by keys.
+// K and V are converted to bf16, V two features of a key at a time, which two byte permutes then pair
+// up by keys.  The unit's products of 4- and 8-bit codes (v_mfma_scale_f32_*_f8f6f4) would take K as it
+// is, but where an operand is E4M3 they sum the 32 products of a group without what lies 2^14 below the
+// largest of them: with Q in two E4M3 parts, logits beside a product of 4096 were off by 0.1.  Q in four E2M3
+// parts, whose sums with E2M1 codes are exact, takes as long as the conversions (4 x 512 rows on 4096 keys,
+// 64 / 8 heads of 128, 4 bits: 260 us and 264; with the two E4M3 parts 242).
+//
 // The reference that the exponentials are relative to follows the logits only when the weights of a
 // lane's keys have become 2^16 times as large as it left them: bf16 holds numbers of any size, and most
 // steps rescale nothing, look for no maximum and exchange nothing between lanes.
@@ -32,7 +29,6 @@
 namespace cs {
 namespace {
 
-typedef int i32x8 __attribute__((ext_vector_type(8)));
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
 
@@ -79,11 +75,8 @@ struct QuantParams {
 // Query rows
 
 // 16 rows as the B operand: lane l holds row l & 15 (`row`, null: zeros), quarter l >> 4.
-template <int D, int kBits>
-struct Rows16;
-
 template <int D>
-struct Rows16<D, 8> {
+struct Rows16 {
   bf16x8 q[D / 32];
   __device__ __forceinline__ void load(const uint16_t* row, int lane) {
     // step s of the contracted index: features (D / 4) qd + 8 s .. + 7, as K's lanes hold them
@@ -95,102 +88,9 @@ struct Rows16<D, 8> {
   }
 };
 
-// the largest magnitude of 16 features
-__device__ __forceinline__ unsigned top_of(const u32x4 (&x)[2]) {
-  unsigned top = 0;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const unsigned w = x[i / 4][i % 4];
-    top = max(top, max(w & 0x7fffu, (w >> 16) & 0x7fffu));
-  }
-  return top;
-}
-
-// 16 features as E4M3 heads times `scale` and what is left times scale / 16
-__device__ __forceinline__ void split16(const u32x4 (&x)[2], float scale, int* head, int* rest) {
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    i16_pair h = {0, 0}, r = {0, 0};
-#pragma unroll
-    for (int p = 0; p < 2; ++p) {
-      const uint32_t w = x[i / 2][2 * (i % 2) + p];
-      h = p ? __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(h, as_pair(w), scale, true)
-            : __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(h, as_pair(w), scale, false);
-      const uint32_t back = read_pair<8>(__builtin_bit_cast(uint32_t, h), scale, p);
-      const float a = __builtin_bit_cast(float, w << 16) - __builtin_bit_cast(float, back << 16);
-      const float b = __builtin_bit_cast(float, w & 0xffff0000u) - __builtin_bit_cast(float, back & 0xffff0000u);
-      r = p ? __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(r, a, b, scale * 0.0625f, true)
-            : __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(r, a, b, scale * 0.0625f, false);
-    }
-    head[i] = __builtin_bit_cast(int, h);
-    rest[i] = __builtin_bit_cast(int, r);
-  }
-}
-
-// The scale byte of a group of a query: E4M3's, with room for the rest's below it.
-__device__ __forceinline__ int query_scale(unsigned top) { return max(scale_byte<128, 8>(top), 14); }
-
-template <int D>
-struct Rows16<D, 4> {
-  // D = 128: [0] the heads, [1] the rests; D = 64: both in one
-  i32x8 q[D / 64];
-  int scale[D / 64];
-  __device__ __forceinline__ void load(const uint16_t* row, int lane) {
-    const int qd = lane >> 4;
-    // the 8-bit operand's lane holds indices 16 qd .. + 15 and 64 + 16 qd .. + 15
-    u32x4 x[D / 64][2];
-#pragma unroll
-    for (int s = 0; s < D / 64; ++s)
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        x[s][i] = u32x4{};
-        if (row != nullptr) x[s][i] = *reinterpret_cast<const u32x4*>(row + 64 * s + 16 * qd + 8 * i);
-      }
-    // the group's other 16 features are lane qd ^ 1's
-    int byte[D / 64];
-#pragma unroll
-    for (int s = 0; s < D / 64; ++s) {
-      unsigned top = top_of(x[s]);
-      top = max(top, (unsigned)__shfl_xor((int)top, 16));
-      byte[s] = query_scale(top);
-    }
-#pragma unroll
-    for (int s = 0; s < D / 64; ++s) {
-      int head[4], rest[4];
-      // (a group that is not finite is NaN by its scale; its codes do not matter)
-      split16(x[s], byte[s] == kNanScale ? 1.f : scale_of(byte[s]), head, rest);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        if constexpr (D == 128) {
-          q[0][4 * s + i] = head[i];
-          q[1][4 * s + i] = rest[i];
-        } else {
-          q[0][i] = head[i];
-          q[0][4 + i] = rest[i];
-        }
-      }
-    }
-    // lane qd supplies the scale of indices 32 qd .. + 31: at D = 128 of group qd, whose lanes are
-    // 2 qd and 2 qd + 1 (mod 4); at D = 64 of the heads' group qd or the rests' group qd - 2
-    const int from = (lane & 15) + 16 * (2 * qd & 3);
-    const int first = __shfl(byte[0], from);
-    if constexpr (D == 128) {
-      const int second = __shfl(byte[1], from);
-      const int b = qd < 2 ? first : second;
-      scale[0] = b;
-      scale[1] = b == kNanScale ? b : b - 4;
-    } else {
-      scale[0] = qd < 2 || first == kNanScale ? first : first - 4;
-    }
-  }
-};
-
 // 32 rows as the B operand of 32 x 32 products: lane l holds row l & 31, half l >> 5.
-template <int D, int kBits>
-struct Rows32;
-
 template <int D>
-struct Rows32<D, 8> {
+struct Rows32 {
   bf16x8 q[D / 16];
   __device__ __forceinline__ void load(const uint16_t* row, int lane) {
     // step s of the contracted index: features (D / 2) half + 8 s .. + 7, as K's lanes take them
@@ -202,44 +102,6 @@ struct Rows32<D, 8> {
   }
 };
 
-template <int D>
-struct Rows32<D, 4> {
-  // of 64 features each the heads, [0], and the rests, [1]
-  i32x8 q[D / 64][2];
-  int scale[D / 64][2];
-  __device__ __forceinline__ void load(const uint16_t* row, int lane) {
-    const int half = lane >> 5;
-#pragma unroll
-    for (int f = 0; f < D / 64; ++f) {
-      // the 8-bit operand's lane holds indices 16 half .. + 15 of both groups of 32
-      u32x4 x[2][2];
-      int byte[2];
-#pragma unroll
-      for (int g = 0; g < 2; ++g) {
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          x[g][i] = u32x4{};
-          if (row != nullptr) x[g][i] = *reinterpret_cast<const u32x4*>(row + 64 * f + 32 * g + 16 * half + 8 * i);
-        }
-        unsigned top = top_of(x[g]);
-        top = max(top, (unsigned)__shfl_xor((int)top, 32));
-        byte[g] = query_scale(top);
-        int head[4], rest[4];
-        split16(x[g], byte[g] == kNanScale ? 1.f : scale_of(byte[g]), head, rest);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          q[f][0][4 * g + i] = head[i];
-          q[f][1][4 * g + i] = rest[i];
-        }
-      }
-      // and the scale of indices 32 half .. + 31
-      const int b = half ? byte[1] : byte[0];
-      scale[f][0] = b;
-      scale[f][1] = b == kNanScale ? b : b - 4;
-    }
-  }
-};
-
 // ---------------------------------------------------------------------------
 // Keys
 
@@ -247,7 +109,7 @@ struct Rows32<D, 4> {
 template <int D, int kBits>
 struct Block {
   using T = QuantTile<D, kBits>;
-  static constexpr int kKWords = kBits == 4 ? 4 : D / 16;      // a lane's codes of K, in words
+  static constexpr int kKWords = D / 4 * kBits / 32;           // a lane's codes of K, in words
   static constexpr int kVWords = T::kPartBytes;                // of V: 4 keys of kPartBytes
   uint32_t k[kKWords];
   uint32_t v[kVWords];
@@ -279,15 +141,8 @@ struct Block {
   template <int kPolicy = 0>
   __device__ __forceinline__ void load_keys(__amdgpu_buffer_rsrc_t rs, int lane) {
     const int key = lane & 15, qd = lane >> 4;
-    int k_off, ks_off;
-    if constexpr (kBits == 4) {
-      const int g = D == 128 ? qd : qd & 1;      // D = 64: indices 64 .. 127 are the same keys again
-      k_off = key * T::kRowBytes + 16 * g;
-      ks_off = T::kKScales + key * T::kGroups + g;
-    } else {
-      k_off = key * T::kRowBytes + D / 4 * qd;
-      ks_off = T::kKScales + key * T::kGroups + qd * T::kGroups / 4;
-    }
+    const int k_off = key * T::kRowBytes + T::kRowBytes / 4 * qd;
+    const int ks_off = T::kKScales + key * T::kGroups + qd * T::kGroups / 4;
     load_words<kPolicy>(k, rs, k_off);
     ks = __builtin_amdgcn_raw_buffer_load_b8(rs, ks_off, 0, 0);
   }
@@ -361,23 +216,25 @@ struct Block {
       }
   }
 
-  // S^T of the block's keys and 16 rows: lane l has row l & 15 and keys 4 (l >> 4) .. + 3
-  __device__ __forceinline__ f32x4 logits(const Rows16<D, kBits>& rows) const {
-    f32x4 s = f32x4{};
+  // The lane's features 8 i .. + 7 of its key as bf16
+  __device__ __forceinline__ u32x4 key_features(int i, float scale) const {
     if constexpr (kBits == 4) {
-      const i32x8 a = {(int)k[0], (int)k[1], (int)k[2], (int)k[3], 0, 0, 0, 0};
-#pragma unroll
-      for (int i = 0; i < D / 64; ++i)
-        s = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, rows.q[i], s, 4, 0, 0, ks, 0, rows.scale[i]);
+      return u32x4{read_pair<4>(k[i], scale, 0), read_pair<4>(k[i], scale, 1), read_pair<4>(k[i], scale, 2),
+                   read_pair<4>(k[i], scale, 3)};
     } else {
-      const float scale = scale_of(ks);
-#pragma unroll
-      for (int i = 0; i < D / 32; ++i) {
-        const u32x4 a = {read_pair<8>(k[2 * i], scale, 0), read_pair<8>(k[2 * i], scale, 1),
-                         read_pair<8>(k[2 * i + 1], scale, 0), read_pair<8>(k[2 * i + 1], scale, 1)};
-        s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), rows.q[i], s, 0, 0, 0);
-      }
+      return u32x4{read_pair<8>(k[2 * i], scale, 0), read_pair<8>(k[2 * i], scale, 1),
+                   read_pair<8>(k[2 * i + 1], scale, 0), read_pair<8>(k[2 * i + 1], scale, 1)};
     }
+  }
+
+  // S^T of the block's keys and 16 rows: lane l has row l & 15 and keys 4 (l >> 4) .. + 3
+  __device__ __forceinline__ f32x4 logits(const Rows16<D>& rows) const {
+    f32x4 s = f32x4{};
+    const float scale = scale_of(ks);
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i)
+      s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, key_features(i, scale)), rows.q[i], s, 0,
+                                                  0, 0);
     return s;
   }
 
@@ -512,7 +369,7 @@ struct Softmax {
 // first `seen`.  Lane l has of row l & 15 O's features D / 4 qd + D / 16 r + t in o[t][r].
 template <int D, int kBits>
 __device__ __forceinline__ void add_unit(Softmax<16>& soft, f32x4 (&o)[D / 16], const Unit<D, kBits>& u,
-                                         const Rows16<D, kBits>& rows, float c, int seen, int lane) {
+                                         const Rows16<D>& rows, float c, int seen, int lane) {
   Softmax<16>::Logits s;
 #pragma unroll
   for (int b = 0; b < 2; ++b) {
@@ -651,7 +508,7 @@ __global__ __launch_bounds__(kThreads, kDecodeGroupsPerCu) void quant_decode_ker
       left -= xe - x;
       const ScalarInts table = (ScalarInts)(p.block_tables + (size_t)r * p.max_blocks_per_seq);
       const int last = (len - 1) / kBlock;
-      Rows16<D, kBits> rows;
+      Rows16<D> rows;
       rows.load(j < p.group ? p.q + ((size_t)r * p.num_q_heads + g * p.group + j) * D : nullptr, lane);
       Softmax<16> soft;
       f32x4 o[D / 16];
@@ -765,21 +622,21 @@ __global__ __launch_bounds__(kMergeThreads) void quant_decode_merge_kernel(Quant
 // Prefill.  Rows of a KV head are (token, query head of it), heads fastest; a wave takes 32 of them,
 // or at D = 64, where the launch fills the device so, 64 (kTiles).  A work-group's steps are 64
 // keys: each wave reads one of the four blocks ahead into registers, and a step later leaves it in
-// LDS as all waves then take it, K's 4-bit codes as they are, 8-bit K and V as bf16 fragments, so that
-// a conversion is done once for the work-group's rows.  A step's buffer is written while the other
-// one is read: one barrier a step.
+// LDS as all waves then take it, K and V as bf16 fragments, so that a conversion is done once for the
+// work-group's rows.  A step's buffer is written while the other one is read: one barrier a step.
 //
 // Within a wave the logits of the next 32 keys, the weights of the present ones and the values of the
 // last 32 stand side by side, so that the matrix unit's work does not depend on the vector unit's.
 // Several parts of a tile's keys on as many work-groups leave partial results.
 //
-// us a call: 64 / 8 heads of 128, 4 x (4096 + 512), 4 bits 247 (1.18 PFLOP/s; a large bf16 product of
-// the library reaches 1.24); 32 / 8 heads, 16 ragged invocations, 8 bits 1003 (0.93).  Bound by the step's
-// own work: of 305 us in short runs of the first the products alone take 135, and all but the
-// products 177 (LDS reads and barriers 95, weights 47, conversions and their loads and stores 34),
-// which overlap little.  Each wave converting all for itself took 317 and 2850; 16 x 16 products,
-// three waves a SIMD and, at D = 128, 64 rows a wave (O in accumulation registers) were as fast or
-// slower; loads one more step ahead, the rows' all at once, are within 1% both ways.  Of a small launch
+// us a call: 64 / 8 heads of 128, 4 x (4096 + 512), 264 at 4 bits (1.11 PFLOP/s; a large bf16 product of
+// the library reaches 1.24), 286 at 8; heads of 64 149 and 152; 32 / 8 heads, 16 ragged invocations, 8 bits
+// 1005 (0.93).
+// Bound by the step's own work: the 264 are 249 without the exponentials, 225 without the conversions and
+// their stores, 215 without LDS reads, and 203 without the products.  Each wave converting all for itself
+// took 317 and 2850; 16 x 16 products, three waves a SIMD and, at D = 128, 64 rows a wave (O in
+// accumulation registers) were as fast or slower; loads one more step ahead, the rows' all at once, and K's
+// fragments read a chunk ahead like V's are within 1% both ways.  Of a small launch
 // (83 rows x 32 / 8 heads on 3094 keys, 21 us in this kernel) a wave alone on its SIMD takes 1.3 us a
 // step, 6 to get to the second step, and 4 to store its partial results.
 
@@ -790,9 +647,8 @@ constexpr int kStepKeys = 16 * kStepBlocks;
 // values of blocks 4 x - 2 .. 4 x + 1.
 template <int D, int kBits>
 struct PrefillLds {
-  // of K at 4 bits lane by lane what Block holds, at 8 bits fragments of 16 keys; V^T fragments
-  u32x4 k[2][kStepBlocks][kBits == 4 ? 1 : D / 32][64];
-  int ks[2][kBits == 4 ? kStepBlocks : 1][64];
+  // fragments of K, 16 keys, and of V^T
+  u32x4 k[2][kStepBlocks][D / 32][64];
   u32x4 v[2][kStepBlocks][D / 32][64];
 };
 
@@ -849,20 +705,13 @@ __global__ __launch_bounds__(kThreads, kTiles == 1 ? 2 : 1) void quant_prefill_k
     block.load_values(Block<D, kBits>::tile(base, stride, v_id), lane);
   };
   auto store_keys = [&](int step) __attribute__((always_inline)) {
-    if constexpr (kBits == 4) {
-      sm.k[step & 1][wave][0][lane] = u32x4{block.k[0], block.k[1], block.k[2], block.k[3]};
-      sm.ks[step & 1][wave][lane] = block.ks;
-    } else {
-      // lane (key, qd)'s features D / 4 qd + 8 i .. + 7: step s of the products, half h of the wave
-      const float scale = scale_of(block.ks);
-      const int qd = lane >> 4;
+    // lane (key, qd)'s features D / 4 qd + 8 i .. + 7: step s of the products, half h of the wave
+    const float scale = scale_of(block.ks);
+    const int qd = lane >> 4;
 #pragma unroll
-      for (int i = 0; i < D / 32; ++i) {
-        const int step8 = qd % 2 * (D / 32) + i;
-        (&sm.k[step & 1][wave][0][0])[(step8 * 2 + qd / 2) * 16 + (lane & 15)] =
-            u32x4{read_pair<8>(block.k[2 * i], scale, 0), read_pair<8>(block.k[2 * i], scale, 1),
-                  read_pair<8>(block.k[2 * i + 1], scale, 0), read_pair<8>(block.k[2 * i + 1], scale, 1)};
-      }
+    for (int i = 0; i < D / 32; ++i) {
+      const int step8 = qd % 2 * (D / 32) + i;
+      (&sm.k[step & 1][wave][0][0])[(step8 * 2 + qd / 2) * 16 + (lane & 15)] = block.key_features(i, scale);
     }
   };
   // Of a 32 x 16 fragment of V^T lane l holds feature group l & 31, D / 32 features each in as many
@@ -887,16 +736,13 @@ __global__ __launch_bounds__(kThreads, kTiles == 1 ? 2 : 1) void quant_prefill_k
   };
 
   if (x0 < xe) load(x0 - 1, x0);
-  long long q_row[kTiles];      // of q and out; negative: none
-  int end[kTiles];              // keys that the row sees
-  Rows32<D, kBits> rows[kTiles];
+  Rows32<D> rows[kTiles];
 #pragma unroll
   for (int x = 0; x < kTiles; ++x) {
     const int row = row0 + 32 * x + (lane & 31);
     const int t = (unsigned)row / group;
-    q_row[x] = row < n_rows ? (long long)(q0 + t) * p.num_q_heads + g * p.group + (row - t * p.group) : -1;
-    end[x] = before + min(t, t1) + 1;
-    rows[x].load(row < n_rows ? p.q + q_row[x] * D : nullptr, lane);
+    const long long q_row = (long long)(q0 + t) * p.num_q_heads + g * p.group + (row - t * p.group);
+    rows[x].load(row < n_rows ? p.q + q_row * D : nullptr, lane);
   }
   // lane l has of row l & 31 and with h = l >> 5 the weights of keys 8 i + 4 h .. + 3 and O's
   // features of groups 8 i + 4 h .. + 3, i < 4
@@ -910,43 +756,25 @@ __global__ __launch_bounds__(kThreads, kTiles == 1 ? 2 : 1) void quant_prefill_k
   auto barrier = [&]() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); };
   // of the buffer's blocks 2 half and 2 half + 1
   const int key = lane & 15, k_block = lane >> 4 & 1, k_half = lane >> 5;
-  // The work of half a step comes in as many chunks as its logits take products of 64 cycles.
+  // The work of half a step comes in chunks, each of two products for the logits and two for the values.
   constexpr int kChunks = D / 32;
   struct Keys {
-    u32x4 w[kBits == 4 ? kChunks / 2 : 2 * kChunks];
-    int ks[kBits == 4 ? kChunks / 2 : 1];
+    u32x4 w[2 * kChunks];
   };
   auto read_keys = [&](int step, int half) __attribute__((always_inline)) {
     const int buf = step & 1, b = 2 * half + k_block;
     Keys k;
-    if constexpr (kBits == 4) {
 #pragma unroll
-      for (int f = 0; f < D / 64; ++f) {
-        k.w[f] = sm.k[buf][b][0][(2 * f + k_half) * 16 + key];
-        k.ks[f] = sm.ks[buf][b][(2 * f + k_half) * 16 + key];
-      }
-    } else {
-#pragma unroll
-      for (int i = 0; i < D / 16; ++i) k.w[i] = (&sm.k[buf][b][0][0])[(2 * i + k_half) * 16 + key];
-    }
+    for (int i = 0; i < D / 16; ++i) k.w[i] = (&sm.k[buf][b][0][0])[(2 * i + k_half) * 16 + key];
     return k;
   };
   auto add_logits = [&](int chunk, const Keys& k, Logits (&s)[kTiles]) __attribute__((always_inline)) {
-    if constexpr (kBits == 4) {
-      const u32x4 w = k.w[chunk / 2];
-      const i32x8 a = {(int)w[0], (int)w[1], (int)w[2], (int)w[3], 0, 0, 0, 0};
+#pragma unroll
+    for (int e = 2 * chunk; e < 2 * chunk + 2; ++e) {
+      const u32x4 a = k.w[e];
 #pragma unroll
       for (int x = 0; x < kTiles; ++x)
-        s[x] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, rows[x].q[chunk / 2][chunk % 2], s[x], 4, 0, 0,
-                                                               k.ks[chunk / 2], 0, rows[x].scale[chunk / 2][chunk % 2]);
-    } else {
-#pragma unroll
-      for (int e = 2 * chunk; e < 2 * chunk + 2; ++e) {
-        const u32x4 a = k.w[e];
-#pragma unroll
-        for (int x = 0; x < kTiles; ++x)
-          s[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), rows[x].q[e], s[x], 0, 0, 0);
-      }
+        s[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), rows[x].q[e], s[x], 0, 0, 0);
     }
   };
   auto read_values = [&](int step, int half, int i) {
@@ -964,9 +792,14 @@ __global__ __launch_bounds__(kThreads, kTiles == 1 ? 2 : 1) void quant_prefill_k
     const int key0 = x * kStepKeys + 32 * half;
     if (key0 + 32 > before + t0 + 1) {
 #pragma unroll
-      for (int y = 0; y < kTiles; ++y)
+      for (int y = 0; y < kTiles; ++y) {
+        // keys that the row sees (found anew here: few steps are masked, and registers are short)
+        int first = row0 + 32 * y;
+        asm volatile("" : "+s"(first));
+        const int end = before + min((int)((unsigned)(first + (lane & 31)) / group), t1) + 1;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) s[y][i] = key0 + 8 * (i / 4) + 4 * k_half + i % 4 < end[y] ? s[y][i] : -INFINITY;
+        for (int i = 0; i < 16; ++i) s[y][i] = key0 + 8 * (i / 4) + 4 * k_half + i % 4 < end ? s[y][i] : -INFINITY;
+      }
     }
     // Chunk by chunk, so that a fragment is read one chunk before its products and few are held at a
     // time (the order within a chunk makes no difference that was measured)
@@ -1035,7 +868,12 @@ __global__ __launch_bounds__(kThreads, kTiles == 1 ? 2 : 1) void quant_prefill_k
     float la, lb;
     swap32(soft[x].l, la, lb);
     const float l = la + lb;
-    if (q_row[x] < 0) continue;
+    int row = row0 + 32 * x;
+    asm volatile("" : "+s"(row));
+    row += lane & 31;
+    if (row >= n_rows) continue;
+    const int t = (unsigned)row / group;
+    const long long q_row = (long long)(q0 + t) * p.num_q_heads + g * p.group + (row - t * p.group);
     // D / 8 neighbouring features for each i, feature k of them in o[k % (D / 32)]
     if (p.parts == 1) {
       const float inv_l = 1.f / l;
@@ -1046,10 +884,10 @@ __global__ __launch_bounds__(kThreads, kTiles == 1 ? 2 : 1) void quant_prefill_k
           bf16x8 y;
 #pragma unroll
           for (int e = 0; e < 8; ++e) y[e] = (__bf16)(o[x][(k + e) % (D / 32)][4 * i + (k + e) / (D / 32)] * inv_l);
-          *reinterpret_cast<bf16x8*>(p.out + q_row[x] * D + D / 4 * i + D / 8 * k_half + k) = y;
+          *reinterpret_cast<bf16x8*>(p.out + q_row * D + D / 4 * i + D / 8 * k_half + k) = y;
         }
     } else {
-      const size_t to = (size_t)part * p.total_q * p.num_q_heads + q_row[x];
+      const size_t to = (size_t)part * p.total_q * p.num_q_heads + q_row;
 #pragma unroll
       for (int i = 0; i < 4; ++i)
 #pragma unroll

@@ -17,10 +17,10 @@ HQ, HKV = 8, 2
 
 
 def scaled(bits, power):
-    """bf16 bits of numbers times 2^power, exactly; zeros and NaN as they are."""
-    x = bits.copy()
-    x[((bits & 0x7F80) != 0) & ((bits & 0x7F80) != 0x7F80)] += np.uint16(power << 7 & 0xFFFF)
-    return x
+    """bf16 bits of numbers times 2^power, exactly, but for those that would be subnormal: zeros; NaN as it is."""
+    exponent = (bits >> 7 & 0xFF).astype(np.int32)
+    x = np.where(exponent + power > 0, bits + np.uint16(power << 7 & 0xFFFF), bits & 0x8000)
+    return np.where((exponent == 0) | (exponent == 255), bits, x).astype(np.uint16)
 
 
 def compare(got, q, pg, r, first, d, unit=1.0):
@@ -131,3 +131,35 @@ def test_logits_past_float32s_whole_numbers(name, d, bits):
     got, cu = run_prefill(pg, qp, invs, bits, scale)
     for r, (p, s) in enumerate(invs):
         compare(got[cu[r]:cu[r + 1]], qp[cu[r]:cu[r + 1]], pg, r, p, d)
+
+
+@pytest.mark.parametrize("bits", [4, 8])
+@pytest.mark.parametrize("d", [64, 128])
+def test_a_large_feature_that_all_keys_share(d, bits):
+    """A channel of 32 in every key and of +-128 in every query, as biased projections have them: its
+    product, 4096, is the same for all keys, and the 31 features of its group decide the weights.  A logit is a sum of
+    up to 128 products that fp32 holds to 2^-24 of some 2^13 each, 2^-4 scale at the worst."""
+    scale = float(np.float32(d ** -0.5))
+    print(f"[case] a large shared feature, head_dim {d}, {bits} bits", flush=True)
+    invs = [(600, 40), (0, 33), (2000, 3)]
+    pg = QuantPaged(55, [p + s for p, s in invs], HKV, d, bits)
+    rng = pg.rng
+    pg.k[..., 1:32] = scaled(pg.k[..., 1:32], 3)
+    pg.k[..., 0] = np.where(pg.k[..., 0] == 0x7FC0, pg.k[..., 0], 0x4200)
+    pg.requantise(bits)
+    q, qp = bf16_bits(rng, len(invs), HQ, d), bf16_bits(rng, sum(s for _, s in invs), HQ, d)
+    for x in (q, qp):
+        x[..., 0] = 0x4300 | (x[..., 0] & 0x8000)
+
+    def check(got, q, r, first):
+        slack = np.expm1(2 * scale * 2.0 ** -4)
+        out, mag = window_attention(q, pg.k, pg.v, pg.tables[r], first, HQ, HKV, scale)
+        worst = float((np.abs(got - out) / (quant_attention_bound(out, mag) + slack * (mag + np.abs(out)))).max())
+        assert worst <= 1, f"{worst} of the bound"
+
+    got = run_decode(pg, q, bits, scale)
+    for r, n in enumerate(pg.lens):
+        check(got[r:r + 1], q[r:r + 1], r, int(n) - 1)
+    got, cu = run_prefill(pg, qp, invs, bits, scale)
+    for r, (p, _) in enumerate(invs):
+        check(got[cu[r]:cu[r + 1]], qp[cu[r]:cu[r + 1]], r, p)
