@@ -1470,7 +1470,6 @@ int cs_prefill_quant_attn(const void* q, const void* quant_pool, const int32_t* 
   a.out = static_cast<uint16_t*>(out);
   a.batch = batch;
   a.total_q = total_q;
-  a.max_q_len = max_q_len;
   a.max_blocks_per_seq = max_blocks_per_seq;
   a.num_q_heads = num_q_heads;
   a.num_kv_heads = num_kv_heads;

@@ -256,7 +256,6 @@ struct QuantAttnLaunch {
   uint16_t* out;
   int batch;
   int total_q;
-  int max_q_len;
   int max_blocks_per_seq;
   int num_q_heads;
   int num_kv_heads;

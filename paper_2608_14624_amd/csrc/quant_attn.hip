@@ -405,7 +405,7 @@ __device__ __forceinline__ void add_unit(Softmax<16>& soft, f32x4 (&o)[D / 16], 
 // head in equal contiguous ranges.  A work-group's waves take the units of a piece (a sequence's
 // part of the range) in turn and merge in LDS; a sequence cut over several ranges leaves partial
 // results (O relative to m, m, and l) that a second kernel merges.  Bound by HBM: 128 sequences of 4.2k-10.8k
-// keys, 32 / 8 heads of 128, take 172 us at 4 bits (1.08 GB, 6.2 TB/s), 320 at 8 (6.5).  Where sequences
+// keys, 32 / 8 heads of 128, take 173 us at 4 bits (1.08 GB, 6.2 TB/s), 320 at 8 (6.5).  Where sequences
 // share anchors, by conversions and products: 64 / 8 heads, 61 sequences, 8 bits, 65 us (73 where the caches
 // are cold), of which all but the loads 52; with every anchor in L2 61.
 
@@ -426,7 +426,10 @@ struct DecodeLds {
 };
 
 // How many sequences hold the block at index 31 that the one before them holds: a batch's agents'
-// sequences usually stand together, and a prefix that short is not worth asking for.
+// sequences usually stand together, and a prefix that short is not worth asking for.  Where they do not
+// stand together their blocks are loaded as read once.  us a call by agents and in random order: the 61
+// sequences of 4 agents below, three states in turn, 79 and 84 at 8 bits, 51 and 52 at 4; 128 of 8 agents, 32 / 8
+// heads of 64, 8 bits, 60 and 65.  Asking for every pair among 64 sequences took 10 us more in any order.
 constexpr int kProbeBlock = 31;
 __device__ __forceinline__ int count_sharing(const QuantParams& p, int lane) {
   int count = 0;
@@ -1016,7 +1019,9 @@ hipError_t launch_quant_decode(const QuantAttnLaunch& a, const QuantDecodeGeomet
 }
 
 constexpr int kPrefillMaxParts = 16;
-// fewest steps of a part of the longest sequence: work-groups start and merge for about the time of 30
+// Fewest steps of a part of the longest sequence.  A part's work-group takes about 10 us besides its steps of
+// 1.3 (6 to the second step, 4 to store), and the merge launch 4.5 once.  us a call of 83 rows x 32 / 8 heads on 3094
+// keys with 3, 4, 6, 8, 12 and 24: 29, 29.6, 25.5, 25.7, 28 and 38.
 constexpr int kPrefillPartSteps = 6;
 
 QuantPrefillGeometry quant_prefill_geometry(int batch, int total_q, int max_q_len, int max_kv_len,
